@@ -579,6 +579,116 @@ f8_status f8_rmsnorm_bwd_add(const void* x_bf16, const void* g_bf16, const float
                              float* amax_dx_inout, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The residual sum of a block's branch with the norms before and after it, its
+ * gate and its scales, in one pass:
+ *   u = y * rstd_post * g_post   rstd_post[m] = 1 / sqrt(mean_d y[m, d]^2 + eps)
+ *                                (g_post NULL: u = y)
+ *   h = bf16(skip_scale * x + branch_scale * gate * u)   (gate NULL: 1)
+ *   n = h * rstd_pre * g_pre     rstd_pre of the h that is kept, in bf16
+ *                                (g_pre NULL: no n; n NULL too)
+ * x (the residual stream), y (the branch's output), h, n: [M, D] bf16 with their
+ * row pitches; g_post, g_pre [D] bf16; gate [gate_rows, D] bf16 packed, row m
+ * taking gate row m / (M / gate_rows): 1 for a gate per channel, the number of
+ * sequences for one per sequence, M for one per token; gate_rows 0 with gate
+ * NULL.  rstd_post, rstd_pre (nullable) [M] fp32, kept for the backward.
+ * amax_n (nullable, 1 float): exact maximum magnitude of the bf16 values of n,
+ * for f8_linear_fwd_chained (workspace, only then: f8_workspace_bytes(M, D)).
+ * fp32 arithmetic, h and n rounded once.  Without g_post and gate and with both
+ * scales 1 the results are those of f8_add followed by f8_rmsnorm, bit for bit.
+ * h may be x or y, and n may be y, at the same pitch; no other overlaps.
+ * Any M >= 0; D and the pitches multiples of 8, D <= 16384; eps >= 0.
+ *
+ * f8_residual_norm_bwd: with t = dh + (gradient of h through n),
+ *   dx = skip_scale * t,  v = branch_scale * gate * t (the gradient of u),
+ *   dy = v through the norm of y (v itself without g_post),
+ *   dgate[r] = sum over the rows of gate row r of branch_scale * t * u,
+ *   dg_post = sum_m v * y * rstd_post,  dg_pre = sum_m dn * h * rstd_pre
+ * dh, dn: gradients of h and n (dn with g_pre only; dh may be NULL then).  h is
+ * read with g_pre, y with g_post or a gate (NULL is allowed otherwise).  dx, dy
+ * [M, D] bf16, dg_post, dg_pre [D] and dgate [gate_rows, D] fp32: each may be
+ * NULL, not all.  amax_dy (nullable, 1 float): exact maximum magnitude of dy,
+ * for f8_linear_bwd_chained.  dx may be dh or dn and dy may be dh, dn, h or y, at
+ * the same pitch; dx and dy are apart.  Sums over rows are taken in a fixed
+ * order (results are reproducible).  workspace (with any dg, dgate or amax_dy):
+ * f8_residual_norm_bwd_workspace_bytes.
+ */
+f8_status f8_residual_norm(const void* x_bf16, int64_t ldx, const void* y_bf16, int64_t ldy, int64_t M, int64_t D,
+                           const void* g_post_bf16, const void* gate_bf16, int64_t gate_rows, const void* g_pre_bf16,
+                           float skip_scale, float branch_scale, float eps, void* h_bf16, int64_t ldh, void* n_bf16,
+                           int64_t ldn, float* rstd_post, float* rstd_pre, float* amax_n, void* workspace,
+                           size_t workspace_bytes, void* stream);
+f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf16, int64_t ldy, const void* dh_bf16,
+                               int64_t lddh, const void* dn_bf16, int64_t lddn, int64_t M, int64_t D,
+                               const void* g_post_bf16, const void* gate_bf16, int64_t gate_rows, const void* g_pre_bf16,
+                               const float* rstd_post, const float* rstd_pre, float skip_scale, float branch_scale,
+                               void* dx_bf16, int64_t lddx, void* dy_bf16, int64_t lddy, float* dg_post, float* dgate,
+                               float* dg_pre, float* amax_dy, void* workspace, size_t workspace_bytes, void* stream);
+size_t f8_residual_norm_bwd_workspace_bytes(int64_t M, int64_t D, int64_t gate_rows);
+
+/*
+ * From the logits of an output projection to the loss and back.  logits [M, *]
+ * bf16 (row pitch ld, a multiple of 8; rows are read up to the next multiple of
+ * 8 columns), of which the first V columns are the vocabulary: a Float8 linear's
+ * N is a multiple of 16, its columns from V on are padding that takes no part.
+ * Per row, with z = scale * logits (scale > 0: the inverse temperature) and
+ * p = softmax(z):
+ *   logp = log p[target]; a negative target stands for no token (logp 0, no
+ *     gradient), one >= V gives NaN;
+ *   entropy = -sum_j p_j log p_j;
+ *   top_ids / top_logp [M, top_k]: the top_k largest logits in order, the lower
+ *     column first among equals, and their log p; 0 <= top_k <= min(V, 128);
+ *   stats [M, 2] fp32, kept for the backward: the largest logit, and the log of
+ *     sum_j exp(z_j - z_max) (scale times the first plus the second is the log
+ *     of the softmax denominator).
+ * logp (with targets), entropy, top_ids and top_logp (with top_k > 0) are
+ * nullable.  Logits of -inf are masked entries (p = 0); in a row of nothing else
+ * logp and top_logp are -inf, entropy is 0 and there is no gradient.  A NaN or
+ * +inf in a row makes its outputs NaN (top_ids stay columns of the row).
+ *
+ * f8_token_logprobs_bwd: with d_logp (nullable, with targets) and d_entropy
+ * (nullable, with entropy) [M] fp32, the gradients of the two,
+ *   dlogits_j = scale * (d_logp ([j = target] - p_j) - d_entropy p_j (log p_j + entropy))
+ * [M, cols] bf16 (pitch ldd), cols >= V a multiple of 8 (the projection's N): zeros
+ * from V on, and in rows whose gradients are zero.  dlogits may be logits itself,
+ * at the same pitch.  amax_d (nullable, 1 float): exact maximum magnitude of
+ * dlogits, for f8_linear_bwd_chained (workspace: at least 8 KiB, only then).
+ *
+ * f8_distill: a student against a teacher's listed entries per row,
+ * teacher_ids [M, K] int64 (a negative id: no entry; >= V: NaN) and teacher_logp
+ * [M, K] fp32, packed, 1 <= K <= 128, e.g. the top_ids and top_logp of
+ * f8_token_logprobs on the teacher's logits:
+ *   tail = 0: q = softmax over the row's entries of teacher_scale * teacher_logp,
+ *     loss = sum_k q_k (log q_k - log p[id_k]);
+ *   tail = 1: q = exp(teacher_logp) as given (teacher_scale must be 1), and what
+ *     both leave outside the list is one more class:
+ *     loss = sum_k q_k (log q_k - log p[id_k]) + q_rest (log q_rest - log p_rest),
+ *     q_rest = 1 - sum_k q_k (below 2^-20: 0).
+ * A row without entries has loss 0 and no gradient.  An id that occurs twice
+ * counts with both weights.  logp (nullable, with targets): as above, for a term
+ * on the given tokens in the same pass.  stats [M, 4] fp32, kept for the backward:
+ * the two numbers above, and two of the teacher's.
+ * f8_distill_bwd: dlogits from d_loss and (nullable, with targets) d_logp, [M] fp32.
+ * workspace of both forwards: f8_logits_workspace_bytes(M, V, top_k) bytes (top_k
+ * 0 for f8_distill).  1 <= V <= 2^22; any M >= 0.  No atomics on results: they are reproducible.
+ */
+size_t f8_logits_workspace_bytes(int64_t M, int64_t V, int64_t top_k);
+f8_status f8_token_logprobs(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale,
+                            const int64_t* targets, float* stats, float* logp, float* entropy, int64_t top_k,
+                            int64_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes, void* stream);
+f8_status f8_token_logprobs_bwd(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale,
+                                const int64_t* targets, const float* stats, const float* entropy, const float* d_logp,
+                                const float* d_entropy, void* dlogits_bf16, int64_t ldd, int64_t cols, float* amax_d,
+                                void* workspace, size_t workspace_bytes, void* stream);
+f8_status f8_distill(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale, const int64_t* teacher_ids,
+                     const float* teacher_logp, int64_t K, int tail, float teacher_scale, const int64_t* targets,
+                     float* stats, float* loss, float* logp, void* workspace, size_t workspace_bytes, void* stream);
+f8_status f8_distill_bwd(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale,
+                         const int64_t* teacher_ids, const float* teacher_logp, int64_t K, int tail, float teacher_scale,
+                         const int64_t* targets, const float* stats, const float* d_loss, const float* d_logp,
+                         void* dlogits_bf16, int64_t ldd, int64_t cols, float* amax_d, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
  * Forward of the linear whose input is already quantised in saved->x (codes in
  * saved->x.q, scale, inv_scale; e.g. by f8_silu_mul_quantise_delayed):
  * quantises W [N,K] as state->mode says (the w members of the state; for

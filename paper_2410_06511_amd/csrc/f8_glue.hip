@@ -124,6 +124,10 @@ __global__ __launch_bounds__(kGlueThreads) void glue_amax_final_kernel(const uin
     m = block_max_u32<kGlueWaves>(m, red);
     if (threadIdx.x == 0) amax_out[0] = mag_to_float(m);
 }
+void amax_final(const uint32_t* partial, int n, float* amax_out, hipStream_t st)
+{
+    glue_amax_final_kernel<<<1, kGlueThreads, 0, st>>>(partial, n, amax_out);
+}
 
 // RMS normalisation, forward: y[m, :] = x[m, :] * rstd[m] * g, rstd[m] = 1 / sqrt(mean x[m, :]^2 + eps).
 // One wavefront per row, rows strided over the grid; the row is read twice (the second time

@@ -112,6 +112,7 @@ bool gemm_rows(int g, int M, int N, int K, const uint8_t* A, const uint8_t* B, c
                uint32_t* amax_bits, hipStream_t st);
 int cu_count();  // of the current device
 void zero_word(uint32_t* p, hipStream_t st);  // not a memset: the call may be captured
+void amax_final(const uint32_t* partial, int n, float* amax_out, hipStream_t st);  // of the blocks' partial maxima (bf16 magnitudes)
 // Largest scratch a split product can use (ranges x output elements x 4 bytes, with ranges x tiles
 // at most one per compute unit): part of what workspace_bytes returns.
 constexpr size_t kSplitKMaxBytes = (size_t)256 * 256 * 256 * sizeof(float);

@@ -1,0 +1,771 @@
+// From the logits of an output projection to the loss and back to the logits' gradient (which is the output gradient of a Float8
+// linear), a row of V logits z = scale * logits per token:
+//   p = softmax(z),  logp[t] = z_t - lse,  H = -sum p log p,  the k largest z with their log p;
+//   dz_j = scale * (dlogp (1[j = t] - p_j) - dH p_j (log p_j + H))
+// and distillation from a teacher's listed entries (id_k, q_k), with p_rest, q_rest the masses outside the list:
+//   loss = sum_k q_k (log q_k - log p_k) [+ q_rest (log q_rest - log p_rest)]
+//   dz_j = scale * (g (c p_j - q_j) + the given token's term above),  c = 1 for listed j, 1 [- q_rest / p_rest] for the others.
+// Bound by memory: one read of the logits forward (2 bytes an element), one read and one write backward (4 bytes).
+// Softmax statistics are kept as (largest logit, log of the sum of exp(z - z_max)): a difference of two bf16 values is exact in
+// fp32 where their ratio is below 2^16, so that p keeps its precision however large the logits are, which one number lse would not.
+#include <float.h>
+
+#include "f8_device.hpp"
+#include "f8_host.hpp"
+
+namespace f8 {
+
+constexpr int kLgThreads = 512;
+constexpr int kLgWaves = kLgThreads / kWave;
+constexpr int kLgUnroll = 4;            // 16-byte loads in flight a thread
+constexpr int kLgSegCols = 131072;      // columns that a block takes at most: its chunks' maxima are 2 bytes each in LDS
+constexpr int kLgMaxSeg = 32;           // blocks that share a row, at most
+constexpr int64_t kLgMaxCols = (int64_t)kLgSegCols * kLgMaxSeg;
+constexpr int kLgMaxTop = 128;          // alternatives, and entries of a teacher's list
+constexpr int kLgCandidates = 1024;     // elements that the selection ranks at once
+constexpr int kLgGradBlocks = 1024;     // of the gradient: one partial maximum each
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr uint32_t kNegInf2 = 0xFF80FF80u;
+static_assert((size_t)kLgGradBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial maximum per block fits the minimum workspace");
+
+__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---- statistics of a softmax, joined over lanes, waves and blocks -------------------------------
+
+// m: largest logit seen (-FLT_MAX: none but -inf), s = sum e, d = sum e log2(e), e = exp(scale (z - m)); c = scale * log2(e).
+// Exponents end at kFar, where e is 0: differences of masked values (-inf, the type's lowest) would make 0 * inf.
+constexpr float kFar = -1000.0f;
+struct Stat {
+    float m, s, d;
+};
+__device__ inline Stat join(const Stat& a, const Stat& b, float c)
+{
+    const float m = fmaxf(a.m, b.m), ga = fmaxf((a.m - m) * c, kFar), gb = fmaxf((b.m - m) * c, kFar), fa = exp2_hw(ga), fb = exp2_hw(gb);
+    return {m, a.s * fa + b.s * fb, fa * (a.d + a.s * ga) + fb * (b.d + b.s * gb)};
+}
+__device__ inline Stat wave_join(Stat v, float c)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1)
+        v = join(v, {__shfl_xor(v.m, off, kWave), __shfl_xor(v.s, off, kWave), __shfl_xor(v.d, off, kWave)}, c);
+    return v;
+}
+
+// ---- order of logits -----------------------------------------------------------------------------
+
+// bf16 bits -> 16 bits whose integer order is that of the values; both zeros alike, NaN below everything
+__device__ inline uint32_t order16(uint32_t b)
+{
+    b = b == 0x8000u ? 0u : b;
+    return (b & 0x7FFFu) > 0x7F80u ? 0u : b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;
+}
+__device__ inline float order_value(uint32_t o) { return __uint_as_float((o & 0x8000u ? o & 0x7FFFu : ~o & 0xFFFFu) << 16); }
+// elements in their order, the lower column first among equals
+__device__ inline uint64_t element_key(uint32_t o, uint32_t col) { return (uint64_t)o << 32 | (uint32_t)~col; }
+__device__ inline uint32_t key_column(uint64_t k) { return ~(uint32_t)k; }
+__device__ inline uint32_t chunk_key(uint32_t o, int lc) { return o << 16 | (uint32_t)(65535 - lc); }
+
+__device__ inline void unpack(uint4 v, float* z)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[2 * j] = bf16_lo(w[j]), z[2 * j + 1] = bf16_hi(w[j]);
+}
+// chunk c of a row; columns from V on read as -inf
+__device__ inline uint4 load_logits(const uint4* row, int c, int V)
+{
+    uint4 v = row[c];
+    const int left = V - c * 8;
+    if (left < 8) {
+        uint32_t* w = &v.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = left <= 2 * j ? kNegInf2 : left == 2 * j + 1 ? (w[j] & 0xFFFFu) | (kNegInf2 & 0xFFFF0000u) : w[j];
+    }
+    return v;
+}
+
+// ---- a teacher's list in LDS ----------------------------------------------------------------------
+
+// The entries of one row that fall into a block's columns.  head[chunk] is the last entry (+ 1) of the chunk, next[] the one before
+// it, so that a sweep asks one byte a chunk; an id that occurs again is dropped after its weight went to the first.
+struct List {
+    int id[kLgMaxTop];       // column, -1: none
+    float q[kLgMaxTop];
+    uint8_t next[kLgMaxTop];
+};
+// Threads below K bring their entry (q: its weight); all threads call.
+__device__ inline void list_store(List& L, int K, int id, float q)
+{
+    const int k = threadIdx.x;
+    __syncthreads();
+    if (k < K) L.id[k] = id, L.q[k] = q;
+    __syncthreads();
+    bool first = k < K && id >= 0;
+    if (first) {
+        float sum = 0.0f;
+        for (int j = 0; j < K; ++j)
+            if (L.id[j] == id) {
+                if (j < k) first = false;
+                sum += L.q[j];
+            }
+        q = sum;
+    }
+    __syncthreads();
+    if (k < K) L.id[k] = first ? id : -1, L.q[k] = q;
+}
+// the heads of chunks c0 .. c1 - 1
+__device__ inline void list_heads(List& L, int K, uint8_t* head, int c0, int c1)
+{
+    for (int i = threadIdx.x; i < (c1 - c0 + 3) / 4; i += kLgThreads) reinterpret_cast<uint32_t*>(head)[i] = 0;
+    __syncthreads();
+    const int k = threadIdx.x;
+    if (k < K && L.id[k] >= 0) {
+        const int c = L.id[k] >> 3;
+        int before = 0;
+        bool last = true;
+        for (int j = 0; j < K; ++j)
+            if (j != k && L.id[j] >= 0 && L.id[j] >> 3 == c) {
+                if (j < k) before = j + 1;
+                else last = false;
+            }
+        L.next[k] = (uint8_t)before;
+        if (last && c >= c0 && c < c1) head[c - c0] = (uint8_t)(k + 1);
+    }
+    __syncthreads();
+}
+
+// ---- forward ---------------------------------------------------------------------------------------
+
+struct TeacherArgs {
+    const int64_t* ids;  // [M, K], negative: no entry
+    const float* logp;   // [M, K]
+    int K, tail;
+    float scale;
+};
+struct StatArgs {
+    const uint16_t* logits;
+    int64_t ld, M;
+    int V, nseg, seg_chunks, top;
+    float scale;
+    const int64_t* targets;  // nullable
+    float *stats, *logp, *entropy;
+    int64_t* top_ids;
+    float* top_logp;
+    TeacherArgs t;
+    float* loss;
+    float4* part;        // per block of a shared row: (m, s, d, -)
+    uint64_t* part_top;  // and its elements
+};
+
+// a remainder that sums of fp32 probabilities do not tell from zero counts as none
+constexpr double kNoRest = 0x1p-20;
+
+// What a row's outputs are, from its statistics; called by one whole wave.
+// With a teacher: rest is the sum outside the list where the remainder is a class (v.s then lacks the list's part).
+template <bool LIST>
+__device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v, const List* L)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    const uint16_t* z = a.logits + row * a.ld;
+    constexpr int E = kLgMaxTop / kWave;
+    float zk[E] = {}, total = v.s;
+    bool has[E] = {}, wrong = false;
+    if constexpr (LIST) {
+        float listed = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int k = lane + kWave * e;
+            if (k >= a.t.K) continue;
+            const int64_t id = a.t.ids[row * a.t.K + k];
+            has[e] = id >= 0 && id < a.V;
+            wrong |= id >= a.V;
+            if (!has[e]) continue;
+            zk[e] = (__uint_as_float((uint32_t)z[id] << 16) - v.m) * a.scale;
+            if (a.t.tail && L->id[k] >= 0) listed += exp2_hw(zk[e] * kLog2e);
+        }
+        if (a.t.tail) {
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) listed += __shfl_xor(listed, off, kWave);
+            total += listed;
+        }
+    }
+    const bool none = total == 0.0f;  // every logit is -inf
+    const float m = none ? -INFINITY : v.m, log_total = none ? -INFINITY : logf(total);
+    if (lane == 0) {
+        float* s = a.stats + row * (LIST ? 4 : 2);
+        s[0] = m, s[1] = log_total;
+        if (a.entropy) a.entropy[row] = none ? 0.0f : log_total - v.d * kLn2 / total;
+        if (a.logp) {
+            const int64_t t = a.targets[row];
+            a.logp[row] = t < 0 ? 0.0f : t >= a.V ? NAN : none ? -INFINITY : (__uint_as_float((uint32_t)z[t] << 16) - m) * a.scale - log_total;
+        }
+    }
+    if constexpr (LIST) {
+        // the teacher's probabilities: given, or the softmax over its entries
+        float lq[E], top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            lq[e] = has[e] ? a.t.logp[row * a.t.K + lane + kWave * e] * a.t.scale : -INFINITY;
+            top = lq[e] > top || lq[e] != lq[e] ? lq[e] : top;
+        }
+        double sum = 0.0;
+        float norm = 0.0f;
+        if (!a.t.tail) {
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) {
+                const float o = __shfl_xor(top, off, kWave);
+                top = o > top || o != o ? o : top;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum += lq[e] == -INFINITY ? 0.0 : (double)expf(lq[e] - top);
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+            norm = sum == 0.0 ? 0.0f : top + logf((float)sum);
+        }
+        double loss = 0.0, mass = 0.0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float l = lq[e] - norm, q = lq[e] == -INFINITY ? 0.0f : expf(l);
+            mass += q;
+            if (q != 0.0f) loss += (double)q * (l - (none ? -INFINITY : zk[e] - log_total));
+        }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) loss += __shfl_xor(loss, off, kWave), mass += __shfl_xor(mass, off, kWave);
+        float coef = sum == 0.0 ? 0.0f : 1.0f;
+        if (a.t.tail) {
+            const double left = 1.0 - mass, rest = none ? 0.0 : (double)v.s / total;
+            const float q_rest = left < kNoRest ? 0.0f : (float)left;  // (a NaN stays)
+            coef = rest > 0.0 ? (float)(1.0 - (double)q_rest / rest) : 0.0f;
+            if (q_rest != 0.0f) loss += (double)q_rest * (logf(q_rest) - (rest > 0.0 ? logf((float)rest) : -INFINITY));
+            if (mass != mass) coef = NAN;
+        }
+        if (none) coef = 0.0f;
+        if (__any(wrong)) loss = coef = NAN;
+        if (lane == 0) {
+            a.loss[row] = (float)loss;
+            a.stats[row * 4 + 2] = coef, a.stats[row * 4 + 3] = norm;
+        }
+    }
+}
+
+// The K largest of a block's elements, in order: emit(rank, key).
+// Every thread has the key of its best chunk (order of the chunk's maximum, the lower chunk first among equals).  The K-th
+// largest of these keys bounds the search: at least K elements reach it, so the K best do, and they lie in chunks that
+// reach it, which are read again: about K of them where the large elements are spread.  What reaches the bound is ranked by counting.
+// Rows built so that more than kLgCandidates elements reach it (their largest share few threads) take a search by halves.
+template <class Emit>
+__device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K, uint32_t best, const uint16_t* cmax, uint64_t* cand, uint32_t* words, Emit&& emit)
+{
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    uint32_t* keys = reinterpret_cast<uint32_t*>(cand);  // until the candidates come
+    static_assert(kLgThreads * sizeof(uint32_t) <= kLgCandidates * sizeof(uint64_t), "a key a thread");
+    keys[tid] = best;
+    if (tid == 0) words[0] = 0;
+    __syncthreads();
+    if (tid < kWave) {
+        uint32_t k[kLgWaves], t = 0;
+#pragma unroll
+        for (int i = 0; i < kLgWaves; ++i) k[i] = keys[lane + kWave * i];
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t at = t | 1u << bit;
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < kLgWaves; ++i) n += __popcll(__ballot(k[i] >= at));
+            if (n >= K) t = at;
+        }
+        if (lane == 0) words[1] = t;
+    }
+    __syncthreads();
+    const uint32_t bound = words[1];
+    auto collect = [&](uint64_t least) {  // elements of at least this key, of chunks that reach the bound
+        for (int c = c0 + tid; c < c1; c += kLgThreads) {
+            const int lc = c - c0;
+            if (chunk_key(cmax[lc], lc) < bound) continue;
+            const uint4 v = row[c];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t o = order16(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu);
+                const uint64_t key = element_key(o, (uint32_t)(c * 8 + j));
+                if (c * 8 + j < V && chunk_key(o, lc) >= bound && key >= least) {
+                    const uint32_t at = atomicAdd(words, 1u);
+                    if (at < (uint32_t)kLgCandidates) cand[at] = key;
+                }
+            }
+        }
+    };
+    collect(0);
+    __syncthreads();
+    uint32_t n = words[0];
+    if (n > (uint32_t)kLgCandidates) {
+        // the K-th largest key itself, bit by bit (the columns' upper bits are alike, but need no case of their own)
+        uint64_t t = 0;
+        for (int bit = 47; bit >= 0; --bit) {
+            const uint64_t at = t | (uint64_t)1 << bit;
+            __syncthreads();
+            if (tid == 0) words[0] = 0;
+            __syncthreads();
+            uint32_t mine = 0;
+            for (int c = c0 + tid; c < c1; c += kLgThreads) {
+                const int lc = c - c0;
+                if (chunk_key(cmax[lc], lc) < bound || cmax[lc] < (uint32_t)(at >> 32)) continue;
+                const uint4 v = row[c];
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t o = order16(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu);
+                    mine += c * 8 + j < V && chunk_key(o, lc) >= bound && element_key(o, (uint32_t)(c * 8 + j)) >= at;
+                }
+            }
+            if (mine) atomicAdd(words, mine);
+            __syncthreads();
+            if (words[0] >= (uint32_t)K) t = at;
+        }
+        __syncthreads();
+        if (tid == 0) words[0] = 0;
+        __syncthreads();
+        collect(t);
+        __syncthreads();
+        n = words[0];
+    }
+    for (uint32_t i = tid; i < n; i += kLgThreads) {
+        const uint64_t key = cand[i];
+        int rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += cand[j] > key;
+        if (rank < K) emit(rank, key);
+    }
+}
+
+// One block takes one row, or one of nseg pieces of it.  LDS: chunk maxima (TOP) or the list's heads (LIST) by chunk.
+template <bool ENT, bool TOP, bool LIST>
+__global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs a)
+{
+    extern __shared__ uint8_t by_chunk[];
+    __shared__ Stat wave_stat[kLgWaves];
+    __shared__ uint32_t words[2];
+    __shared__ uint64_t cand[TOP ? kLgCandidates : 1];
+    __shared__ List list[1];
+    uint16_t* cmax = reinterpret_cast<uint16_t*>(by_chunk);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int chunks = (a.V + 7) / 8;
+    const float c2 = a.scale * kLog2e;
+    for (int64_t unit = blockIdx.x; unit < a.M * a.nseg; unit += gridDim.x) {
+        const int64_t rowi = unit / a.nseg;
+        const int seg = (int)(unit - rowi * a.nseg), c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
+        const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
+        if (LIST && a.t.tail) {
+            int64_t id = -1;
+            if (tid < a.t.K) id = a.t.ids[rowi * a.t.K + tid];
+            list_store(list[0], a.t.K, id >= 0 && id < a.V ? (int)id : -1, 0.0f);
+            __syncthreads();
+            list_heads(list[0], a.t.K, by_chunk, c0, c1);
+        }
+        Stat v = {-FLT_MAX, 0.0f, 0.0f};
+        uint32_t best = 0;
+        for (int c = c0 + tid; c < c1; c += kLgUnroll * kLgThreads) {
+            uint4 w[kLgUnroll];
+#pragma unroll
+            for (int u = 0; u < kLgUnroll; ++u) {
+                const int cu = c + u * kLgThreads;
+                w[u] = cu < c1 ? load_logits(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+            }
+            float m = v.m;
+            float z[kLgUnroll][8];
+#pragma unroll
+            for (int u = 0; u < kLgUnroll; ++u) {
+                unpack(w[u], z[u]);
+                float cm = z[u][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) cm = fmaxf(cm, z[u][j]);
+                m = fmaxf(m, cm);
+                const int cu = c + u * kLgThreads;
+                if constexpr (TOP) {
+                    if (cu < c1) {
+                        const uint32_t o = order16(__float_as_uint(cm) >> 16);
+                        cmax[cu - c0] = (uint16_t)o;
+                        const uint32_t key = chunk_key(o, cu - c0);
+                        best = key > best ? key : best;
+                    }
+                }
+                if constexpr (LIST) {
+                    if (a.t.tail && cu < c1)
+                        for (int k = by_chunk[cu - c0]; k; k = list[0].next[k - 1]) {
+                            const int j0 = list[0].id[k - 1] & 7;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[u][j] = j == j0 ? -INFINITY : z[u][j];
+                        }
+                }
+            }
+            const float gone = fmaxf((v.m - m) * c2, kFar), f = exp2_hw(gone);
+            if constexpr (ENT) v.d = f * (v.d + v.s * gone);
+            v.s *= f;
+            v.m = m;
+#pragma unroll
+            for (int u = 0; u < kLgUnroll; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float l = (z[u][j] - m) * c2, e = exp2_hw(l);
+                    v.s += e;
+                    if constexpr (ENT) v.d += e * fmaxf(l, kFar);
+                }
+        }
+        v = wave_join(v, c2);
+        if (lane == 0) wave_stat[wave] = v;
+        __syncthreads();
+        v = wave_stat[0];
+#pragma unroll
+        for (int i = 1; i < kLgWaves; ++i) v = join(v, wave_stat[i], c2);
+        if (a.nseg > 1) {
+            if (tid == 0) a.part[unit] = make_float4(v.m, v.s, v.d, 0.0f);
+        } else if (wave == 0) {
+            finish_row<LIST>(a, rowi, v, list);
+        }
+        if constexpr (TOP) {
+            const float log_total = logf(v.s);
+            block_top(row, c0, c1, a.V, a.top, best, cmax, cand, words, [&](int rank, uint64_t key) {
+                if (a.nseg > 1) {
+                    a.part_top[unit * a.top + rank] = key;
+                } else {
+                    a.top_ids[rowi * a.top + rank] = key_column(key);
+                    a.top_logp[rowi * a.top + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
+                }
+            });
+        }
+        __syncthreads();  // LDS is used again
+    }
+}
+
+// Rows that blocks shared: their statistics, and the best of their elements.
+template <bool LIST>
+__global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs a)
+{
+    extern __shared__ uint64_t lists[];  // [nseg][top]
+    __shared__ List list[1];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const float c2 = a.scale * kLog2e;
+    for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+        Stat v = {-FLT_MAX, 0.0f, 0.0f};
+        if (lane < a.nseg) {
+            const float4 p = a.part[row * a.nseg + lane];
+            v = {p.x, p.y, p.z};
+        }
+        v = wave_join(v, c2);
+        if (LIST && a.t.tail) {
+            int64_t id = -1;
+            if (tid < a.t.K) id = a.t.ids[row * a.t.K + tid];
+            list_store(list[0], a.t.K, id >= 0 && id < a.V ? (int)id : -1, 0.0f);
+            __syncthreads();
+        }
+        if (tid < kWave) finish_row<LIST>(a, row, v, list);
+        if (a.top) {
+            const int K = a.top, n = a.nseg * K;
+            for (int i = tid; i < n; i += kLgThreads) lists[i] = a.part_top[row * n + i];
+            __syncthreads();
+            const float log_total = logf(v.s);
+            for (int i = tid; i < n; i += kLgThreads) {
+                const uint64_t key = lists[i];
+                int rank = i % K;
+                for (int s = 0; s < a.nseg && rank < K; ++s) {
+                    const uint64_t* l = lists + s * K;
+                    if (s == i / K || l[0] < key) continue;
+                    int lo = 1, hi = K;  // how many of the list are larger
+                    while (lo < hi) {
+                        const int mid = (lo + hi) / 2;
+                        if (l[mid] > key) lo = mid + 1;
+                        else hi = mid;
+                    }
+                    rank += lo;
+                }
+                if (rank < K) {
+                    a.top_ids[row * K + rank] = key_column(key);
+                    a.top_logp[row * K + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---- backward ----------------------------------------------------------------------------------------
+
+struct GradArgs {
+    const uint16_t* logits;
+    int64_t ld, M;
+    int V, cols, nseg, seg_chunks;
+    float scale;
+    const int64_t* targets;
+    const float *stats, *entropy, *d_logp, *d_entropy, *d_loss;
+    TeacherArgs t;
+    uint16_t* dlogits;
+    int64_t ldd;
+    uint32_t* partial;
+};
+
+template <bool ENT, bool LIST>
+__global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs a)
+{
+    extern __shared__ uint8_t by_chunk[];
+    __shared__ uint32_t red[kLgWaves];
+    __shared__ List list[1];
+    const int tid = threadIdx.x;
+    const int chunks = a.cols / 8, read = (a.V + 7) / 8;
+    const float c2 = a.scale * kLog2e;
+    uint32_t mag = 0;
+    for (int64_t unit = blockIdx.x; unit < a.M * a.nseg; unit += gridDim.x) {
+        const int64_t rowi = unit / a.nseg;
+        const int seg = (int)(unit - rowi * a.nseg), c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
+        const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
+        uint4* out = reinterpret_cast<uint4*>(a.dlogits + rowi * a.ldd);
+        const float* st = a.stats + rowi * (LIST ? 4 : 2);
+        const float m = st[0], log2_total = st[1] * kLog2e;
+        const int64_t target = a.targets ? a.targets[rowi] : -1;
+        const float dlp = target < 0 || !a.d_logp ? 0.0f : target >= a.V ? NAN : a.d_logp[rowi] * a.scale;
+        // dz = p (A + B log2 p), + dlp at the given token; of listed entries p AL - their weight
+        float A = -dlp, B = 0.0f, AL = 0.0f;
+        if constexpr (ENT) {
+            const float dh = a.d_entropy[rowi] * a.scale;
+            if (dh != 0.0f) A -= dh * a.entropy[rowi], B = -dh * kLn2;
+        }
+        float g = 0.0f;
+        if constexpr (LIST) {
+            g = a.d_loss[rowi] * a.scale;
+            if (g != 0.0f) A += g * st[2];
+            AL = g - dlp;
+        }
+        // nothing to hand back: no weight, or no logit that a change could move
+        const bool zero = (A == 0.0f && B == 0.0f && dlp == 0.0f && g == 0.0f) || st[1] == -INFINITY;
+        if constexpr (LIST) {
+            if (!zero) {  // (alike for the whole block)
+                int64_t id = -1;
+                float q = 0.0f;
+                if (tid < a.t.K) {
+                    id = a.t.ids[rowi * a.t.K + tid];
+                    if (id >= 0 && id < a.V) q = g == 0.0f ? 0.0f : g * expf(a.t.logp[rowi * a.t.K + tid] * a.t.scale - st[3]);
+                }
+                list_store(list[0], a.t.K, id >= 0 && id < a.V ? (int)id : -1, q);
+                __syncthreads();
+                list_heads(list[0], a.t.K, by_chunk, c0, c1);
+            }
+        }
+        for (int c = c0 + tid; c < c1; c += kLgUnroll * kLgThreads) {
+            uint4 w[kLgUnroll];
+#pragma unroll
+            for (int u = 0; u < kLgUnroll; ++u) {
+                const int cu = c + u * kLgThreads;
+                w[u] = cu < c1 && cu < read && !zero ? load_logits(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+            }
+#pragma unroll
+            for (int u = 0; u < kLgUnroll; ++u) {
+                const int cu = c + u * kLgThreads;
+                if (cu >= c1) break;
+                uint4 o = make_uint4(0, 0, 0, 0);
+                if (!zero && cu < read) {
+                    float z[8], p[8];
+                    unpack(w[u], z);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float l2 = __builtin_fmaf(z[j] - m, c2, -log2_total);
+                        p[j] = exp2_hw(l2);
+                        z[j] = ENT ? p[j] * __builtin_fmaf(B, fmaxf(l2, kFar), A) : p[j] * A;
+                    }
+                    if constexpr (LIST) {
+                        for (int k = by_chunk[cu - c0]; k; k = list[0].next[k - 1]) {
+                            const int j0 = list[0].id[k - 1] & 7;
+                            const float q = list[0].q[k - 1];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[j] = j == j0 ? p[j] * AL - q : z[j];
+                        }
+                    }
+                    if (cu == (int)(target >> 3)) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) z[j] += j == (int)(target & 7) ? dlp : 0.0f;
+                    }
+                    const int left = a.V - cu * 8;
+                    if (left < 8) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) z[j] = j < left ? z[j] : 0.0f;
+                    }
+                    o = make_uint4(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7]));
+                    mag = absmax_acc(mag, o);
+                }
+                store_stream(out + cu, o);
+            }
+        }
+        if constexpr (LIST) __syncthreads();  // LDS is used again
+    }
+    if (a.partial) {
+        const uint32_t mx = block_max_u32<kLgWaves>(pk_collapse(mag), red);
+        if (tid == 0) a.partial[blockIdx.x] = mx;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+
+// Into how many pieces of how many chunks rows are cut: enough blocks for the chip where there are few rows, no piece shorter
+// than one chunk a thread.
+struct Split {
+    int nseg, seg_chunks;
+};
+static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted)
+{
+    const int64_t chunks = (cols + 7) / 8;
+    int64_t n = M > 0 ? blocks_wanted / M : 1;
+    if (n > chunks / kLgThreads) n = chunks / kLgThreads;
+    if (n > kLgMaxSeg) n = kLgMaxSeg;
+    const int64_t least = (cols + kLgSegCols - 1) / kLgSegCols;
+    if (n < least) n = least;
+    if (n < 1) n = 1;
+    const int64_t per = (chunks + n - 1) / n;
+    return {(int)((chunks + per - 1) / per), (int)per};
+}
+constexpr int64_t kLgBlocksWanted = 512;
+
+static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
+{
+    const Split s = split_rows(M, V, kLgBlocksWanted);
+    return s.nseg > 1 ? (size_t)M * s.nseg * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
+}
+
+static f8_status check_logits(const void* logits, int64_t ld, int64_t M, int64_t V, float scale, const void* stats)
+{
+    if (M != 0 && (!logits || !stats)) return F8_ERR_NULL;  // (without rows there is nothing that pointers point to)
+    if (M < 0 || M > 0x7FFFFFFF || V < 1 || V > kLgMaxCols || ld < V || (ld % 8) || ld > 0x7FFFFFFF || !(scale > 0.0f) || !(scale <= FLT_MAX)) return F8_ERR_SHAPE;
+    if (!aligned16(logits)) return F8_ERR_ALIGN;
+    return F8_OK;
+}
+
+static f8_status check_teacher(int64_t M, const int64_t* ids, const float* logp, int64_t K, int tail, float scale)
+{
+    if (M != 0 && (!ids || !logp)) return F8_ERR_NULL;
+    if (tail != 0 && tail != 1) return F8_ERR_ENUM;
+    if (K < 1 || K > kLgMaxTop || !(scale > 0.0f) || !(scale <= FLT_MAX) || (tail && scale != 1.0f)) return F8_ERR_SHAPE;
+    return F8_OK;
+}
+
+template <bool LIST>
+static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_t st)
+{
+    if (a.M == 0) return F8_OK;
+    const Split s = split_rows(a.M, a.V, kLgBlocksWanted);
+    a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
+    if (a.nseg > 1) {
+        if (!ws || ws_bytes < logits_part_bytes(a.M, a.V, a.top)) return F8_ERR_WORKSPACE;
+        if (!aligned16(ws)) return F8_ERR_ALIGN;
+        a.part = (float4*)ws;
+        a.part_top = (uint64_t*)(a.part + a.M * a.nseg);
+    }
+    const int64_t units = a.M * a.nseg;
+    const unsigned blocks = (unsigned)(units < (1 << 20) ? units : (1 << 20));
+    const size_t lds = LIST ? (a.t.tail ? (size_t)(a.seg_chunks + 3) / 4 * 4 : 0) : a.top ? (size_t)a.seg_chunks * 2 : 0;
+    if constexpr (LIST) {
+        logits_stat_kernel<false, false, true><<<blocks, kLgThreads, lds, st>>>(a);
+    } else {
+        const auto kernel = a.entropy ? (a.top ? logits_stat_kernel<true, true, false> : logits_stat_kernel<true, false, false>)
+                                      : (a.top ? logits_stat_kernel<false, true, false> : logits_stat_kernel<false, false, false>);
+        kernel<<<blocks, kLgThreads, lds, st>>>(a);
+    }
+    if (a.nseg > 1) {
+        const unsigned rows = (unsigned)(a.M < (1 << 20) ? a.M : (1 << 20));
+        logits_join_kernel<LIST><<<rows, kLgThreads, (size_t)a.nseg * a.top * sizeof(uint64_t), st>>>(a);
+    }
+    return last_launch_status();
+}
+
+template <bool ENT, bool LIST>
+static f8_status launch_grad(GradArgs& a, float* amax, void* ws, hipStream_t st)
+{
+    int nb = 0;
+    if (a.M > 0) {
+        const Split s = split_rows(a.M, a.cols, kLgGradBlocks);
+        a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
+        a.partial = amax ? (uint32_t*)ws : nullptr;
+        const int64_t units = a.M * a.nseg;
+        nb = (int)(units < kLgGradBlocks ? units : kLgGradBlocks);
+        logits_grad_kernel<ENT, LIST><<<nb, kLgThreads, LIST ? (size_t)(a.seg_chunks + 3) / 4 * 4 : 0, st>>>(a);
+    }
+    if (amax) amax_final((const uint32_t*)ws, nb, amax, st);
+    return last_launch_status();
+}
+
+static f8_status check_grad(int64_t M, int64_t V, const void* dlogits, int64_t ldd, int64_t cols, const float* amax, const void* ws, size_t ws_bytes)
+{
+    if (M != 0 && !dlogits) return F8_ERR_NULL;
+    if (cols < V || (cols % 8) || cols > kLgMaxCols || ldd < cols || (ldd % 8) || ldd > 0x7FFFFFFF) return F8_ERR_SHAPE;
+    if (!aligned16(dlogits)) return F8_ERR_ALIGN;
+    if (amax && (!ws || ws_bytes < kMinWorkspaceBytes)) return F8_ERR_WORKSPACE;
+    return F8_OK;
+}
+
+}  // namespace f8
+
+using namespace f8;
+
+extern "C" {
+
+size_t f8_logits_workspace_bytes(int64_t M, int64_t V, int64_t top_k)
+{
+    size_t n = M > 0 && V > 0 && V <= kLgMaxCols && top_k >= 0 && top_k <= kLgMaxTop ? logits_part_bytes(M, V, top_k) : 0;
+    if (n < kMinWorkspaceBytes) n = kMinWorkspaceBytes;
+    return (n + 255) / 256 * 256;
+}
+
+f8_status f8_token_logprobs(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale, const int64_t* targets, float* stats, float* logp,
+                            float* entropy, int64_t top_k, int64_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    f8_status s = check_logits(logits_bf16, ld, M, V, scale, stats);
+    if (s != F8_OK) return s;
+    if (M != 0 && ((logp != nullptr) != (targets != nullptr) || (top_k > 0 && (!top_ids || !top_logp)))) return F8_ERR_NULL;
+    if (top_k < 0 || top_k > kLgMaxTop || top_k > V) return F8_ERR_SHAPE;
+    StatArgs a = {};
+    a.logits = (const uint16_t*)logits_bf16, a.ld = ld, a.M = M, a.V = (int)V, a.top = (int)top_k, a.scale = scale;
+    a.targets = targets, a.stats = stats, a.logp = logp, a.entropy = entropy, a.top_ids = top_ids, a.top_logp = top_logp;
+    return launch_stats<false>(a, workspace, workspace_bytes_, (hipStream_t)stream);
+}
+
+f8_status f8_token_logprobs_bwd(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale, const int64_t* targets, const float* stats,
+                                const float* entropy, const float* d_logp, const float* d_entropy, void* dlogits_bf16, int64_t ldd, int64_t cols,
+                                float* amax_d, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    f8_status s = check_logits(logits_bf16, ld, M, V, scale, stats);
+    if (s != F8_OK) return s;
+    if (M != 0 && ((d_logp != nullptr) != (targets != nullptr) || (d_entropy && !entropy) || (!d_logp && !d_entropy))) return F8_ERR_NULL;
+    if ((s = check_grad(M, V, dlogits_bf16, ldd, cols, amax_d, workspace, workspace_bytes_)) != F8_OK) return s;
+    GradArgs a = {};
+    a.logits = (const uint16_t*)logits_bf16, a.ld = ld, a.M = M, a.V = (int)V, a.cols = (int)cols, a.scale = scale, a.targets = targets;
+    a.stats = stats, a.entropy = entropy, a.d_logp = d_logp, a.d_entropy = d_entropy, a.dlogits = (uint16_t*)dlogits_bf16, a.ldd = ldd;
+    return d_entropy ? launch_grad<true, false>(a, amax_d, workspace, (hipStream_t)stream)
+                     : launch_grad<false, false>(a, amax_d, workspace, (hipStream_t)stream);
+}
+
+f8_status f8_distill(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale, const int64_t* teacher_ids, const float* teacher_logp, int64_t K,
+                     int tail, float teacher_scale, const int64_t* targets, float* stats, float* loss, float* logp, void* workspace,
+                     size_t workspace_bytes_, void* stream)
+{
+    f8_status s = check_logits(logits_bf16, ld, M, V, scale, stats);
+    if (s != F8_OK) return s;
+    if ((s = check_teacher(M, teacher_ids, teacher_logp, K, tail, teacher_scale)) != F8_OK) return s;
+    if (M != 0 && (!loss || (logp != nullptr) != (targets != nullptr))) return F8_ERR_NULL;
+    StatArgs a = {};
+    a.logits = (const uint16_t*)logits_bf16, a.ld = ld, a.M = M, a.V = (int)V, a.scale = scale;
+    a.targets = targets, a.stats = stats, a.logp = logp, a.t = {teacher_ids, teacher_logp, (int)K, tail, teacher_scale}, a.loss = loss;
+    return launch_stats<true>(a, workspace, workspace_bytes_, (hipStream_t)stream);
+}
+
+f8_status f8_distill_bwd(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale, const int64_t* teacher_ids, const float* teacher_logp, int64_t K,
+                         int tail, float teacher_scale, const int64_t* targets, const float* stats, const float* d_loss, const float* d_logp,
+                         void* dlogits_bf16, int64_t ldd, int64_t cols, float* amax_d, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    f8_status s = check_logits(logits_bf16, ld, M, V, scale, stats);
+    if (s != F8_OK) return s;
+    if ((s = check_teacher(M, teacher_ids, teacher_logp, K, tail, teacher_scale)) != F8_OK) return s;
+    if (M != 0 && (!d_loss || (d_logp != nullptr) != (targets != nullptr))) return F8_ERR_NULL;
+    if ((s = check_grad(M, V, dlogits_bf16, ldd, cols, amax_d, workspace, workspace_bytes_)) != F8_OK) return s;
+    GradArgs a = {};
+    a.logits = (const uint16_t*)logits_bf16, a.ld = ld, a.M = M, a.V = (int)V, a.cols = (int)cols, a.scale = scale, a.targets = targets;
+    a.stats = stats, a.d_loss = d_loss, a.d_logp = d_logp, a.t = {teacher_ids, teacher_logp, (int)K, tail, teacher_scale};
+    a.dlogits = (uint16_t*)dlogits_bf16, a.ldd = ldd;
+    return launch_grad<false, true>(a, amax_d, workspace, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -30,6 +30,8 @@ EXPORTS = ["f8_workspace_bytes", "f8_status_string", "f8_amax", "f8_scale", "f8_
            "f8_silu_mul_bwd_quantise_delayed", "f8_linear_bwd_dyq",
            "f8_rope", "f8_rope_qkv", "f8_rope_qk_bwd", "f8_transpose_bf16", "f8_add", "f8_rmsnorm_bwd", "f8_sdpa_fwd", "f8_sdpa_bwd", "f8_sdpa_bwd_rows", "f8_sdpa_bwd_workspace_bytes",
            "f8_rmsnorm_bwd_add", "f8_linear_fwd_wq", "f8_linear_fwd_noalloc", "f8_linear_fwd_quantise",
+           "f8_residual_norm", "f8_residual_norm_bwd", "f8_residual_norm_bwd_workspace_bytes", "f8_logits_workspace_bytes",
+           "f8_token_logprobs", "f8_token_logprobs_bwd", "f8_distill", "f8_distill_bwd",
            "f8_probe_mfma", "f8_probe_copy", "f8_probe_read", "f8_probe_clock"]
 
 
@@ -119,9 +121,20 @@ def lib():
         l.f8_sdpa_bwd_rows.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _i64, _p, _i64, _p, _i64,
                                        _p, _i64, _p, _p, _p, C.c_size_t, _p]
         l.f8_sdpa_bwd_workspace_bytes.argtypes = [_i64] * 5
+        f = C.c_float
+        l.f8_residual_norm.argtypes = [_p, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _p, f, f, f, _p, _i64, _p, _i64, _p, _p, _p, _p, C.c_size_t, _p]
+        l.f8_residual_norm_bwd.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _p, _p, _p, f, f, _p, _i64, _p, _i64,
+                                           _p, _p, _p, _p, _p, C.c_size_t, _p]
+        l.f8_residual_norm_bwd_workspace_bytes.argtypes = [_i64] * 3
+        l.f8_logits_workspace_bytes.argtypes = [_i64] * 3
+        l.f8_token_logprobs.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _p, _p, _i64, _p, _p, _p, C.c_size_t, _p]
+        l.f8_token_logprobs_bwd.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _p, _p, _p, _p, _i64, _i64, _p, _p, C.c_size_t, _p]
+        l.f8_distill.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _i64, _int, f, _p, _p, _p, _p, _p, C.c_size_t, _p]
+        l.f8_distill_bwd.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _i64, _int, f, _p, _p, _p, _p, _p, _i64, _i64, _p, _p, C.c_size_t, _p]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = _int
-        l.f8_sdpa_bwd_workspace_bytes.restype = C.c_size_t
+        for name in ("f8_sdpa_bwd_workspace_bytes", "f8_residual_norm_bwd_workspace_bytes", "f8_logits_workspace_bytes"):
+            getattr(l, name).restype = C.c_size_t
         _lib = l
     return _lib
 
@@ -472,6 +485,122 @@ def sdpa_bwd_rows(q, k, v, o, do, lse, B, S, Hq, Hkv, hd, dq, dk, dv, delta, wor
     _check(lib().f8_sdpa_bwd_rows(_ptr(q), q.stride(0), _ptr(k), k.stride(0), _ptr(v), v.stride(0), _ptr(o), o.stride(0), _ptr(do),
                                   do.stride(0), _ptr(lse), B, S, Hq, Hkv, hd, _ptr(dq), dq.stride(0), _ptr(dk), dk.stride(0), _ptr(dv),
                                   dv.stride(0), _ptr(delta), _ptr(amax_dv_inout), wp, wb, _stream(stream)))
+
+
+# ---- residual sum with the norms around it; logits, loss and back -----------------------
+
+F8_ERR_SHAPE = 2
+
+
+def _arg(name, t, dtype, *shape, packed=True):
+    """The address of an argument after a look at what the library cannot see: type, shape, strides and where it lies."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not (t.is_contiguous() if packed else t.stride(1) == 1 or shape[1] <= 1):
+        raise F8Error(F8_ERR_SHAPE, f"{name}: a GPU tensor of {dtype} and shape {shape} is wanted, {'packed' if packed else 'rows of adjacent elements'}; "
+                                    f"got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(name, t, M, D):
+    """Address and row pitch of a bf16 matrix (any, if it has less than two rows)."""
+    if t is None:
+        return None, 0
+    return _arg(name, t, torch.bfloat16, M, D, packed=False), t.stride(0) if M > 1 else max(t.stride(0), (D + 7) // 8 * 8)
+
+
+def _gate(gate, D):
+    return (None, 0) if gate is None else (_arg("gate", gate, torch.bfloat16, gate.shape[0], D), gate.shape[0])
+
+
+def residual_norm(x, y, h, n=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, eps=1e-5, rstd_post=None, rstd_pre=None,
+                  amax_n=None, workspace=None, stream=None):
+    """h = skip_scale x + branch_scale gate norm(y) g_post; n = norm(h) g_pre.  gate: [gate_rows, D]."""
+    M, D = x.shape
+    wp, wb = _ws(workspace)
+    bf, f32 = torch.bfloat16, torch.float32
+    _check(lib().f8_residual_norm(*_rows("x", x, M, D), *_rows("y", y, M, D), M, D, _arg("g_post", g_post, bf, D), *_gate(gate, D), _arg("g_pre", g_pre, bf, D),
+                                  skip_scale, branch_scale, eps, *_rows("h", h, M, D), *_rows("n", n, M, D), _arg("rstd_post", rstd_post, f32, M),
+                                  _arg("rstd_pre", rstd_pre, f32, M), _arg("amax_n", amax_n, f32, 1), wp, wb, _stream(stream)))
+
+
+def residual_norm_bwd_workspace_bytes(M, D, gate_rows=0):
+    return int(lib().f8_residual_norm_bwd_workspace_bytes(M, D, gate_rows))
+
+
+def residual_norm_bwd(y, dx, dy, h=None, dh=None, dn=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, rstd_post=None,
+                      rstd_pre=None, dg_post=None, dgate=None, dg_pre=None, amax_dy=None, workspace=None, stream=None):
+    """y may be None without g_post and gate; dx or dy may be None."""
+    M, D = next(t.shape for t in (dn, dh, h, dx, dy) if t is not None)
+    wp, wb = _ws(workspace)
+    bf, f32 = torch.bfloat16, torch.float32
+    gp, gr = _gate(gate, D)
+    _check(lib().f8_residual_norm_bwd(*_rows("h", h, M, D), *_rows("y", y, M, D), *_rows("dh", dh, M, D), *_rows("dn", dn, M, D), M, D,
+                                      _arg("g_post", g_post, bf, D), gp, gr, _arg("g_pre", g_pre, bf, D), _arg("rstd_post", rstd_post, f32, M),
+                                      _arg("rstd_pre", rstd_pre, f32, M), skip_scale, branch_scale, *_rows("dx", dx, M, D), *_rows("dy", dy, M, D),
+                                      _arg("dg_post", dg_post, f32, D), _arg("dgate", dgate, f32, gr, D), _arg("dg_pre", dg_pre, f32, D),
+                                      _arg("amax_dy", amax_dy, f32, 1), wp, wb, _stream(stream)))
+
+
+def logits_workspace_bytes(M, vocab, top_k=0):
+    return int(lib().f8_logits_workspace_bytes(M, vocab, top_k))
+
+
+def token_logprobs(logits, vocab, stats, targets=None, logp=None, entropy=None, top_ids=None, top_logp=None, scale=1.0, workspace=None, stream=None):
+    """logits: [M, N], the first `vocab` columns are the vocabulary; stats [M, 2]; top_ids, top_logp [M, k]."""
+    M, N = logits.shape
+    wp, wb = _ws(workspace)
+    i64, f32 = torch.int64, torch.float32
+    k = 0 if top_ids is None else top_ids.shape[1]
+    if vocab > N:
+        raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
+    _check(lib().f8_token_logprobs(*_rows("logits", logits, M, N), M, vocab, scale, _arg("targets", targets, i64, M), _arg("stats", stats, f32, M, 2),
+                                   _arg("logp", logp, f32, M), _arg("entropy", entropy, f32, M), k, _arg("top_ids", top_ids, i64, M, k),
+                                   _arg("top_logp", top_logp, f32, M, k), wp, wb, _stream(stream)))
+
+
+def token_logprobs_bwd(logits, vocab, stats, dlogits, targets=None, entropy=None, d_logp=None, d_entropy=None, scale=1.0, amax_d=None, workspace=None,
+                       stream=None):
+    """dlogits: [M, at least vocab columns]; may be logits itself."""
+    M, N = logits.shape
+    cols = dlogits.shape[1]
+    wp, wb = _ws(workspace)
+    f32 = torch.float32
+    if vocab > N:
+        raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
+    _check(lib().f8_token_logprobs_bwd(*_rows("logits", logits, M, N), M, vocab, scale, _arg("targets", targets, torch.int64, M),
+                                       _arg("stats", stats, f32, M, 2), _arg("entropy", entropy, f32, M), _arg("d_logp", d_logp, f32, M),
+                                       _arg("d_entropy", d_entropy, f32, M), *_rows("dlogits", dlogits, M, cols), cols, _arg("amax_d", amax_d, f32, 1), wp, wb,
+                                       _stream(stream)))
+
+
+def distill(logits, vocab, teacher_ids, teacher_logp, stats, loss, targets=None, logp=None, tail=False, teacher_scale=1.0, scale=1.0, workspace=None,
+            stream=None):
+    """teacher_ids, teacher_logp: [M, K]; stats [M, 4]."""
+    M, N = logits.shape
+    K = teacher_ids.shape[1]
+    wp, wb = _ws(workspace)
+    i64, f32 = torch.int64, torch.float32
+    if vocab > N:
+        raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
+    _check(lib().f8_distill(*_rows("logits", logits, M, N), M, vocab, scale, _arg("teacher_ids", teacher_ids, i64, M, K),
+                            _arg("teacher_logp", teacher_logp, f32, M, K), K, int(bool(tail)), teacher_scale, _arg("targets", targets, i64, M),
+                            _arg("stats", stats, f32, M, 4), _arg("loss", loss, f32, M), _arg("logp", logp, f32, M), wp, wb, _stream(stream)))
+
+
+def distill_bwd(logits, vocab, teacher_ids, teacher_logp, stats, dlogits, d_loss, targets=None, d_logp=None, tail=False, teacher_scale=1.0, scale=1.0,
+                amax_d=None, workspace=None, stream=None):
+    """dlogits: [M, at least vocab columns]; may be logits itself."""
+    M, N = logits.shape
+    K, cols = teacher_ids.shape[1], dlogits.shape[1]
+    wp, wb = _ws(workspace)
+    i64, f32 = torch.int64, torch.float32
+    if vocab > N:
+        raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
+    _check(lib().f8_distill_bwd(*_rows("logits", logits, M, N), M, vocab, scale, _arg("teacher_ids", teacher_ids, i64, M, K),
+                                _arg("teacher_logp", teacher_logp, f32, M, K), K, int(bool(tail)), teacher_scale, _arg("targets", targets, i64, M),
+                                _arg("stats", stats, f32, M, 4), _arg("d_loss", d_loss, f32, M), _arg("d_logp", d_logp, f32, M),
+                                *_rows("dlogits", dlogits, M, cols), cols, _arg("amax_d", amax_d, f32, 1), wp, wb, _stream(stream)))
 
 
 # ---- measuring helpers ---------------------------------------------------------------

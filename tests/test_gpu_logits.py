@@ -1,0 +1,498 @@
+"""f8.token_logprobs, f8.distill and their backwards through the C ABI against oracle/head_oracle.py (fp64).
+
+Tolerances, with z = scale * logits, l = log p and u = 2^-24 (half a step of fp32).  The exponent (z_j - z_max) log2(e) is off by
+at most 4 u of itself (the difference, the constant, its product with the scale, their product), the exponential itself by 4 u, and
+a sum over V terms takes at most V / 512 / blocks + 40 additions one after the other.  So the log of the sum is off by
+  dl = 4 u sum_j p_j |z_j - z_max| + (V / 512 + 48) u + 2 u |log sum|
+and every p_j by a factor within 4 u |z_j - z_max| + dl + 8 u.  bf16 results add half a step, 2^-8 of the value."""
+import numpy as np
+import pytest
+import torch
+
+import oracle as o
+from oracle import head_oracle as ho
+from paper_2410_06511_amd import f8
+from helpers import bits
+
+pytestmark = pytest.mark.gpu
+
+HALF, U = 2.0 ** -8, 2.0 ** -24
+LOWEST = -3.3895313892515355e38  # bf16's
+
+
+def wide(t):
+    return o.bf16_to_f32(bits(t)).astype(np.float64)
+
+
+def f64(t):
+    return t.cpu().numpy().astype(np.float64)
+
+
+def make_logits(M, V, seed, std=3.0, cols=None, pitch=0):
+    """[M, cols] on the GPU (cols: V rounded up to 16), `pitch` more columns between rows; what is beyond V is NaN."""
+    cols = cols or (V + 15) // 16 * 16
+    g = torch.Generator("cpu")
+    g.manual_seed(seed)
+    t = torch.full((M, cols + pitch), float("nan"), dtype=torch.bfloat16, device="cuda")
+    t[:, :V] = (torch.randn((M, V), generator=g) * std).to(torch.bfloat16).cuda()
+    return t[:, :cols]
+
+
+def make_targets(M, V, seed):
+    t = torch.from_numpy(np.random.default_rng(seed).integers(0, V, M))
+    t[::7] = -1
+    if M > 1:
+        t[1] = V - 1
+    return t.cuda()
+
+
+def forward(z, V, scale=1.0, targets=None, k=0, entropy=True, stream=None):
+    M = z.shape[0]
+    f32 = lambda *s: torch.full(s, 77.0, device="cuda")
+    r = dict(stats=f32(M, 2), logp=f32(M) if targets is not None else None, entropy=f32(M) if entropy else None,
+             top_ids=torch.full((M, k), -7, dtype=torch.int64, device="cuda") if k else None, top_logp=f32(M, k) if k else None)
+    ws = torch.full((f8.logits_workspace_bytes(M, V, k),), 255, dtype=torch.uint8, device="cuda")
+    f8.token_logprobs(z, V, r["stats"], targets, r["logp"], r["entropy"], r["top_ids"], r["top_logp"], scale, ws, stream)
+    return r
+
+
+def errors(zw, scale):
+    """(dl a row, factor of every p) as derived above, for rows with something left"""
+    M, V = zw.shape
+    with np.errstate(invalid="ignore", over="ignore"):
+        m = zw.max(axis=1, keepdims=True)
+        d = np.where(np.isfinite(m) & (zw > -np.inf), scale * (m - zw), 0.0)
+        p = np.where(zw > -np.inf, np.exp(-np.minimum(d, 800)), 0.0)
+        s = np.maximum(p.sum(axis=1, keepdims=True), 1e-300)
+    dl = (4 * U * (p / s * d).sum(axis=1) + (V / 512 + 48) * U + 2 * U * np.abs(np.log(s[:, 0])))
+    return dl, 4 * U * np.minimum(d, 800) + dl[:, None] + 8 * U, p / s, d + np.log(s)
+
+
+def check_forward(z, V, r, scale, targets, k):
+    zw = wide(z)[:, :V]
+    M = zw.shape[0]
+    t = None if targets is None else targets.cpu().numpy()
+    ref = ho.token_logprobs(zw, scale, t, k)
+    dl, fp, p, nl = errors(zw, scale)
+    got = f64(r["stats"])
+    assert np.array_equal(got[:, 0], ref["stats"][:, 0])
+    some = ref["stats"][:, 1] > -np.inf
+    assert np.array_equal(got[~some, 1], ref["stats"][~some, 1])
+    assert (np.abs(got[some, 1] - ref["stats"][some, 1]) <= dl[some]).all()
+
+    def logs_close(got, ref, dl):
+        # between the type's lowest and largest value lie 6.8e38, twice fp32's largest: the nearest fp32 value is -inf
+        with np.errstate(over="ignore"):
+            dead = ref.astype(np.float32) == -np.inf
+        assert np.array_equal(got == -np.inf, dead)
+        assert (np.abs(got[~dead] - ref[~dead]) <= np.broadcast_to(dl, got.shape)[~dead] + 6 * U * np.abs(ref[~dead])).all()
+    if t is not None:
+        # (z_t - z_max) scale = logp + log sum, each rounded: 6 U of logp and, within dl, 2 U of the log
+        logs_close(f64(r["logp"]), ref["logp"], 2 * dl)
+    if r["entropy"] is not None:
+        dh = 2 * dl + (p * nl * (fp + 4 * U)).sum(axis=1) + 8 * U * ref["entropy"] + (V / 512 + 48) * U * (p * nl).sum(axis=1)
+        assert (np.abs(f64(r["entropy"]) - ref["entropy"]) <= dh).all()
+    if k:
+        assert np.array_equal(r["top_ids"].cpu().numpy(), ref["top_ids"])
+        logs_close(f64(r["top_logp"]), ref["top_logp"], 2 * dl[:, None])
+    return ref
+
+
+def backward(z, V, r, scale, targets, d_logp, d_entropy, cols=None, out=None, amax=True, stream=None):
+    M = z.shape[0]
+    dz = out if out is not None else torch.full((M, cols or z.shape[1]), 9.0, dtype=torch.bfloat16, device="cuda")
+    am = torch.full((1,), -1.0, device="cuda") if amax else None
+    f8.token_logprobs_bwd(z, V, r["stats"], dz, targets, r["entropy"] if d_entropy is not None else None, d_logp, d_entropy, scale, am,
+                          f8.new_workspace(1, 1), stream)
+    return dz, am
+
+
+def check_gradient(zw, V, dz, am, ref, scale, weight, dh_weight=None):
+    """weight: the sum of the magnitudes that multiply p_j in each element, per row; dh_weight: |d_entropy| a row"""
+    got = wide(dz)
+    assert not got[:, V:].any()
+    _, fp, p, nl = errors(zw, scale)
+    mag = p * weight[:, None]
+    bound = HALF * np.abs(ref) + scale * mag * (fp + 16 * U)
+    if dh_weight is not None:
+        H = (p * nl).sum(axis=1, keepdims=True)
+        # the log of p_j is off by the factor of p_j, the entropy by as much in the mean
+        bound += scale * p * dh_weight[:, None] * ((nl + H) * (fp + 16 * U) + 2 * fp + 2 * (p * (fp + 16 * U) * (1 + nl)).sum(axis=1, keepdims=True)
+                                                   + (V / 512 + 48) * U * H)
+    bad = np.abs(got[:, :V] - ref) > bound + 1e-38
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4])
+    if am is not None:
+        assert am.item() == np.abs(got).max(initial=0.0)
+
+
+# vocabularies below, at and above what a thread, a block and a row's pieces take; odd ones; few rows (shared by blocks) and many
+SIZES = [(1, 1, 1), (2, 7, 3), (5, 8, 8), (3, 100, 20), (9, 513, 5), (4, 4099, 64), (2, 20000, 128), (1, 50001, 20), (70, 9001, 32), (600, 1000, 1),
+         (3, 131072, 128), (520, 8192, 10), (2, 300007, 50)]
+
+
+@pytest.mark.parametrize("M,V,k", SIZES)
+@pytest.mark.parametrize("scale", (1.0, 0.3))
+def test_logprobs_against_the_oracle(M, V, k, scale):
+    z = make_logits(M, V, M + V)
+    targets = make_targets(M, V, V)
+    r = forward(z, V, scale, targets, k)
+    torch.cuda.synchronize()
+    check_forward(z, V, r, scale, targets, k)
+    g = torch.Generator("cpu")
+    g.manual_seed(V)
+    d_logp, d_entropy = torch.randn(M, generator=g).cuda(), torch.randn(M, generator=g).cuda()
+    zw, t = wide(z)[:, :V], targets.cpu().numpy()
+    wl, wh = np.abs(f64(d_logp)) * (t >= 0), np.abs(f64(d_entropy))
+    for dlp, dh in ((d_logp, None), (d_logp, d_entropy), (None, d_entropy)):
+        tt = targets if dlp is not None else None
+        dz, am = backward(z, V, r, scale, tt, dlp, dh)
+        torch.cuda.synchronize()
+        ref = ho.token_logprobs_bwd(zw, scale, t, None if dlp is None else f64(dlp), None if dh is None else f64(dh))
+        check_gradient(zw, V, dz, am, ref, scale, wl if dlp is not None else 0 * wl, wh if dh is not None else None)
+
+
+def test_outputs_do_not_depend_on_which_are_asked_for():
+    M, V = 6, 70000
+    z, targets = make_logits(M, V, 1), make_targets(M, V, 1)
+    full = forward(z, V, 1.0, targets, 16)
+    for entropy in (False, True):
+        for k in (0, 3, 16):
+            r = forward(z, V, 1.0, targets, k, entropy)
+            assert torch.equal(r["stats"], full["stats"]) and torch.equal(r["logp"], full["logp"])
+            if entropy:
+                assert torch.equal(r["entropy"], full["entropy"])
+            if k:
+                assert torch.equal(r["top_ids"], full["top_ids"][:, :k]) and torch.equal(r["top_logp"], full["top_logp"][:, :k])
+    alone = forward(z, V)
+    assert torch.equal(alone["stats"], full["stats"])
+
+
+def special_rows(V):
+    g = np.random.default_rng(V)
+    rows = {
+        "one value": np.full(V, 1.5),
+        "both zeros": np.where(g.random(V) < 0.5, 0.0, -0.0),
+        "nothing left": np.full(V, -np.inf),
+        "one left": np.where(np.arange(V) == V // 2, -2.0, -np.inf),
+        "a few left": np.where(np.arange(V) % 997 == 3, g.normal(size=V), -np.inf),
+        "a stretch left": np.where((np.arange(V) > V // 3) & (np.arange(V) < V // 3 + 300), g.normal(size=V), -np.inf),
+        "all lowest": np.full(V, LOWEST),
+        "lowest as a mask": np.where(np.arange(V) % 3 == 0, g.normal(size=V), LOWEST),
+        "lowest and -inf": np.where(np.arange(V) % 2 == 0, LOWEST, -np.inf),
+        "largest": np.where(np.arange(V) == 5, -LOWEST, LOWEST),
+        "far above": 1000.0 + g.normal(size=V),
+        "ascending": np.linspace(-8, 8, V),
+        "descending": np.linspace(8, -8, V),
+        "large ones a block's threads apart": np.where(np.arange(V) // 8 % 512 < 3, 5 + g.random(V), g.normal(size=V) * 0.01),
+        "every element of some threads": np.where(np.arange(V) // 8 % 512 < 60, 5 + g.random(V), -1.0),
+        "few values": np.round(g.normal(size=V)),
+    }
+    return list(rows), np.stack(list(rows.values()))
+
+
+# rows shared by blocks (few), and a row a block (many copies), with a length that no chunk divides
+@pytest.mark.parametrize("V,copies,k", [(41, 1, 20), (5003, 1, 128), (5003, 40, 64), (100003, 1, 100), (100003, 40, 128)])
+def test_masked_tied_and_ordered_rows(V, copies, k):
+    names, rows = special_rows(V)
+    n = len(names)
+    z = torch.full((n * copies, (V + 15) // 16 * 16), float("nan"), dtype=torch.bfloat16, device="cuda")
+    z[:, :V] = torch.from_numpy(np.tile(rows, (copies, 1)).astype(np.float32)).to(torch.bfloat16).cuda()
+    targets = torch.full((n * copies,), V // 2, dtype=torch.int64, device="cuda")
+    r = forward(z, V, 1.0, targets, k)
+    first = {key: v[:n] for key, v in r.items()}
+    for key, v in r.items():  # every copy alike
+        assert torch.equal(v, first[key].repeat((copies,) + (1,) * (v.dim() - 1))), key
+    check_forward(z[:n], V, first, 1.0, targets[:n], k)
+    d = torch.ones(n * copies, device="cuda")
+    dz, am = backward(z, V, r, 1.0, targets, d, 0.5 * d)
+    torch.cuda.synchronize()
+    zw = wide(z[:n])[:, :V]
+    ref = ho.token_logprobs_bwd(zw, 1.0, targets[:n].cpu().numpy(), np.ones(n), 0.5 * np.ones(n))
+    assert torch.equal(dz.view(torch.int16), dz[:n].repeat(copies, 1).view(torch.int16))
+    check_gradient(zw, V, dz[:n], am, ref, 1.0, np.ones(n), 0.5 * np.ones(n))
+
+
+@pytest.mark.parametrize("M", (3, 600))
+def test_rows_with_nan_or_infinity_are_nan_and_stay_alone(M):
+    V, k = 9000, 40
+    z = make_logits(M, V, 5)
+    z[0, 17], z[2, 8999] = float("nan"), float("inf")
+    targets = torch.full((M,), 3, dtype=torch.int64, device="cuda")
+    r = forward(z, V, 1.0, targets, k)
+    dz, _ = backward(z, V, r, 1.0, targets, torch.ones(M, device="cuda"), torch.ones(M, device="cuda"), amax=False)
+    torch.cuda.synchronize()
+    for row in (0, 2):
+        assert torch.isnan(r["logp"][row]) and torch.isnan(r["entropy"][row]) and torch.isnan(r["stats"][row, 1]) and torch.isnan(r["top_logp"][row]).all()
+        ids = r["top_ids"][row]
+        assert ((ids >= 0) & (ids < V)).all() and len(set(ids.tolist())) == k
+        assert torch.isnan(dz[row, :V]).all() and not dz[row, V:].any()
+    rest = [i for i in range(M) if i not in (0, 2)]
+    assert torch.isfinite(r["logp"][rest]).all() and torch.isfinite(dz[rest].float()).all()
+    check_forward(z[1:2], V, {key: v[1:2] for key, v in r.items()}, 1.0, targets[1:2], k)
+
+
+def test_tokens_that_are_none_or_beyond_the_vocabulary():
+    M, V = 4, 1000
+    z = make_logits(M, V, 6)
+    targets = torch.tensor([-1, V, 5, -100], device="cuda")
+    r = forward(z, V, 1.0, targets)
+    dz, _ = backward(z, V, r, 1.0, targets, torch.ones(M, device="cuda"), None, amax=False)
+    torch.cuda.synchronize()
+    assert r["logp"][0].item() == 0 and r["logp"][3].item() == 0 and torch.isnan(r["logp"][1]) and torch.isfinite(r["logp"][2])
+    assert not dz[0].any() and not dz[3].any() and torch.isnan(dz[1, :V]).all() and torch.isfinite(dz[2].float()).all()
+
+
+def test_pitches_in_place_and_no_rows():
+    M, V = 11, 1003
+    z = make_logits(M, V, 7, pitch=24)
+    targets = make_targets(M, V, 7)
+    d = torch.randn(M, device="cuda")
+    r = forward(z, V, 0.5, targets, 4)
+    check_forward(z, V, r, 0.5, targets, 4)
+    want, am = backward(z, V, r, 0.5, targets, d, d)
+    wider = torch.full((M, 1100 + 4), 9.0, dtype=torch.bfloat16, device="cuda")[:, :1088]
+    backward(z, V, r, 0.5, targets, d, d, out=wider)
+    torch.cuda.synchronize()
+    assert torch.equal(wider[:, :1008], want) and not wider[:, 1008:].any() and (wider.as_strided((M, 16), (1104, 1), 1088) == 9.0).all()
+    beside = z.as_strided((M, 24), (1008 + 24, 1), 1008).clone()
+    backward(z, V, r, 0.5, targets, d, d, out=z)
+    assert torch.equal(z, want)
+    assert torch.equal(z.as_strided((M, 24), (1008 + 24, 1), 1008).view(torch.int16), beside.view(torch.int16))
+    none = torch.empty((0, 1008), dtype=torch.bfloat16, device="cuda")
+    r = forward(none, V, 1.0, torch.empty(0, dtype=torch.int64, device="cuda"), 3)
+    _, am = backward(none, V, r, 1.0, torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda"), None)
+    torch.cuda.synchronize()
+    assert am.item() == 0
+
+
+def test_offsets_beyond_32_bits():
+    M, V = 16500, 131072   # 2.16e9 elements
+    z = torch.zeros((M, V), dtype=torch.bfloat16, device="cuda")
+    z[-3:] = make_logits(3, V, 8)
+    z[0] = z[-1]
+    targets = torch.full((M,), V - 1, dtype=torch.int64, device="cuda")
+    r = forward(z, V, 1.0, targets, 8)
+    tail = {k: v[-3:] for k, v in r.items()}
+    check_forward(z[-3:], V, tail, 1.0, targets[-3:], 8)
+    assert torch.equal(r["top_ids"][0], r["top_ids"][-1]) and r["logp"][0].item() == r["logp"][-1].item()
+    small, _ = backward(z[-3:], V, tail, 1.0, targets[-3:], torch.ones(3, device="cuda"), None, amax=False)
+    backward(z, V, r, 1.0, targets, torch.ones(M, device="cuda"), None, out=z, amax=False)
+    torch.cuda.synchronize()
+    assert torch.equal(z[-3:], small) and torch.equal(z[0], small[2])
+
+
+# ---- distillation ---------------------------------------------------------------------------------
+
+def make_teacher(zw, K, seed, ragged=True):
+    """ids the teacher's best on noisy logits, log probabilities of total mass 0.5 .. 0.95; some lists short, some ids twice"""
+    g = np.random.default_rng(seed)
+    M, V = zw.shape
+    ids = np.argsort(-(np.where(zw > -np.inf, zw, -50) + g.normal(size=(M, V))), axis=1)[:, :K].astype(np.int64)
+    if ids.shape[1] < K:
+        ids = np.concatenate([ids, np.full((M, K - ids.shape[1]), -1)], axis=1)
+    t = np.log(g.dirichlet(np.ones(K), size=M) * g.uniform(0.5, 0.95, size=(M, 1)) + 1e-6).astype(np.float32)
+    if ragged and M > 3 and K > 3:
+        ids[1, 1:] = -1
+        ids[2] = -1
+        ids[3, 2] = ids[3, 0]
+        t[0, 1] = -np.inf
+    return np.ascontiguousarray(ids), t
+
+
+def distill_forward(z, V, ids, t, scale, tail, ts, targets=None, stream=None):
+    M = z.shape[0]
+    r = dict(stats=torch.full((M, 4), 77.0, device="cuda"), loss=torch.full((M,), 77.0, device="cuda"),
+             logp=torch.full((M,), 77.0, device="cuda") if targets is not None else None)
+    ws = torch.full((f8.logits_workspace_bytes(M, V),), 255, dtype=torch.uint8, device="cuda")
+    f8.distill(z, V, ids, t, r["stats"], r["loss"], targets, r["logp"], tail, ts, scale, ws, stream)
+    return r
+
+
+def distill_backward(z, V, ids, t, r, d_loss, scale, tail, ts, targets=None, d_logp=None, out=None, stream=None):
+    dz = out if out is not None else torch.full(z.shape, 9.0, dtype=torch.bfloat16, device="cuda")
+    am = torch.full((1,), -1.0, device="cuda")
+    f8.distill_bwd(z, V, ids, t, r["stats"], dz, d_loss, targets, d_logp, tail, ts, scale, am, f8.new_workspace(1, 1), stream)
+    return dz, am
+
+
+def check_distill(zw, ids, t, r, dz, am, scale, tail, ts, d_loss, targets, d_logp):
+    """Beside the student's errors: the teacher's weights, exp of a value that was scaled and shifted in fp32, are off by a
+    factor of 4 u (|t| + 4); the coefficient of the unlisted in the mode with the rest's class, 1 - q_rest / p_rest, by what
+    q_rest = 1 - sum q inherits, relative to p_rest."""
+    M, V = zw.shape
+    dl, fp, p, nl = errors(zw, scale)
+    ref = ho.distill(zw, ids, t, scale, tail, ts)
+    there = (ids >= 0) & (t > -np.inf)
+    tt = np.where(there, t * ts, 0.0)
+    q = np.zeros(t.shape)
+    for i in range(M):
+        cols, w = ho._teacher_row(ids[i], t[i].astype(np.float64), tail, ts)
+        q[i, there[i]] = w
+    dq = 4 * U * (np.abs(tt).max(axis=1) + 4) + 8 * U               # of every weight, relative
+    nlk = np.take_along_axis(nl, np.maximum(ids, 0), axis=1)
+    with np.errstate(divide="ignore"):
+        lq = np.where(q > 0, np.log(np.where(q > 0, q, 1.0)), 0.0)
+    fk = np.take_along_axis(fp, np.maximum(ids, 0), axis=1)
+    bound = (q * (2 * dq[:, None] * (1 + np.abs(lq) + nlk) + 2 * fk + 4 * U * nlk)).sum(axis=1) + 2 * dl + 4 * U * np.abs(ref)
+    listed = np.zeros((M, V), dtype=bool)
+    for i in range(M):
+        listed[i, ids[i][ids[i] >= 0]] = True
+    dcoef = np.full(M, 4 * U)
+    if tail:
+        q_rest = np.maximum(1 - q.sum(axis=1), 0)
+        p_rest = np.where(listed, 0, p).sum(axis=1)
+        f_rest = np.where(listed, 0, p * fp).sum(axis=1) / np.maximum(p_rest, 1e-300) + 2 * dl + (V / 512 + 48) * U
+        dr = (q.sum(axis=1) * dq + 4 * U)
+        with np.errstate(divide="ignore", invalid="ignore"):
+            bound += np.where(q_rest > 0, dr * (1 + np.abs(np.log(q_rest)) + np.abs(np.log(p_rest))) + q_rest * (f_rest + 4 * U * np.abs(np.log(p_rest))) + dr, 0)
+            dcoef = np.where(p_rest > 0, (dr + q_rest * (f_rest + 8 * U)) / p_rest + 4 * U, 0.0)
+    got, finite = f64(r["loss"]), np.isfinite(ref)   # infinite where a class with weight has no probability
+    assert np.array_equal(got[~finite], ref[~finite])
+    assert (np.abs(got[finite] - ref[finite]) <= bound[finite]).all(), (np.abs(got[finite] - ref[finite]) / bound[finite]).max()
+    rd = ho.distill_bwd(zw, ids, t.astype(np.float64), d_loss, scale, tail, ts, targets, d_logp)
+    got = wide(dz)
+    assert not got[:, V:].any()
+    w = np.abs(d_loss) if d_logp is None else np.abs(d_loss) + np.abs(d_logp) * (targets >= 0)
+    qs = np.zeros((M, V))
+    for i in range(M):
+        np.add.at(qs[i], ids[i][ids[i] >= 0], q[i][ids[i] >= 0])
+    with np.errstate(invalid="ignore"):
+        coef = np.where(listed, 1.0, np.abs(np.where(p_rest > 0, 1 - q_rest / np.where(p_rest > 0, p_rest, 1), 0.0))[:, None]) if tail else np.ones((M, V))
+    bound = HALF * np.abs(rd) + scale * (p * w[:, None] * (1 + coef) * (fp + 16 * U) + np.where(listed, 0, p * (np.abs(d_loss) * dcoef)[:, None])
+                                         + np.abs(d_loss)[:, None] * qs * (dq[:, None] + 8 * U))
+    bad = np.abs(got[:, :V] - rd) > bound + 1e-38
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4])
+    assert am.item() == np.abs(got).max(initial=0.0)
+
+
+@pytest.mark.parametrize("M,V,K", [(1, 100, 1), (5, 37, 37), (6, 513, 128), (40, 5003, 16), (3, 50001, 100), (600, 1000, 8), (4, 131072, 64), (530, 9001, 128),
+                                   (4, 140001, 10)])
+@pytest.mark.parametrize("tail", (False, True))
+def test_distill_against_the_oracle(M, V, K, tail):
+    scale, ts = 0.7, 1.0 if tail else 1.4
+    z = make_logits(M, V, M * V + K)
+    zw = wide(z)[:, :V]
+    ids, t = make_teacher(zw, K, V)
+    targets = make_targets(M, V, K)
+    g = np.random.default_rng(K)
+    d_loss, d_logp = (g.normal(size=M).astype(np.float32) for _ in range(2))
+    di, dt = torch.from_numpy(ids).cuda(), torch.from_numpy(t).cuda()
+    dv, dw = torch.from_numpy(d_loss).cuda(), torch.from_numpy(d_logp).cuda()
+    for hard in (False, True):
+        r = distill_forward(z, V, di, dt, scale, tail, ts, targets if hard else None)
+        dz, am = distill_backward(z, V, di, dt, r, dv, scale, tail, ts, targets if hard else None, dw if hard else None)
+        torch.cuda.synchronize()
+        tn = targets.cpu().numpy()
+        check_distill(zw, ids, t, r, dz, am, scale, tail, ts, d_loss.astype(np.float64), tn if hard else None, d_logp.astype(np.float64) if hard else None)
+        if hard:
+            lone = forward(z, V, scale, targets)
+            dl, _, _, _ = errors(zw, scale)
+            assert (np.abs(f64(r["logp"]) - f64(lone["logp"])) <= 4 * dl + 12 * U * np.abs(f64(lone["logp"]))).all()
+
+
+@pytest.mark.parametrize("M", (4, 560))
+def test_distill_masked_students_and_lists(M):
+    """A student row with nothing left; listed tokens that the student masks; the whole vocabulary listed; ids beyond it."""
+    V, K = 2050, 6
+    z = make_logits(M, V, 9)
+    z[0] = float("-inf")
+    ids = torch.arange(K, device="cuda").repeat(M, 1)
+    t = torch.log_softmax(torch.randn(M, K, device="cuda"), dim=1) - 0.1
+    z[1, 3] = float("-inf")              # a listed token without probability: an infinite loss, a finite gradient
+    z[2, K:V] = float("-inf")            # nothing outside the list
+    ids[3, 4] = V
+    one = torch.ones(M, device="cuda")
+    for tail in (False, True):
+        r = distill_forward(z, V, ids, t, 1.0, tail, 1.0)
+        dz, _ = distill_backward(z, V, ids, t, r, one, 1.0, tail, 1.0)
+        torch.cuda.synchronize()
+        loss, d = r["loss"], dz.float()
+        assert loss[0].item() == float("inf") and not dz[0].any()
+        assert loss[1].item() == float("inf") and torch.isfinite(d[1]).all()
+        assert torch.isfinite(d[2]).all() and (loss[2].item() == float("inf")) == tail
+        assert torch.isnan(loss[3]) and torch.isnan(d[3, :V]).any()
+        if M > 4:
+            zw = wide(z[4:])[:, :V]
+            check_distill(zw, ids[4:].cpu().numpy(), t[4:].cpu().numpy(), {k: v[4:] if v is not None else None for k, v in r.items()}, dz[4:],
+                          dz[4:].float().abs().max().reshape(1), 1.0, tail, 1.0, np.ones(M - 4), None, None)
+
+
+def test_a_teachers_own_pass_feeds_the_student():
+    """top_ids and top_logp of one call are the lists of the other; a student that is the teacher has nothing to learn."""
+    M, V, K = 12, 4000, 32
+    z = make_logits(M, V, 10)
+    teacher = forward(z, V, 1.0, None, K, entropy=False)
+    r = distill_forward(z, V, teacher["top_ids"], teacher["top_logp"], 1.0, True, 1.0)
+    dz, _ = distill_backward(z, V, teacher["top_ids"], teacher["top_logp"], r, torch.ones(M, device="cuda"), 1.0, True, 1.0)
+    torch.cuda.synchronize()
+    # the loss is second order in the errors of p and q, first order in their sums': some 100 roundings of terms up to log V
+    assert r["loss"].abs().max().item() <= 200 * U * np.log(V)
+    # q_j - p_j and (1 - q_rest / p_rest) p_j: a few roundings of log p (some 10) in p_j <= 1, and those of the masses
+    assert dz.float().abs().max().item() <= 400 * U * 10
+
+
+@pytest.mark.parametrize("which", ("logprobs", "distill"))
+def test_streams_graphs_and_repeats(which):
+    M, V, k = 40, 30011, 12
+    z = make_logits(M, V, 11)
+    targets = make_targets(M, V, 11)
+    ids, t = make_teacher(wide(z)[:, :V], k, 11)
+    ids, t = torch.from_numpy(ids).cuda(), torch.from_numpy(t).cuda()
+    d = torch.randn(M, device="cuda")
+    out = dict(stats=torch.empty(M, 2 if which == "logprobs" else 4, device="cuda"), logp=torch.empty(M, device="cuda"), ent=torch.empty(M, device="cuda"),
+               loss=torch.empty(M, device="cuda"), ids=torch.empty(M, k, dtype=torch.int64, device="cuda"), top=torch.empty(M, k, device="cuda"),
+               dz=torch.empty_like(z), am=torch.empty(1, device="cuda"))
+    ws = torch.empty(f8.logits_workspace_bytes(M, V, k), dtype=torch.uint8, device="cuda")
+
+    def step():
+        if which == "logprobs":
+            f8.token_logprobs(z, V, out["stats"], targets, out["logp"], out["ent"], out["ids"], out["top"], 0.9, ws)
+            f8.token_logprobs_bwd(z, V, out["stats"], out["dz"], targets, out["ent"], d, d, 0.9, out["am"], ws)
+        else:
+            f8.distill(z, V, ids, t, out["stats"], out["loss"], targets, out["logp"], True, 1.0, 0.9, ws)
+            f8.distill_bwd(z, V, ids, t, out["stats"], out["dz"], d, targets, d, True, 1.0, 0.9, out["am"], ws)
+    written = ["stats", "logp", "dz", "am"] + (["ent", "ids", "top"] if which == "logprobs" else ["loss"])
+    snapshot = lambda: {n: out[n].clone().view(torch.uint8) for n in written}
+    step()
+    torch.cuda.synchronize()
+    want = snapshot()
+    side = torch.cuda.Stream()
+    for n in written:
+        out[n].zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    got = snapshot()
+    assert all(torch.equal(got[n], want[n]) for n in written)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        z[:, :V] = (torch.randn(M, V, device="cuda") * (1 + i)).to(torch.bfloat16)
+        d.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = snapshot()
+        for n in written:
+            out[n].zero_()
+        step()
+        torch.cuda.synchronize()
+        want = snapshot()
+        assert all(torch.equal(got[n], want[n]) for n in written), i
+
+
+def test_two_calls_at_once():
+    """Streams with workspaces and outputs of their own."""
+    V, k = 60000, 20
+    z = [make_logits(3, V, 20 + i) for i in range(2)]
+    want = [forward(x, V, 1.0, None, k) for x in z]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for x, s in zip(z, streams):
+        with torch.cuda.stream(s):
+            got.append(forward(x, V, 1.0, None, k))
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(a[n], b[n]) for n in ("stats", "entropy", "top_ids", "top_logp"))
