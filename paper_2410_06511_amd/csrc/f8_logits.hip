@@ -10,60 +10,73 @@
 // fp32 where their ratio is below 2^16, so that p keeps its precision however large the logits are, which one number lse would not.
 #include <float.h>
 
+#include <type_traits>
+
 #include "f8_device.hpp"
 #include "f8_host.hpp"
 
 namespace f8 {
 
-constexpr int kLgThreads = 512;
+constexpr int kLgThreads = 256;
 constexpr int kLgWaves = kLgThreads / kWave;
-constexpr int kLgUnroll = 4;            // 16-byte loads in flight a thread
-constexpr int kLgSegCols = 131072;      // columns that a block takes at most: its chunks' maxima are 2 bytes each in LDS
+constexpr int kLgUnroll = 4;            // 16-byte loads in flight a thread: the chunks of one step
+constexpr int kLgSegCols = 131072;      // columns that a block takes at most
 constexpr int kLgMaxSeg = 32;           // blocks that share a row, at most
 constexpr int64_t kLgMaxCols = (int64_t)kLgSegCols * kLgMaxSeg;
 constexpr int kLgMaxTop = 128;          // alternatives, and entries of a teacher's list
 constexpr int kLgCandidates = 1024;     // elements that the selection ranks at once
-constexpr int kLgGradBlocks = 1024;     // of the gradient: one partial maximum each
+constexpr int kLgGradBlocks = 2048;     // of the gradient: one partial maximum each
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint32_t kNegInf2 = 0xFF80FF80u;
 static_assert((size_t)kLgGradBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial maximum per block fits the minimum workspace");
+static_assert(kLgMaxTop <= kLgThreads, "a thread an entry");
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---- statistics of a softmax, joined over lanes, waves and blocks -------------------------------
 
-// m: largest logit seen (-FLT_MAX: none but -inf), s = sum e, d = sum e log2(e), e = exp(scale (z - m)); c = scale * log2(e).
+// m: largest logit seen (-FLT_MAX: none but -inf), s = sum e, e = exp(scale (z - m)); c = scale * log2(e);
+// d: sum e log2(e) (ENT), or a second sum of e (a teacher's listed entries).
 // Exponents end at kFar, where e is 0: differences of masked values (-inf, the type's lowest) would make 0 * inf.
 constexpr float kFar = -1000.0f;
 struct Stat {
     float m, s, d;
 };
+// v as seen from a larger maximum
+template <bool ENT>
+__device__ inline Stat raised(const Stat& v, float m, float c)
+{
+    const float g = fmaxf((v.m - m) * c, kFar), f = exp2_hw(g);
+    return {m, v.s * f, f * (ENT ? v.d + v.s * g : v.d)};
+}
+template <bool ENT>
 __device__ inline Stat join(const Stat& a, const Stat& b, float c)
 {
-    const float m = fmaxf(a.m, b.m), ga = fmaxf((a.m - m) * c, kFar), gb = fmaxf((b.m - m) * c, kFar), fa = exp2_hw(ga), fb = exp2_hw(gb);
-    return {m, a.s * fa + b.s * fb, fa * (a.d + a.s * ga) + fb * (b.d + b.s * gb)};
+    const float m = fmaxf(a.m, b.m);
+    const Stat x = raised<ENT>(a, m, c), y = raised<ENT>(b, m, c);
+    return {m, x.s + y.s, x.d + y.d};
 }
+template <bool ENT>
 __device__ inline Stat wave_join(Stat v, float c)
 {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1)
-        v = join(v, {__shfl_xor(v.m, off, kWave), __shfl_xor(v.s, off, kWave), __shfl_xor(v.d, off, kWave)}, c);
+        v = join<ENT>(v, {__shfl_xor(v.m, off, kWave), __shfl_xor(v.s, off, kWave), __shfl_xor(v.d, off, kWave)}, c);
     return v;
 }
 
 // ---- order of logits -----------------------------------------------------------------------------
 
-// bf16 bits -> 16 bits whose integer order is that of the values; both zeros alike, NaN below everything
+// bf16 bits -> 16 bits whose integer order is that of the values; both zeros alike, NaN as -inf (0x7F, the least)
 __device__ inline uint32_t order16(uint32_t b)
 {
-    b = b == 0x8000u ? 0u : b;
-    return (b & 0x7FFFu) > 0x7F80u ? 0u : b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;
+    b = b == 0x8000u ? 0u : (b & 0x7FFFu) > 0x7F80u ? 0xFF80u : b;
+    return b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;
 }
 __device__ inline float order_value(uint32_t o) { return __uint_as_float((o & 0x8000u ? o & 0x7FFFu : ~o & 0xFFFFu) << 16); }
 // elements in their order, the lower column first among equals
 __device__ inline uint64_t element_key(uint32_t o, uint32_t col) { return (uint64_t)o << 32 | (uint32_t)~col; }
 __device__ inline uint32_t key_column(uint64_t k) { return ~(uint32_t)k; }
-__device__ inline uint32_t chunk_key(uint32_t o, int lc) { return o << 16 | (uint32_t)(65535 - lc); }
 
 __device__ inline void unpack(uint4 v, float* z)
 {
@@ -87,52 +100,47 @@ __device__ inline uint4 load_logits(const uint4* row, int c, int V)
 
 // ---- a teacher's list in LDS ----------------------------------------------------------------------
 
-// The entries of one row that fall into a block's columns.  head[chunk] is the last entry (+ 1) of the chunk, next[] the one before
-// it, so that a sweep asks one byte a chunk; an id that occurs again is dropped after its weight went to the first.
+// The entries of one row that fall into a block's columns.  A chunk that holds some is marked by a bit; the sweep leaves it out,
+// and the thread of its first entry takes it with all its entries.
 struct List {
-    int id[kLgMaxTop];       // column, -1: none
+    int id[kLgMaxTop];  // column, -1: none here
     float q[kLgMaxTop];
-    uint8_t next[kLgMaxTop];
+    uint32_t marks[kLgSegCols / 8 / 32];
+    __device__ bool marked(int lc) const { return marks[lc >> 5] >> (lc & 31) & 1; }
 };
-// Threads below K bring their entry (q: its weight); all threads call.
-__device__ inline void list_store(List& L, int K, int id, float q)
+// Threads below K bring their entry (q: its weight), all threads call; chunks c0 .. c1 - 1.
+__device__ inline void list_fill(List& L, int K, int64_t id, float q, int c0, int c1)
 {
     const int k = threadIdx.x;
+    const bool here = k < K && id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8;
+    for (int i = k; i < (c1 - c0 + 31) / 32; i += kLgThreads) L.marks[i] = 0;
+    if (k < K) L.id[k] = here ? (int)id : -1, L.q[k] = q;
     __syncthreads();
-    if (k < K) L.id[k] = id, L.q[k] = q;
+    if (here) atomicOr(&L.marks[((int)id / 8 - c0) >> 5], 1u << (((int)id / 8 - c0) & 31));
     __syncthreads();
-    bool first = k < K && id >= 0;
-    if (first) {
-        float sum = 0.0f;
-        for (int j = 0; j < K; ++j)
-            if (L.id[j] == id) {
-                if (j < k) first = false;
-                sum += L.q[j];
-            }
-        q = sum;
-    }
-    __syncthreads();
-    if (k < K) L.id[k] = first ? id : -1, L.q[k] = q;
 }
-// the heads of chunks c0 .. c1 - 1
-__device__ inline void list_heads(List& L, int K, uint8_t* head, int c0, int c1)
+// The chunk that this thread takes (-1: none): which of its elements are listed, and their weights (an id that occurs again
+// counts with each of its weights).
+__device__ inline int list_chunk(const List& L, int K, uint32_t* mask, float* w)
 {
-    for (int i = threadIdx.x; i < (c1 - c0 + 3) / 4; i += kLgThreads) reinterpret_cast<uint32_t*>(head)[i] = 0;
-    __syncthreads();
-    const int k = threadIdx.x;
-    if (k < K && L.id[k] >= 0) {
-        const int c = L.id[k] >> 3;
-        int before = 0;
-        bool last = true;
-        for (int j = 0; j < K; ++j)
-            if (j != k && L.id[j] >= 0 && L.id[j] >> 3 == c) {
-                if (j < k) before = j + 1;
-                else last = false;
-            }
-        L.next[k] = (uint8_t)before;
-        if (last && c >= c0 && c < c1) head[c - c0] = (uint8_t)(k + 1);
+    const int k = threadIdx.x, id = k < K ? L.id[k] : -1;
+    int c = id >> 3;
+    if (id < 0) return -1;
+    *mask = 1u << (id & 7);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = e == (id & 7) ? L.q[k] : 0.0f;
+    const int own = c;
+#pragma unroll 8
+    for (int j = 0; j < K; ++j) {
+        const int other = L.id[j];
+        if (j != k && other >> 3 == own) {  // (-1 >> 3 is no chunk)
+            if (j < k) c = -1;
+            *mask |= 1u << (other & 7);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] += e == (other & 7) ? L.q[j] : 0.0f;
+        }
     }
-    __syncthreads();
+    return c;
 }
 
 // ---- forward ---------------------------------------------------------------------------------------
@@ -162,17 +170,17 @@ struct StatArgs {
 constexpr double kNoRest = 0x1p-20;
 
 // What a row's outputs are, from its statistics; called by one whole wave.
-// With a teacher: rest is the sum outside the list where the remainder is a class (v.s then lacks the list's part).
+// With a teacher whose remainder is a class of its own v.s is the sum outside the list and v.d the list's.
 template <bool LIST>
-__device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v, const List* L)
+__device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v)
 {
     const int lane = threadIdx.x & (kWave - 1);
     const uint16_t* z = a.logits + row * a.ld;
     constexpr int E = kLgMaxTop / kWave;
-    float zk[E] = {}, total = v.s;
+    float zk[E] = {};
+    const float total = LIST ? v.s + v.d : v.s;
     bool has[E] = {}, wrong = false;
     if constexpr (LIST) {
-        float listed = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int k = lane + kWave * e;
@@ -180,14 +188,7 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v, const 
             const int64_t id = a.t.ids[row * a.t.K + k];
             has[e] = id >= 0 && id < a.V;
             wrong |= id >= a.V;
-            if (!has[e]) continue;
-            zk[e] = (__uint_as_float((uint32_t)z[id] << 16) - v.m) * a.scale;
-            if (a.t.tail && L->id[k] >= 0) listed += exp2_hw(zk[e] * kLog2e);
-        }
-        if (a.t.tail) {
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) listed += __shfl_xor(listed, off, kWave);
-            total += listed;
+            if (has[e]) zk[e] = (__uint_as_float((uint32_t)z[id] << 16) - v.m) * a.scale;
         }
     }
     const bool none = total == 0.0f;  // every logit is -inf
@@ -249,104 +250,149 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v, const 
     }
 }
 
-// The K largest of a block's elements, in order: emit(rank, key).
-// Every thread has the key of its best chunk (order of the chunk's maximum, the lower chunk first among equals).  The K-th
-// largest of these keys bounds the search: at least K elements reach it, so the K best do, and they lie in chunks that
-// reach it, which are read again: about K of them where the large elements are spread.  What reaches the bound is ranked by counting.
-// Rows built so that more than kLgCandidates elements reach it (their largest share few threads) take a search by halves.
-template <class Emit>
-__device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K, uint32_t best, const uint16_t* cmax, uint64_t* cand, uint32_t* words, Emit&& emit)
+// Selection of a block's K largest elements.  A step's chunks of one thread (32 elements) leave their maximum in LDS, 2 bytes,
+// and every thread knows its own largest.  The K-th largest of these bounds the search: K elements reach it, so the K best do, and
+// they lie in steps whose maximum does.  Those are read again (about K, where the large elements are spread) and what reaches the
+// bound is ranked by counting.
+struct Select {
+    uint64_t cand[kLgCandidates];
+    uint16_t step[kLgCandidates];
+    uint32_t best[kLgThreads];
+    uint32_t bound, nstep, ncand;
+};
+
+// The largest value that at least K of the threads' maxima reach (every one of kLgThreads >= K has one, 0 if it saw nothing).
+__device__ inline uint32_t kth_best(const uint32_t* best, int K)
 {
-    const int tid = threadIdx.x, lane = tid & (kWave - 1);
-    uint32_t* keys = reinterpret_cast<uint32_t*>(cand);  // until the candidates come
-    static_assert(kLgThreads * sizeof(uint32_t) <= kLgCandidates * sizeof(uint64_t), "a key a thread");
-    keys[tid] = best;
-    if (tid == 0) words[0] = 0;
+    const int lane = threadIdx.x & (kWave - 1);
+    uint32_t k[kLgWaves], hi = 0, lo = 0;
+#pragma unroll
+    for (int i = 0; i < kLgWaves; ++i) k[i] = best[lane + kWave * i], hi = k[i] > hi ? k[i] : hi, lo = i == 0 || k[i] < lo ? k[i] : lo;
+    hi = wave_max_u32(hi), lo = ~wave_max_u32(~lo);
+    while (lo < hi) {
+        const uint32_t at = (lo + hi + 1) / 2;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kLgWaves; ++i) n += __popcll(__ballot(k[i] >= at));
+        if (n >= K) lo = at;
+        else hi = at - 1;
+    }
+    return lo;
+}
+
+// f(order, column) for the elements of chunk c that the row has
+template <class F>
+__device__ inline void each_element(const uint4* row, int c, int V, F&& f)
+{
+    const uint4 v = row[c];
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c * 8 + j < V) f(order16(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu), (uint32_t)(c * 8 + j));
+}
+
+// The K largest in order: emit(rank, key).  smax: maxima by step * kLgThreads + thread; best: of this thread.
+template <class Emit>
+__device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K, uint32_t best, const uint16_t* smax, Select& S, Emit&& emit)
+{
+    const int tid = threadIdx.x, steps = (c1 - c0 + kLgUnroll * kLgThreads - 1) / (kLgUnroll * kLgThreads);
+    S.best[tid] = best;
+    if (tid == 0) S.nstep = S.ncand = 0;
     __syncthreads();
     if (tid < kWave) {
-        uint32_t k[kLgWaves], t = 0;
-#pragma unroll
-        for (int i = 0; i < kLgWaves; ++i) k[i] = keys[lane + kWave * i];
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t at = t | 1u << bit;
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < kLgWaves; ++i) n += __popcll(__ballot(k[i] >= at));
-            if (n >= K) t = at;
-        }
-        if (lane == 0) words[1] = t;
+        const uint32_t t = kth_best(S.best, K);
+        if (tid == 0) S.bound = t;
     }
     __syncthreads();
-    const uint32_t bound = words[1];
-    auto collect = [&](uint64_t least) {  // elements of at least this key, of chunks that reach the bound
-        for (int c = c0 + tid; c < c1; c += kLgThreads) {
-            const int lc = c - c0;
-            if (chunk_key(cmax[lc], lc) < bound) continue;
-            const uint4 v = row[c];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t o = order16(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu);
-                const uint64_t key = element_key(o, (uint32_t)(c * 8 + j));
-                if (c * 8 + j < V && chunk_key(o, lc) >= bound && key >= least) {
-                    const uint32_t at = atomicAdd(words, 1u);
-                    if (at < (uint32_t)kLgCandidates) cand[at] = key;
-                }
-            }
-        }
+    const uint32_t bound = S.bound;
+    auto put = [&](uint32_t o, uint32_t col) {
+        const uint32_t at = atomicAdd(&S.ncand, 1u);
+        if (at < (uint32_t)kLgCandidates) S.cand[at] = element_key(o, col);
     };
-    collect(0);
-    __syncthreads();
-    uint32_t n = words[0];
-    if (n > (uint32_t)kLgCandidates) {
-        // the K-th largest key itself, bit by bit (the columns' upper bits are alike, but need no case of their own)
-        uint64_t t = 0;
-        for (int bit = 47; bit >= 0; --bit) {
-            const uint64_t at = t | (uint64_t)1 << bit;
-            __syncthreads();
-            if (tid == 0) words[0] = 0;
-            __syncthreads();
-            uint32_t mine = 0;
-            for (int c = c0 + tid; c < c1; c += kLgThreads) {
-                const int lc = c - c0;
-                if (chunk_key(cmax[lc], lc) < bound || cmax[lc] < (uint32_t)(at >> 32)) continue;
-                const uint4 v = row[c];
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t o = order16(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu);
-                    mine += c * 8 + j < V && chunk_key(o, lc) >= bound && element_key(o, (uint32_t)(c * 8 + j)) >= at;
-                }
+    if (best >= bound)
+        for (int i = 0; i < steps; ++i)
+            if (smax[i * kLgThreads + tid] >= bound && c0 + i * kLgUnroll * kLgThreads + tid < c1) {
+                const uint32_t at = atomicAdd(&S.nstep, 1u);
+                if (at < (uint32_t)kLgCandidates) S.step[at] = (uint16_t)(i * kLgThreads + tid);
             }
-            if (mine) atomicAdd(words, mine);
-            __syncthreads();
-            if (words[0] >= (uint32_t)K) t = at;
+    __syncthreads();
+    const uint32_t nstep = S.nstep;
+    if (nstep <= (uint32_t)kLgCandidates) {
+        for (uint32_t i = tid; i < nstep * kLgUnroll; i += kLgThreads) {
+            const int st = S.step[i / kLgUnroll], c = c0 + (st / kLgThreads * kLgUnroll + (int)(i % kLgUnroll)) * kLgThreads + st % kLgThreads;
+            if (c < c1) each_element(row, c, V, [&](uint32_t o, uint32_t col) { if (o >= bound) put(o, col); });
         }
         __syncthreads();
-        if (tid == 0) words[0] = 0;
+    }
+    uint32_t n = S.ncand;
+    if (nstep > (uint32_t)kLgCandidates || n > (uint32_t)kLgCandidates) {
+        // More equals of the bound than there is room for (rows of few values, or with little left by a mask): what is larger, and
+        // then the equals from the row's front until there are enough.
+        constexpr uint32_t kPiece = kWave * 8;  // elements of a wave's chunks
         __syncthreads();
-        collect(t);
+        if (tid == 0) S.ncand = 0;
         __syncthreads();
-        n = words[0];
+        if (best > bound)
+            for (int i = 0; i < steps; ++i)
+                if (smax[i * kLgThreads + tid] > bound)
+                    for (int u = 0; u < kLgUnroll; ++u) {
+                        const int c = c0 + (i * kLgUnroll + u) * kLgThreads + tid;
+                        if (c < c1) each_element(row, c, V, [&](uint32_t o, uint32_t col) { if (o > bound) put(o, col); });
+                    }
+        __syncthreads();
+        n = S.ncand;
+        if (n <= kLgCandidates - kPiece) {
+            for (int c = c0; c < c1 && n < (uint32_t)K; c += kWave) {
+                if (tid < kWave && c + tid < c1) each_element(row, c + tid, V, [&](uint32_t o, uint32_t col) { if (o == bound) put(o, col); });
+                __syncthreads();
+                n = S.ncand;
+                __syncthreads();
+            }
+        } else {
+            // Large elements that share few threads: the K-th largest key itself, bit by bit.
+            uint64_t t = 0;
+            for (int bit = 47; bit >= 0; --bit) {
+                const uint64_t at = t | (uint64_t)1 << bit;
+                __syncthreads();
+                if (tid == 0) S.ncand = 0;
+                __syncthreads();
+                uint32_t mine = 0;
+                for (int i = 0; i < steps; ++i)
+                    if (smax[i * kLgThreads + tid] >= (uint32_t)(at >> 32))
+                        for (int u = 0; u < kLgUnroll; ++u) {
+                            const int c = c0 + (i * kLgUnroll + u) * kLgThreads + tid;
+                            if (c < c1) each_element(row, c, V, [&](uint32_t o, uint32_t col) { mine += element_key(o, col) >= at; });
+                        }
+                if (mine) atomicAdd(&S.ncand, mine);
+                __syncthreads();
+                if (S.ncand >= (uint32_t)K) t = at;
+            }
+            __syncthreads();
+            if (tid == 0) S.ncand = 0;
+            __syncthreads();
+            for (int c = c0 + tid; c < c1; c += kLgThreads)
+                each_element(row, c, V, [&](uint32_t o, uint32_t col) { if (element_key(o, col) >= t) put(o, col); });
+            __syncthreads();
+            n = S.ncand;
+        }
     }
     for (uint32_t i = tid; i < n; i += kLgThreads) {
-        const uint64_t key = cand[i];
+        const uint64_t key = S.cand[i];
         int rank = 0;
-        for (uint32_t j = 0; j < n; ++j) rank += cand[j] > key;
+#pragma unroll 8
+        for (uint32_t j = 0; j < n; ++j) rank += S.cand[j] > key;
         if (rank < K) emit(rank, key);
     }
 }
 
-// One block takes one row, or one of nseg pieces of it.  LDS: chunk maxima (TOP) or the list's heads (LIST) by chunk.
+// One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.
 template <bool ENT, bool TOP, bool LIST>
 __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs a)
 {
-    extern __shared__ uint8_t by_chunk[];
+    extern __shared__ uint16_t smax[];
     __shared__ Stat wave_stat[kLgWaves];
-    __shared__ uint32_t words[2];
-    __shared__ uint64_t cand[TOP ? kLgCandidates : 1];
-    __shared__ List list[1];
-    uint16_t* cmax = reinterpret_cast<uint16_t*>(by_chunk);
+    __shared__ std::conditional_t<TOP, Select, int> sel;
+    __shared__ std::conditional_t<LIST, List, int> list;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int chunks = (a.V + 7) / 8;
     const float c2 = a.scale * kLog2e;
@@ -354,76 +400,73 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         const int64_t rowi = unit / a.nseg;
         const int seg = (int)(unit - rowi * a.nseg), c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
         const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
-        if (LIST && a.t.tail) {
-            int64_t id = -1;
-            if (tid < a.t.K) id = a.t.ids[rowi * a.t.K + tid];
-            list_store(list[0], a.t.K, id >= 0 && id < a.V ? (int)id : -1, 0.0f);
-            __syncthreads();
-            list_heads(list[0], a.t.K, by_chunk, c0, c1);
-        }
         Stat v = {-FLT_MAX, 0.0f, 0.0f};
         uint32_t best = 0;
-        for (int c = c0 + tid; c < c1; c += kLgUnroll * kLgThreads) {
+        const bool marks = LIST && a.t.tail;
+        if constexpr (LIST) {
+            if (marks) {
+                list_fill(list, a.t.K, tid < a.t.K ? a.t.ids[rowi * a.t.K + tid] : -1, 0.0f, c0, c1);
+                uint32_t mask;
+                float none[8];
+                const int c = list_chunk(list, a.t.K, &mask, none);
+                if (c >= 0) {
+                    float z[8];
+                    unpack(load_logits(row, c, a.V), z);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v.m = fmaxf(v.m, z[j]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float e = exp2_hw((z[j] - v.m) * c2);
+                        (mask >> j & 1 ? v.d : v.s) += e;
+                    }
+                }
+            }
+        }
+        for (int c = c0 + tid, step = 0; c < c1; c += kLgUnroll * kLgThreads, ++step) {
             uint4 w[kLgUnroll];
 #pragma unroll
             for (int u = 0; u < kLgUnroll; ++u) {
                 const int cu = c + u * kLgThreads;
-                w[u] = cu < c1 ? load_logits(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+                bool in = cu < c1;
+                if constexpr (LIST) in = in && !(marks && list.marked(cu - c0));
+                w[u] = in ? load_logits(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
             }
-            float m = v.m;
-            float z[kLgUnroll][8];
+            float z[kLgUnroll][8], m = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kLgUnroll; ++u) {
                 unpack(w[u], z[u]);
-                float cm = z[u][0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j) cm = fmaxf(cm, z[u][j]);
-                m = fmaxf(m, cm);
-                const int cu = c + u * kLgThreads;
-                if constexpr (TOP) {
-                    if (cu < c1) {
-                        const uint32_t o = order16(__float_as_uint(cm) >> 16);
-                        cmax[cu - c0] = (uint16_t)o;
-                        const uint32_t key = chunk_key(o, cu - c0);
-                        best = key > best ? key : best;
-                    }
-                }
-                if constexpr (LIST) {
-                    if (a.t.tail && cu < c1)
-                        for (int k = by_chunk[cu - c0]; k; k = list[0].next[k - 1]) {
-                            const int j0 = list[0].id[k - 1] & 7;
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) z[u][j] = j == j0 ? -INFINITY : z[u][j];
-                        }
-                }
+                for (int j = 0; j < 8; ++j) m = fmaxf(m, z[u][j]);
             }
-            const float gone = fmaxf((v.m - m) * c2, kFar), f = exp2_hw(gone);
-            if constexpr (ENT) v.d = f * (v.d + v.s * gone);
-            v.s *= f;
-            v.m = m;
+            if constexpr (TOP) {
+                const uint32_t o = order16(__float_as_uint(m) >> 16);
+                smax[step * kLgThreads + tid] = (uint16_t)o;
+                best = o > best ? o : best;
+            }
+            v = raised<ENT>(v, fmaxf(v.m, m), c2);
 #pragma unroll
             for (int u = 0; u < kLgUnroll; ++u)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float l = (z[u][j] - m) * c2, e = exp2_hw(l);
+                    const float l = (z[u][j] - v.m) * c2, e = exp2_hw(l);
                     v.s += e;
                     if constexpr (ENT) v.d += e * fmaxf(l, kFar);
                 }
         }
-        v = wave_join(v, c2);
+        v = wave_join<ENT>(v, c2);
         if (lane == 0) wave_stat[wave] = v;
         __syncthreads();
         v = wave_stat[0];
 #pragma unroll
-        for (int i = 1; i < kLgWaves; ++i) v = join(v, wave_stat[i], c2);
+        for (int i = 1; i < kLgWaves; ++i) v = join<ENT>(v, wave_stat[i], c2);
         if (a.nseg > 1) {
             if (tid == 0) a.part[unit] = make_float4(v.m, v.s, v.d, 0.0f);
         } else if (wave == 0) {
-            finish_row<LIST>(a, rowi, v, list);
+            finish_row<LIST>(a, rowi, v);
         }
         if constexpr (TOP) {
             const float log_total = logf(v.s);
-            block_top(row, c0, c1, a.V, a.top, best, cmax, cand, words, [&](int rank, uint64_t key) {
+            block_top(row, c0, c1, a.V, a.top, best, smax, sel, [&](int rank, uint64_t key) {
                 if (a.nseg > 1) {
                     a.part_top[unit * a.top + rank] = key;
                 } else {
@@ -437,11 +480,11 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
 }
 
 // Rows that blocks shared: their statistics, and the best of their elements.
-template <bool LIST>
+template <bool ENT, bool LIST>
 __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs a)
 {
-    extern __shared__ uint64_t lists[];  // [nseg][top]
-    __shared__ List list[1];
+    extern __shared__ uint64_t cand[];  // [nseg * top]
+    __shared__ uint32_t n;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const float c2 = a.scale * kLog2e;
     for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
@@ -450,36 +493,35 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
             const float4 p = a.part[row * a.nseg + lane];
             v = {p.x, p.y, p.z};
         }
-        v = wave_join(v, c2);
-        if (LIST && a.t.tail) {
-            int64_t id = -1;
-            if (tid < a.t.K) id = a.t.ids[row * a.t.K + tid];
-            list_store(list[0], a.t.K, id >= 0 && id < a.V ? (int)id : -1, 0.0f);
-            __syncthreads();
-        }
-        if (tid < kWave) finish_row<LIST>(a, row, v, list);
+        // a key that K of the pieces' elements reach: the least of the pieces' (K / nseg)-th
+        uint64_t least = ~(uint64_t)0;
+        const uint64_t* lists = a.part_top + row * a.nseg * a.top;
+        if (a.top && lane < a.nseg) least = lists[lane * a.top + (a.top + a.nseg - 1) / a.nseg - 1];
+        v = wave_join<ENT>(v, c2);
+        if (tid < kWave) finish_row<LIST>(a, row, v);
         if (a.top) {
-            const int K = a.top, n = a.nseg * K;
-            for (int i = tid; i < n; i += kLgThreads) lists[i] = a.part_top[row * n + i];
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) {
+                const uint64_t o = __shfl_xor(least, off, kWave);
+                least = o < least ? o : least;
+            }
+            if (tid == 0) n = 0;
+            __syncthreads();
+            for (int i = tid; i < a.nseg * a.top; i += kLgThreads) {
+                const uint64_t key = lists[i];
+                if (key >= least) cand[atomicAdd(&n, 1u)] = key;
+            }
             __syncthreads();
             const float log_total = logf(v.s);
-            for (int i = tid; i < n; i += kLgThreads) {
-                const uint64_t key = lists[i];
-                int rank = i % K;
-                for (int s = 0; s < a.nseg && rank < K; ++s) {
-                    const uint64_t* l = lists + s * K;
-                    if (s == i / K || l[0] < key) continue;
-                    int lo = 1, hi = K;  // how many of the list are larger
-                    while (lo < hi) {
-                        const int mid = (lo + hi) / 2;
-                        if (l[mid] > key) lo = mid + 1;
-                        else hi = mid;
-                    }
-                    rank += lo;
-                }
-                if (rank < K) {
-                    a.top_ids[row * K + rank] = key_column(key);
-                    a.top_logp[row * K + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
+            for (uint32_t i = tid; i < n; i += kLgThreads) {
+                const uint64_t key = cand[i];
+                int rank = 0;
+                for (uint32_t j = 0; j < n && rank < a.top; j += 8)
+#pragma unroll
+                    for (uint32_t k = j; k < j + 8; ++k) rank += k < n && cand[k] > key;
+                if (rank < a.top) {
+                    a.top_ids[row * a.top + rank] = key_column(key);
+                    a.top_logp[row * a.top + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
                 }
             }
         }
@@ -502,17 +544,17 @@ struct GradArgs {
     uint32_t* partial;
 };
 
+// Rows from the last one on: where they do not all fit the caches, the forward's last rows are still there.
 template <bool ENT, bool LIST>
 __global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs a)
 {
-    extern __shared__ uint8_t by_chunk[];
     __shared__ uint32_t red[kLgWaves];
-    __shared__ List list[1];
+    __shared__ std::conditional_t<LIST, List, int> list;
     const int tid = threadIdx.x;
     const int chunks = a.cols / 8, read = (a.V + 7) / 8;
     const float c2 = a.scale * kLog2e;
     uint32_t mag = 0;
-    for (int64_t unit = blockIdx.x; unit < a.M * a.nseg; unit += gridDim.x) {
+    for (int64_t unit = a.M * a.nseg - 1 - (int64_t)blockIdx.x; unit >= 0; unit -= gridDim.x) {
         const int64_t rowi = unit / a.nseg;
         const int seg = (int)(unit - rowi * a.nseg), c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
         const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
@@ -535,17 +577,43 @@ __global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs 
         }
         // nothing to hand back: no weight, or no logit that a change could move
         const bool zero = (A == 0.0f && B == 0.0f && dlp == 0.0f && g == 0.0f) || st[1] == -INFINITY;
+        // chunk cu of the row, with the listed ones among its elements
+        auto emit = [&](int cu, uint4 w, uint32_t mask, const float* q) {
+            float z[8];
+            unpack(w, z);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float l2 = __builtin_fmaf(z[j] - m, c2, -log2_total), p = exp2_hw(l2);
+                z[j] = ENT ? p * __builtin_fmaf(B, fmaxf(l2, kFar), A) : p * A;
+                if (LIST && q) z[j] = mask >> j & 1 ? p * AL - q[j] : z[j];
+            }
+            if (cu == (int)(target >> 3)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] += j == (int)(target & 7) ? dlp : 0.0f;
+            }
+            const int left = a.V - cu * 8;
+            if (left < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = j < left ? z[j] : 0.0f;
+            }
+            const uint4 o = make_uint4(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7]));
+            mag = absmax_acc(mag, o);
+            store_stream(out + cu, o);
+        };
         if constexpr (LIST) {
             if (!zero) {  // (alike for the whole block)
                 int64_t id = -1;
                 float q = 0.0f;
                 if (tid < a.t.K) {
                     id = a.t.ids[rowi * a.t.K + tid];
-                    if (id >= 0 && id < a.V) q = g == 0.0f ? 0.0f : g * expf(a.t.logp[rowi * a.t.K + tid] * a.t.scale - st[3]);
+                    if (id >= a.V) id = -1;
+                    if (id >= 0 && g != 0.0f) q = g * expf(a.t.logp[rowi * a.t.K + tid] * a.t.scale - st[3]);
                 }
-                list_store(list[0], a.t.K, id >= 0 && id < a.V ? (int)id : -1, q);
-                __syncthreads();
-                list_heads(list[0], a.t.K, by_chunk, c0, c1);
+                list_fill(list, a.t.K, id, q, c0, c1);
+                uint32_t mask;
+                float w[8];
+                const int c = list_chunk(list, a.t.K, &mask, w);
+                if (c >= 0) emit(c, load_logits(row, c, a.V), mask, w);
             }
         }
         for (int c = c0 + tid; c < c1; c += kLgUnroll * kLgThreads) {
@@ -559,37 +627,13 @@ __global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs 
             for (int u = 0; u < kLgUnroll; ++u) {
                 const int cu = c + u * kLgThreads;
                 if (cu >= c1) break;
-                uint4 o = make_uint4(0, 0, 0, 0);
-                if (!zero && cu < read) {
-                    float z[8], p[8];
-                    unpack(w[u], z);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float l2 = __builtin_fmaf(z[j] - m, c2, -log2_total);
-                        p[j] = exp2_hw(l2);
-                        z[j] = ENT ? p[j] * __builtin_fmaf(B, fmaxf(l2, kFar), A) : p[j] * A;
-                    }
-                    if constexpr (LIST) {
-                        for (int k = by_chunk[cu - c0]; k; k = list[0].next[k - 1]) {
-                            const int j0 = list[0].id[k - 1] & 7;
-                            const float q = list[0].q[k - 1];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) z[j] = j == j0 ? p[j] * AL - q : z[j];
-                        }
-                    }
-                    if (cu == (int)(target >> 3)) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) z[j] += j == (int)(target & 7) ? dlp : 0.0f;
-                    }
-                    const int left = a.V - cu * 8;
-                    if (left < 8) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) z[j] = j < left ? z[j] : 0.0f;
-                    }
-                    o = make_uint4(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7]));
-                    mag = absmax_acc(mag, o);
+                if (zero || cu >= read) {
+                    store_stream(out + cu, make_uint4(0, 0, 0, 0));
+                    continue;
                 }
-                store_stream(out + cu, o);
+                if constexpr (LIST)
+                    if (list.marked(cu - c0)) continue;
+                emit(cu, w[u], 0, nullptr);
             }
         }
         if constexpr (LIST) __syncthreads();  // LDS is used again
@@ -619,7 +663,7 @@ static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted)
     const int64_t per = (chunks + n - 1) / n;
     return {(int)((chunks + per - 1) / per), (int)per};
 }
-constexpr int64_t kLgBlocksWanted = 512;
+constexpr int64_t kLgBlocksWanted = 1024;
 
 static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
 {
@@ -657,7 +701,8 @@ static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_
     }
     const int64_t units = a.M * a.nseg;
     const unsigned blocks = (unsigned)(units < (1 << 20) ? units : (1 << 20));
-    const size_t lds = LIST ? (a.t.tail ? (size_t)(a.seg_chunks + 3) / 4 * 4 : 0) : a.top ? (size_t)a.seg_chunks * 2 : 0;
+    constexpr int kStep = kLgUnroll * kLgThreads;
+    const size_t lds = a.top ? (size_t)(a.seg_chunks + kStep - 1) / kStep * kLgThreads * sizeof(uint16_t) : 0;
     if constexpr (LIST) {
         logits_stat_kernel<false, false, true><<<blocks, kLgThreads, lds, st>>>(a);
     } else {
@@ -667,7 +712,8 @@ static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_
     }
     if (a.nseg > 1) {
         const unsigned rows = (unsigned)(a.M < (1 << 20) ? a.M : (1 << 20));
-        logits_join_kernel<LIST><<<rows, kLgThreads, (size_t)a.nseg * a.top * sizeof(uint64_t), st>>>(a);
+        const auto kernel = a.entropy ? logits_join_kernel<true, LIST> : logits_join_kernel<false, LIST>;
+        kernel<<<rows, kLgThreads, (size_t)a.nseg * a.top * sizeof(uint64_t), st>>>(a);
     }
     return last_launch_status();
 }
@@ -682,7 +728,7 @@ static f8_status launch_grad(GradArgs& a, float* amax, void* ws, hipStream_t st)
         a.partial = amax ? (uint32_t*)ws : nullptr;
         const int64_t units = a.M * a.nseg;
         nb = (int)(units < kLgGradBlocks ? units : kLgGradBlocks);
-        logits_grad_kernel<ENT, LIST><<<nb, kLgThreads, LIST ? (size_t)(a.seg_chunks + 3) / 4 * 4 : 0, st>>>(a);
+        logits_grad_kernel<ENT, LIST><<<nb, kLgThreads, 0, st>>>(a);
     }
     if (amax) amax_final((const uint32_t*)ws, nb, amax, st);
     return last_launch_status();

@@ -26,6 +26,7 @@ struct ResidualArgs {
     int64_t M, per_gate;  // rows that share a row of the gate
     int dc;               // 16-byte chunks of a row
     float a, b, eps, inv_d;
+    double inv_d64;
     uint16_t *h, *n;
     int64_t ldh, ldn;
     float *rstd_post, *rstd_pre;
@@ -46,6 +47,14 @@ __device__ inline uint4 pack8(const float* f)
 }
 __device__ inline const uint4* row_of(const uint16_t* p, int64_t m, int64_t ld) { return reinterpret_cast<const uint4*>(p + m * ld); }
 __device__ inline uint4* row_of(uint16_t* p, int64_t m, int64_t ld) { return reinterpret_cast<uint4*>(p + m * ld); }
+
+// 1 / sqrt(v) rounded once: the instruction and one Newton step in fp64.  (The norm of the branch; the one after the sum has
+// f8_rmsnorm's arithmetic and bits.)
+__device__ inline float rsqrt_exact(double v)
+{
+    const double r = (double)__builtin_amdgcn_rsqf((float)v);
+    return (float)(r + 0.5 * r * (1.0 - v * r * r));
+}
 
 // Sum over a row of the chunks' terms; thread t of the row's has chunks t, t + TPR, ...  Two buffers in turn and one barrier:
 // a buffer is written again only after the barrier of the sum in between.
@@ -105,7 +114,7 @@ __global__ __launch_bounds__(res_threads(TPR)) void residual_norm_kernel(const R
                 unpack8(y[u], f);
                 term[u] = ((f[0] * f[0] + f[1] * f[1]) + (f[2] * f[2] + f[3] * f[3])) + ((f[4] * f[4] + f[5] * f[5]) + (f[6] * f[6] + f[7] * f[7]));
             }
-            r1 = 1.0f / sqrtf(sum(term) * p.inv_d + p.eps);
+            r1 = rsqrt_exact((double)sum(term) * p.inv_d64 + (double)p.eps);
             if (p.rstd_post && t == 0 && live) p.rstd_post[m] = r1;
         }
         const uint4* gate = p.gate && live ? p.gate + (int64_t)((uint32_t)m / (uint32_t)p.per_gate) * p.dc : nullptr;
@@ -482,7 +491,7 @@ f8_status f8_residual_norm(const void* x_bf16, int64_t ldx, const void* y_bf16, 
     if (M > 0 && D > 0) {
         const ResidualArgs a = {(const uint16_t*)x_bf16, (const uint16_t*)y_bf16, ldx, ldy, (const uint4*)g_post_bf16, (const uint4*)gate_bf16,
                                 (const uint4*)g_pre_bf16, M, gate_rows > 0 ? M / gate_rows : M, (int)(D / 8), skip_scale, branch_scale, eps,
-                                1.0f / (float)D, (uint16_t*)h_bf16, (uint16_t*)n_bf16, ldh, ldn, rstd_post, rstd_pre,
+                                1.0f / (float)D, 1.0 / (double)D, (uint16_t*)h_bf16, (uint16_t*)n_bf16, ldh, ldn, rstd_post, rstd_pre,
                                 amax_n ? (uint32_t*)workspace : nullptr};
         with_row_shape(D / 8, [&](auto TPR, auto U) {
             constexpr int kRows = res_threads(TPR()) / TPR();

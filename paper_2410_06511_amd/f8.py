@@ -492,36 +492,44 @@ def sdpa_bwd_rows(q, k, v, o, do, lse, B, S, Hq, Hkv, hd, dq, dk, dv, delta, wor
 F8_ERR_SHAPE = 2
 
 
-def _arg(name, t, dtype, *shape, packed=True):
-    """The address of an argument after a look at what the library cannot see: type, shape, strides and where it lies."""
+def _refuse(name, t, dtype, shape):
+    raise F8Error(F8_ERR_SHAPE, f"{name}: a GPU tensor of {dtype} and shape {shape} with adjacent elements is wanted; "
+                                f"got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+
+
+# What the library cannot see of an argument: type, shape, strides and where it lies.  (In line and in this order because a
+# call of one token takes no longer than its arguments' checks.)
+
+def _packed(name, t, dtype, shape):
+    """The address of a packed tensor."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not (t.is_contiguous() if packed else t.stride(1) == 1 or shape[1] <= 1):
-        raise F8Error(F8_ERR_SHAPE, f"{name}: a GPU tensor of {dtype} and shape {shape} is wanted, {'packed' if packed else 'rows of adjacent elements'}; "
-                                    f"got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, dtype, shape)
     return t.data_ptr()
 
 
-def _rows(name, t, M, D):
-    """Address and row pitch of a bf16 matrix (any, if it has less than two rows)."""
+def _rows(name, t, shape):
+    """Address and row pitch of a bf16 matrix (any pitch that fits, if it has less than two rows)."""
     if t is None:
         return None, 0
-    return _arg(name, t, torch.bfloat16, M, D, packed=False), t.stride(0) if M > 1 else max(t.stride(0), (D + 7) // 8 * 8)
-
-
-def _gate(gate, D):
-    return (None, 0) if gate is None else (_arg("gate", gate, torch.bfloat16, gate.shape[0], D), gate.shape[0])
+    ld, step = t.stride()
+    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != shape or (step != 1 and shape[1] > 1):
+        _refuse(name, t, torch.bfloat16, shape)
+    return t.data_ptr(), ld if shape[0] > 1 else (max(ld, shape[1]) + 7) // 8 * 8
 
 
 def residual_norm(x, y, h, n=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, eps=1e-5, rstd_post=None, rstd_pre=None,
                   amax_n=None, workspace=None, stream=None):
     """h = skip_scale x + branch_scale gate norm(y) g_post; n = norm(h) g_pre.  gate: [gate_rows, D]."""
-    M, D = x.shape
+    shape = M, D = x.shape
+    bf, f32, gr = torch.bfloat16, torch.float32, 0 if gate is None else gate.shape[0]
+    (xp, ldx), (yp, ldy), (hp, ldh), (np_, ldn) = _rows("x", x, shape), _rows("y", y, shape), _rows("h", h, shape), _rows("n", n, shape)
     wp, wb = _ws(workspace)
-    bf, f32 = torch.bfloat16, torch.float32
-    _check(lib().f8_residual_norm(*_rows("x", x, M, D), *_rows("y", y, M, D), M, D, _arg("g_post", g_post, bf, D), *_gate(gate, D), _arg("g_pre", g_pre, bf, D),
-                                  skip_scale, branch_scale, eps, *_rows("h", h, M, D), *_rows("n", n, M, D), _arg("rstd_post", rstd_post, f32, M),
-                                  _arg("rstd_pre", rstd_pre, f32, M), _arg("amax_n", amax_n, f32, 1), wp, wb, _stream(stream)))
+    _check(lib().f8_residual_norm(xp, ldx, yp, ldy, M, D, _packed("g_post", g_post, bf, (D,)), _packed("gate", gate, bf, (gr, D)), gr,
+                                  _packed("g_pre", g_pre, bf, (D,)), skip_scale, branch_scale, eps, hp, ldh, np_, ldn,
+                                  _packed("rstd_post", rstd_post, f32, (M,)), _packed("rstd_pre", rstd_pre, f32, (M,)),
+                                  _packed("amax_n", amax_n, f32, (1,)), wp, wb, _stream(stream)))
 
 
 def residual_norm_bwd_workspace_bytes(M, D, gate_rows=0):
@@ -531,15 +539,16 @@ def residual_norm_bwd_workspace_bytes(M, D, gate_rows=0):
 def residual_norm_bwd(y, dx, dy, h=None, dh=None, dn=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, rstd_post=None,
                       rstd_pre=None, dg_post=None, dgate=None, dg_pre=None, amax_dy=None, workspace=None, stream=None):
     """y may be None without g_post and gate; dx or dy may be None."""
-    M, D = next(t.shape for t in (dn, dh, h, dx, dy) if t is not None)
+    shape = M, D = (dn if dh is None else dh).shape
+    bf, f32, gr = torch.bfloat16, torch.float32, 0 if gate is None else gate.shape[0]
+    (hp, ldh), (yp, ldy), (dhp, lddh), (dnp, lddn) = _rows("h", h, shape), _rows("y", y, shape), _rows("dh", dh, shape), _rows("dn", dn, shape)
+    (dxp, lddx), (dyp, lddy) = _rows("dx", dx, shape), _rows("dy", dy, shape)
     wp, wb = _ws(workspace)
-    bf, f32 = torch.bfloat16, torch.float32
-    gp, gr = _gate(gate, D)
-    _check(lib().f8_residual_norm_bwd(*_rows("h", h, M, D), *_rows("y", y, M, D), *_rows("dh", dh, M, D), *_rows("dn", dn, M, D), M, D,
-                                      _arg("g_post", g_post, bf, D), gp, gr, _arg("g_pre", g_pre, bf, D), _arg("rstd_post", rstd_post, f32, M),
-                                      _arg("rstd_pre", rstd_pre, f32, M), skip_scale, branch_scale, *_rows("dx", dx, M, D), *_rows("dy", dy, M, D),
-                                      _arg("dg_post", dg_post, f32, D), _arg("dgate", dgate, f32, gr, D), _arg("dg_pre", dg_pre, f32, D),
-                                      _arg("amax_dy", amax_dy, f32, 1), wp, wb, _stream(stream)))
+    _check(lib().f8_residual_norm_bwd(hp, ldh, yp, ldy, dhp, lddh, dnp, lddn, M, D, _packed("g_post", g_post, bf, (D,)), _packed("gate", gate, bf, (gr, D)), gr,
+                                      _packed("g_pre", g_pre, bf, (D,)), _packed("rstd_post", rstd_post, f32, (M,)),
+                                      _packed("rstd_pre", rstd_pre, f32, (M,)), skip_scale, branch_scale, dxp, lddx, dyp, lddy,
+                                      _packed("dg_post", dg_post, f32, (D,)), _packed("dgate", dgate, f32, (gr, D)), _packed("dg_pre", dg_pre, f32, (D,)),
+                                      _packed("amax_dy", amax_dy, f32, (1,)), wp, wb, _stream(stream)))
 
 
 def logits_workspace_bytes(M, vocab, top_k=0):
@@ -554,9 +563,9 @@ def token_logprobs(logits, vocab, stats, targets=None, logp=None, entropy=None, 
     k = 0 if top_ids is None else top_ids.shape[1]
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_token_logprobs(*_rows("logits", logits, M, N), M, vocab, scale, _arg("targets", targets, i64, M), _arg("stats", stats, f32, M, 2),
-                                   _arg("logp", logp, f32, M), _arg("entropy", entropy, f32, M), k, _arg("top_ids", top_ids, i64, M, k),
-                                   _arg("top_logp", top_logp, f32, M, k), wp, wb, _stream(stream)))
+    _check(lib().f8_token_logprobs(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("targets", targets, i64, (M,)), _packed("stats", stats, f32, (M, 2)),
+                                   _packed("logp", logp, f32, (M,)), _packed("entropy", entropy, f32, (M,)), k, _packed("top_ids", top_ids, i64, (M, k)),
+                                   _packed("top_logp", top_logp, f32, (M, k)), wp, wb, _stream(stream)))
 
 
 def token_logprobs_bwd(logits, vocab, stats, dlogits, targets=None, entropy=None, d_logp=None, d_entropy=None, scale=1.0, amax_d=None, workspace=None,
@@ -568,9 +577,9 @@ def token_logprobs_bwd(logits, vocab, stats, dlogits, targets=None, entropy=None
     f32 = torch.float32
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_token_logprobs_bwd(*_rows("logits", logits, M, N), M, vocab, scale, _arg("targets", targets, torch.int64, M),
-                                       _arg("stats", stats, f32, M, 2), _arg("entropy", entropy, f32, M), _arg("d_logp", d_logp, f32, M),
-                                       _arg("d_entropy", d_entropy, f32, M), *_rows("dlogits", dlogits, M, cols), cols, _arg("amax_d", amax_d, f32, 1), wp, wb,
+    _check(lib().f8_token_logprobs_bwd(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("targets", targets, torch.int64, (M,)),
+                                       _packed("stats", stats, f32, (M, 2)), _packed("entropy", entropy, f32, (M,)), _packed("d_logp", d_logp, f32, (M,)),
+                                       _packed("d_entropy", d_entropy, f32, (M,)), *_rows("dlogits", dlogits, (M, cols)), cols, _packed("amax_d", amax_d, f32, (1,)), wp, wb,
                                        _stream(stream)))
 
 
@@ -583,9 +592,9 @@ def distill(logits, vocab, teacher_ids, teacher_logp, stats, loss, targets=None,
     i64, f32 = torch.int64, torch.float32
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_distill(*_rows("logits", logits, M, N), M, vocab, scale, _arg("teacher_ids", teacher_ids, i64, M, K),
-                            _arg("teacher_logp", teacher_logp, f32, M, K), K, int(bool(tail)), teacher_scale, _arg("targets", targets, i64, M),
-                            _arg("stats", stats, f32, M, 4), _arg("loss", loss, f32, M), _arg("logp", logp, f32, M), wp, wb, _stream(stream)))
+    _check(lib().f8_distill(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("teacher_ids", teacher_ids, i64, (M, K)),
+                            _packed("teacher_logp", teacher_logp, f32, (M, K)), K, int(bool(tail)), teacher_scale, _packed("targets", targets, i64, (M,)),
+                            _packed("stats", stats, f32, (M, 4)), _packed("loss", loss, f32, (M,)), _packed("logp", logp, f32, (M,)), wp, wb, _stream(stream)))
 
 
 def distill_bwd(logits, vocab, teacher_ids, teacher_logp, stats, dlogits, d_loss, targets=None, d_logp=None, tail=False, teacher_scale=1.0, scale=1.0,
@@ -597,10 +606,10 @@ def distill_bwd(logits, vocab, teacher_ids, teacher_logp, stats, dlogits, d_loss
     i64, f32 = torch.int64, torch.float32
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_distill_bwd(*_rows("logits", logits, M, N), M, vocab, scale, _arg("teacher_ids", teacher_ids, i64, M, K),
-                                _arg("teacher_logp", teacher_logp, f32, M, K), K, int(bool(tail)), teacher_scale, _arg("targets", targets, i64, M),
-                                _arg("stats", stats, f32, M, 4), _arg("d_loss", d_loss, f32, M), _arg("d_logp", d_logp, f32, M),
-                                *_rows("dlogits", dlogits, M, cols), cols, _arg("amax_d", amax_d, f32, 1), wp, wb, _stream(stream)))
+    _check(lib().f8_distill_bwd(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("teacher_ids", teacher_ids, i64, (M, K)),
+                                _packed("teacher_logp", teacher_logp, f32, (M, K)), K, int(bool(tail)), teacher_scale, _packed("targets", targets, i64, (M,)),
+                                _packed("stats", stats, f32, (M, 4)), _packed("d_loss", d_loss, f32, (M,)), _packed("d_logp", d_logp, f32, (M,)),
+                                *_rows("dlogits", dlogits, (M, cols)), cols, _packed("amax_d", amax_d, f32, (1,)), wp, wb, _stream(stream)))
 
 
 # ---- measuring helpers ---------------------------------------------------------------
