@@ -17,8 +17,9 @@
 
 namespace f8 {
 
-constexpr int kLgThreads = 256;
+constexpr int kLgThreads = 256;         // of a block of the forward
 constexpr int kLgWaves = kLgThreads / kWave;
+constexpr int kLgGradUnroll = 4;
 constexpr int kLgUnroll = 4;            // 16-byte loads in flight a thread: the chunks of one step
 constexpr int kLgSegCols = 131072;      // columns that a block takes at most
 constexpr int kLgMaxSeg = 32;           // blocks that share a row, at most
@@ -85,9 +86,10 @@ __device__ inline void unpack(uint4 v, float* z)
     for (int j = 0; j < 4; ++j) z[2 * j] = bf16_lo(w[j]), z[2 * j + 1] = bf16_hi(w[j]);
 }
 // chunk c of a row; columns from V on read as -inf
+template <bool ONCE>
 __device__ inline uint4 load_logits(const uint4* row, int c, int V)
 {
-    uint4 v = row[c];
+    uint4 v = ONCE ? load_once(row + c) : row[c];
     const int left = V - c * 8;
     if (left < 8) {
         uint32_t* w = &v.x;
@@ -108,12 +110,13 @@ struct List {
     uint32_t marks[kLgSegCols / 8 / 32];
     __device__ bool marked(int lc) const { return marks[lc >> 5] >> (lc & 31) & 1; }
 };
-// Threads below K bring their entry (q: its weight), all threads call; chunks c0 .. c1 - 1.
+// Threads below K bring their entry (q: its weight), all THREADS call; chunks c0 .. c1 - 1.
+template <int THREADS>
 __device__ inline void list_fill(List& L, int K, int64_t id, float q, int c0, int c1)
 {
     const int k = threadIdx.x;
     const bool here = k < K && id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8;
-    for (int i = k; i < (c1 - c0 + 31) / 32; i += kLgThreads) L.marks[i] = 0;
+    for (int i = k; i < (c1 - c0 + 31) / 32; i += THREADS) L.marks[i] = 0;
     if (k < K) L.id[k] = here ? (int)id : -1, L.q[k] = q;
     __syncthreads();
     if (here) atomicOr(&L.marks[((int)id / 8 - c0) >> 5], 1u << (((int)id / 8 - c0) & 31));
@@ -169,28 +172,46 @@ struct StatArgs {
 // a remainder that sums of fp32 probabilities do not tell from zero counts as none
 constexpr double kNoRest = 0x1p-20;
 
-// What a row's outputs are, from its statistics; called by one whole wave.
-// With a teacher whose remainder is a class of its own v.s is the sum outside the list and v.d the list's.
+// What a row's outputs need beside its statistics, read by one whole wave: ahead of the sweep, which hides these loads.
+struct RowInputs {
+    int64_t target;
+    float zt;                          // its logit
+    static constexpr int E = kLgMaxTop / kWave;
+    float zk[E], lq[E];                // of the teacher's entries lane, lane + 64: the student's logit, the teacher's value
+    bool has[E], wrong;
+};
 template <bool LIST>
-__device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v)
+__device__ inline RowInputs row_inputs(const StatArgs& a, int64_t row)
 {
     const int lane = threadIdx.x & (kWave - 1);
     const uint16_t* z = a.logits + row * a.ld;
-    constexpr int E = kLgMaxTop / kWave;
-    float zk[E] = {};
-    const float total = LIST ? v.s + v.d : v.s;
-    bool has[E] = {}, wrong = false;
+    RowInputs in = {};
+    in.target = a.logp ? a.targets[row] : -1;
+    if (in.target >= 0 && in.target < a.V) in.zt = __uint_as_float((uint32_t)z[in.target] << 16);
     if constexpr (LIST) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
+        for (int e = 0; e < RowInputs::E; ++e) {
             const int k = lane + kWave * e;
+            in.lq[e] = -INFINITY;
             if (k >= a.t.K) continue;
             const int64_t id = a.t.ids[row * a.t.K + k];
-            has[e] = id >= 0 && id < a.V;
-            wrong |= id >= a.V;
-            if (has[e]) zk[e] = (__uint_as_float((uint32_t)z[id] << 16) - v.m) * a.scale;
+            const float t = a.t.logp[row * a.t.K + k];
+            in.has[e] = id >= 0 && id < a.V;
+            in.wrong |= id >= a.V;
+            if (in.has[e]) in.zk[e] = __uint_as_float((uint32_t)z[id] << 16), in.lq[e] = t * a.t.scale;
         }
     }
+    return in;
+}
+
+// What a row's outputs are, from its statistics; called by the same whole wave.
+// With a teacher whose remainder is a class of its own v.s is the sum outside the list and v.d the list's.
+template <bool LIST>
+__device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInputs& in, Stat v)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    constexpr int E = RowInputs::E;
+    const float total = LIST ? v.s + v.d : v.s;
     const bool none = total == 0.0f;  // every logit is -inf
     const float m = none ? -INFINITY : v.m, log_total = none ? -INFINITY : logf(total);
     if (lane == 0) {
@@ -198,18 +219,15 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v)
         s[0] = m, s[1] = log_total;
         if (a.entropy) a.entropy[row] = none ? 0.0f : log_total - v.d * kLn2 / total;
         if (a.logp) {
-            const int64_t t = a.targets[row];
-            a.logp[row] = t < 0 ? 0.0f : t >= a.V ? NAN : none ? -INFINITY : (__uint_as_float((uint32_t)z[t] << 16) - m) * a.scale - log_total;
+            a.logp[row] = in.target < 0 ? 0.0f : in.target >= a.V ? NAN : none ? -INFINITY : (in.zt - m) * a.scale - log_total;
         }
     }
     if constexpr (LIST) {
         // the teacher's probabilities: given, or the softmax over its entries
-        float lq[E], top = -INFINITY;
+        const float(&lq)[E] = in.lq;
+        float top = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            lq[e] = has[e] ? a.t.logp[row * a.t.K + lane + kWave * e] * a.t.scale : -INFINITY;
-            top = lq[e] > top || lq[e] != lq[e] ? lq[e] : top;
-        }
+        for (int e = 0; e < E; ++e) top = lq[e] > top || lq[e] != lq[e] ? lq[e] : top;
         double sum = 0.0;
         float norm = 0.0f;
         if (!a.t.tail) {
@@ -229,7 +247,7 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v)
         for (int e = 0; e < E; ++e) {
             const float l = lq[e] - norm, q = lq[e] == -INFINITY ? 0.0f : expf(l);
             mass += q;
-            if (q != 0.0f) loss += (double)q * (l - (none ? -INFINITY : zk[e] - log_total));
+            if (q != 0.0f) loss += (double)q * (l - (none ? -INFINITY : (in.zk[e] - m) * a.scale - log_total));
         }
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) loss += __shfl_xor(loss, off, kWave), mass += __shfl_xor(mass, off, kWave);
@@ -242,7 +260,7 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, Stat v)
             if (mass != mass) coef = NAN;
         }
         if (none) coef = 0.0f;
-        if (__any(wrong)) loss = coef = NAN;
+        if (__any(in.wrong)) loss = coef = NAN;
         if (lane == 0) {
             a.loss[row] = (float)loss;
             a.stats[row * 4 + 2] = coef, a.stats[row * 4 + 3] = norm;
@@ -386,7 +404,7 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
 }
 
 // One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.
-template <bool ENT, bool TOP, bool LIST>
+template <bool ENT, bool TOP, bool LIST, bool ONCE>
 __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs a)
 {
     extern __shared__ uint16_t smax[];
@@ -402,16 +420,27 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
         Stat v = {-FLT_MAX, 0.0f, 0.0f};
         uint32_t best = 0;
+        RowInputs in;
+        if (a.nseg == 1 && wave == kLgWaves - 1) in = row_inputs<LIST>(a, rowi);
+        uint4 w[kLgUnroll];
+        auto request = [&](int c) {
+#pragma unroll
+            for (int u = 0; u < kLgUnroll; ++u)
+                w[u] = c + u * kLgThreads < c1 ? load_logits<ONCE>(row, c + u * kLgThreads, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+        };
         const bool marks = LIST && a.t.tail;
         if constexpr (LIST) {
             if (marks) {
-                list_fill(list, a.t.K, tid < a.t.K ? a.t.ids[rowi * a.t.K + tid] : -1, 0.0f, c0, c1);
+                const int64_t id = tid < a.t.K ? a.t.ids[rowi * a.t.K + tid] : -1;
+                uint4 own = make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+                if (id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8) own = load_logits<false>(row, (int)(id >> 3), a.V);
+                request(c0 + tid);
+                list_fill<kLgThreads>(list, a.t.K, id, 0.0f, c0, c1);
                 uint32_t mask;
                 float none[8];
-                const int c = list_chunk(list, a.t.K, &mask, none);
-                if (c >= 0) {
+                if (list_chunk(list, a.t.K, &mask, none) >= 0) {
                     float z[8];
-                    unpack(load_logits(row, c, a.V), z);
+                    unpack(own, z);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v.m = fmaxf(v.m, z[j]);
 #pragma unroll
@@ -423,18 +452,16 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
             }
         }
         for (int c = c0 + tid, step = 0; c < c1; c += kLgUnroll * kLgThreads, ++step) {
-            uint4 w[kLgUnroll];
-#pragma unroll
-            for (int u = 0; u < kLgUnroll; ++u) {
-                const int cu = c + u * kLgThreads;
-                bool in = cu < c1;
-                if constexpr (LIST) in = in && !(marks && list.marked(cu - c0));
-                w[u] = in ? load_logits(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
-            }
+            if (!marks || step > 0) request(c);
             float z[kLgUnroll][8], m = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kLgUnroll; ++u) {
                 unpack(w[u], z[u]);
+                if constexpr (LIST)
+                    if (marks && c + u * kLgThreads < c1 && list.marked(c + u * kLgThreads - c0)) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) z[u][j] = -INFINITY;
+                    }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) m = fmaxf(m, z[u][j]);
             }
@@ -461,8 +488,6 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         for (int i = 1; i < kLgWaves; ++i) v = join<ENT>(v, wave_stat[i], c2);
         if (a.nseg > 1) {
             if (tid == 0) a.part[unit] = make_float4(v.m, v.s, v.d, 0.0f);
-        } else if (wave == 0) {
-            finish_row<LIST>(a, rowi, v);
         }
         if constexpr (TOP) {
             const float log_total = logf(v.s);
@@ -475,6 +500,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
                 }
             });
         }
+        if (a.nseg == 1 && wave == kLgWaves - 1) finish_row<LIST>(a, rowi, in, v);  // (while the first waves rank)
         __syncthreads();  // LDS is used again
     }
 }
@@ -488,18 +514,23 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const float c2 = a.scale * kLog2e;
     for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+        const int keys = a.nseg * a.top;
+        const uint64_t* lists = a.part_top + row * keys;
+        constexpr int AHEAD = 4;  // keys that a thread has on their way beside the statistics
+        RowInputs in;
+        if (tid / kWave == kLgWaves - 1) in = row_inputs<LIST>(a, row);
+        uint64_t mine[AHEAD], least = ~(uint64_t)0;
         Stat v = {-FLT_MAX, 0.0f, 0.0f};
         if (lane < a.nseg) {
             const float4 p = a.part[row * a.nseg + lane];
             v = {p.x, p.y, p.z};
+            // a key that K of the pieces' elements reach: the least of the pieces' (K / nseg)-th
+            if (keys) least = lists[lane * a.top + (a.top + a.nseg - 1) / a.nseg - 1];
         }
-        // a key that K of the pieces' elements reach: the least of the pieces' (K / nseg)-th
-        uint64_t least = ~(uint64_t)0;
-        const uint64_t* lists = a.part_top + row * a.nseg * a.top;
-        if (a.top && lane < a.nseg) least = lists[lane * a.top + (a.top + a.nseg - 1) / a.nseg - 1];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) mine[u] = tid + u * kLgThreads < keys ? lists[tid + u * kLgThreads] : 0;
         v = wave_join<ENT>(v, c2);
-        if (tid < kWave) finish_row<LIST>(a, row, v);
-        if (a.top) {
+        if (keys) {
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) {
                 const uint64_t o = __shfl_xor(least, off, kWave);
@@ -507,7 +538,10 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
             }
             if (tid == 0) n = 0;
             __syncthreads();
-            for (int i = tid; i < a.nseg * a.top; i += kLgThreads) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (mine[u] >= least) cand[atomicAdd(&n, 1u)] = mine[u];
+            for (int i = tid + AHEAD * kLgThreads; i < keys; i += kLgThreads) {
                 const uint64_t key = lists[i];
                 if (key >= least) cand[atomicAdd(&n, 1u)] = key;
             }
@@ -525,6 +559,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
                 }
             }
         }
+        if (tid / kWave == kLgWaves - 1) finish_row<LIST>(a, row, in, v);  // (while the first waves rank)
         __syncthreads();
     }
 }
@@ -544,17 +579,16 @@ struct GradArgs {
     uint32_t* partial;
 };
 
-// Rows from the last one on: where they do not all fit the caches, the forward's last rows are still there.
-template <bool ENT, bool LIST>
-__global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs a)
+template <int THREADS, bool ENT, bool LIST, bool ONCE>
+__global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
 {
-    __shared__ uint32_t red[kLgWaves];
+    __shared__ uint32_t red[THREADS / kWave];
     __shared__ std::conditional_t<LIST, List, int> list;
     const int tid = threadIdx.x;
     const int chunks = a.cols / 8, read = (a.V + 7) / 8;
     const float c2 = a.scale * kLog2e;
     uint32_t mag = 0;
-    for (int64_t unit = a.M * a.nseg - 1 - (int64_t)blockIdx.x; unit >= 0; unit -= gridDim.x) {
+    for (int64_t unit = blockIdx.x; unit < a.M * a.nseg; unit += gridDim.x) {
         const int64_t rowi = unit / a.nseg;
         const int seg = (int)(unit - rowi * a.nseg), c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
         const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
@@ -600,32 +634,38 @@ __global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs 
             mag = absmax_acc(mag, o);
             store_stream(out + cu, o);
         };
+        uint4 w[kLgGradUnroll];
+        auto request = [&](int c) {
+#pragma unroll
+            for (int u = 0; u < kLgGradUnroll; ++u) {
+                const int cu = c + u * THREADS;
+                w[u] = cu < c1 && cu < read && !zero ? load_logits<ONCE>(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+            }
+        };
         if constexpr (LIST) {
             if (!zero) {  // (alike for the whole block)
                 int64_t id = -1;
-                float q = 0.0f;
+                float t = 0.0f;
+                uint4 own = make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
                 if (tid < a.t.K) {
                     id = a.t.ids[rowi * a.t.K + tid];
                     if (id >= a.V) id = -1;
-                    if (id >= 0 && g != 0.0f) q = g * expf(a.t.logp[rowi * a.t.K + tid] * a.t.scale - st[3]);
+                    t = a.t.logp[rowi * a.t.K + tid];
+                    if (id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8) own = load_logits<false>(row, (int)(id >> 3), a.V);
                 }
-                list_fill(list, a.t.K, id, q, c0, c1);
+                request(c0 + tid);
+                list_fill<THREADS>(list, a.t.K, id, id >= 0 && g != 0.0f ? g * expf(t * a.t.scale - st[3]) : 0.0f, c0, c1);
                 uint32_t mask;
-                float w[8];
-                const int c = list_chunk(list, a.t.K, &mask, w);
-                if (c >= 0) emit(c, load_logits(row, c, a.V), mask, w);
+                float q[8];
+                const int c = list_chunk(list, a.t.K, &mask, q);
+                if (c >= 0) emit(c, own, mask, q);
             }
         }
-        for (int c = c0 + tid; c < c1; c += kLgUnroll * kLgThreads) {
-            uint4 w[kLgUnroll];
+        for (int c = c0 + tid; c < c1; c += kLgGradUnroll * THREADS) {
+            if (!LIST || zero || c != c0 + tid) request(c);
 #pragma unroll
-            for (int u = 0; u < kLgUnroll; ++u) {
-                const int cu = c + u * kLgThreads;
-                w[u] = cu < c1 && cu < read && !zero ? load_logits(row, cu, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
-            }
-#pragma unroll
-            for (int u = 0; u < kLgUnroll; ++u) {
-                const int cu = c + u * kLgThreads;
+            for (int u = 0; u < kLgGradUnroll; ++u) {
+                const int cu = c + u * THREADS;
                 if (cu >= c1) break;
                 if (zero || cu >= read) {
                     store_stream(out + cu, make_uint4(0, 0, 0, 0));
@@ -639,7 +679,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs 
         if constexpr (LIST) __syncthreads();  // LDS is used again
     }
     if (a.partial) {
-        const uint32_t mx = block_max_u32<kLgWaves>(pk_collapse(mag), red);
+        const uint32_t mx = block_max_u32<THREADS / kWave>(pk_collapse(mag), red);
         if (tid == 0) a.partial[blockIdx.x] = mx;
     }
 }
@@ -651,11 +691,11 @@ __global__ __launch_bounds__(kLgThreads) void logits_grad_kernel(const GradArgs 
 struct Split {
     int nseg, seg_chunks;
 };
-static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted)
+static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted, int threads)
 {
     const int64_t chunks = (cols + 7) / 8;
     int64_t n = M > 0 ? blocks_wanted / M : 1;
-    if (n > chunks / kLgThreads) n = chunks / kLgThreads;
+    if (n > chunks / threads) n = chunks / threads;
     if (n > kLgMaxSeg) n = kLgMaxSeg;
     const int64_t least = (cols + kLgSegCols - 1) / kLgSegCols;
     if (n < least) n = least;
@@ -663,11 +703,12 @@ static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted)
     const int64_t per = (chunks + n - 1) / n;
     return {(int)((chunks + per - 1) / per), (int)per};
 }
-constexpr int64_t kLgBlocksWanted = 1024;
+constexpr int64_t kLgBlocksWanted = 512;
+constexpr int64_t kLgOnce = (int64_t)1 << 29, kLgGradOnce = (int64_t)1 << 27;
 
 static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
 {
-    const Split s = split_rows(M, V, kLgBlocksWanted);
+    const Split s = split_rows(M, V, kLgBlocksWanted, kLgThreads);
     return s.nseg > 1 ? (size_t)M * s.nseg * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
 }
 
@@ -691,7 +732,7 @@ template <bool LIST>
 static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_t st)
 {
     if (a.M == 0) return F8_OK;
-    const Split s = split_rows(a.M, a.V, kLgBlocksWanted);
+    const Split s = split_rows(a.M, a.V, kLgBlocksWanted, kLgThreads);
     a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
     if (a.nseg > 1) {
         if (!ws || ws_bytes < logits_part_bytes(a.M, a.V, a.top)) return F8_ERR_WORKSPACE;
@@ -701,13 +742,16 @@ static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_
     }
     const int64_t units = a.M * a.nseg;
     const unsigned blocks = (unsigned)(units < (1 << 20) ? units : (1 << 20));
+    const bool once = a.M * a.V >= kLgOnce;
     constexpr int kStep = kLgUnroll * kLgThreads;
     const size_t lds = a.top ? (size_t)(a.seg_chunks + kStep - 1) / kStep * kLgThreads * sizeof(uint16_t) : 0;
     if constexpr (LIST) {
-        logits_stat_kernel<false, false, true><<<blocks, kLgThreads, lds, st>>>(a);
+        const auto kernel = once ? logits_stat_kernel<false, false, true, true> : logits_stat_kernel<false, false, true, false>;
+        kernel<<<blocks, kLgThreads, lds, st>>>(a);
     } else {
-        const auto kernel = a.entropy ? (a.top ? logits_stat_kernel<true, true, false> : logits_stat_kernel<true, false, false>)
-                                      : (a.top ? logits_stat_kernel<false, true, false> : logits_stat_kernel<false, false, false>);
+        const auto kernel = a.top ? (a.entropy ? logits_stat_kernel<true, true, false, false> : logits_stat_kernel<false, true, false, false>)
+                            : once ? (a.entropy ? logits_stat_kernel<true, false, false, true> : logits_stat_kernel<false, false, false, true>)
+                                   : (a.entropy ? logits_stat_kernel<true, false, false, false> : logits_stat_kernel<false, false, false, false>);
         kernel<<<blocks, kLgThreads, lds, st>>>(a);
     }
     if (a.nseg > 1) {
@@ -723,12 +767,17 @@ static f8_status launch_grad(GradArgs& a, float* amax, void* ws, hipStream_t st)
 {
     int nb = 0;
     if (a.M > 0) {
-        const Split s = split_rows(a.M, a.cols, kLgGradBlocks);
+        Split s = split_rows(a.M, a.cols, kLgGradBlocks / 2, 1024);
+        const bool wide = s.seg_chunks >= kLgGradUnroll * 1024 && a.M * s.nseg >= kLgGradBlocks;
+        if (!wide) s = split_rows(a.M, a.cols, LIST ? kLgGradBlocks / 2 : kLgGradBlocks, 512);
         a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
         a.partial = amax ? (uint32_t*)ws : nullptr;
         const int64_t units = a.M * a.nseg;
         nb = (int)(units < kLgGradBlocks ? units : kLgGradBlocks);
-        logits_grad_kernel<ENT, LIST><<<nb, kLgThreads, 0, st>>>(a);
+        const bool once = a.M * a.V >= kLgGradOnce;
+        const auto kernel = wide ? (once ? logits_grad_kernel<1024, ENT, LIST, true> : logits_grad_kernel<1024, ENT, LIST, false>)
+                                 : (once ? logits_grad_kernel<512, ENT, LIST, true> : logits_grad_kernel<512, ENT, LIST, false>);
+        kernel<<<nb, wide ? 1024 : 512, 0, st>>>(a);
     }
     if (amax) amax_final((const uint32_t*)ws, nb, amax, st);
     return last_launch_status();
