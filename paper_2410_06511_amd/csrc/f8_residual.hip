@@ -16,7 +16,8 @@ namespace f8 {
 
 constexpr int64_t kResMaxD = 16384;
 constexpr int kResBlocks = 2048;     // of the forward: one partial maximum each
-constexpr int kResBwdBlocks = 512;   // of the backward: a partial row of each gain's sums each
+constexpr int kResBwdBlocks = 512;   // of the backward: a partial row of each gain's sums each; half as many of more than 512 threads
+constexpr int64_t kResOnce = (int64_t)1 << 25;
 static_assert((size_t)kResBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial per block fits the minimum workspace");
 
 struct ResidualArgs {
@@ -33,7 +34,9 @@ struct ResidualArgs {
     uint32_t* partial;
 };
 
-constexpr int res_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
+// Kernels for THREADS == 64: a row per wave, four waves a block; above: a row per block of at most THREADS threads.
+constexpr int kResWaveRows = 4;
+constexpr int res_threads(int THREADS) { return THREADS == kWave ? kWave * kResWaveRows : THREADS; }
 
 __device__ inline void unpack8(uint4 v, float* f)
 {
@@ -48,6 +51,16 @@ __device__ inline uint4 pack8(const float* f)
 __device__ inline const uint4* row_of(const uint16_t* p, int64_t m, int64_t ld) { return reinterpret_cast<const uint4*>(p + m * ld); }
 __device__ inline uint4* row_of(uint16_t* p, int64_t m, int64_t ld) { return reinterpret_cast<uint4*>(p + m * ld); }
 
+// Maximum over a block of any number of waves, for its first wave.
+__device__ inline uint32_t waves_max(uint32_t v, uint32_t* red)
+{
+    v = wave_max_u32(v);
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
+    __syncthreads();
+    return threadIdx.x < kWave ? wave_max_u32(threadIdx.x < blockDim.x / kWave ? red[threadIdx.x] : 0) : 0;
+}
+
 // 1 / sqrt(v) rounded once: the instruction and one Newton step in fp64.  (The norm of the branch; the one after the sum has
 // f8_rmsnorm's arithmetic and bits.)
 __device__ inline float rsqrt_exact(double v)
@@ -56,46 +69,61 @@ __device__ inline float rsqrt_exact(double v)
     return (float)(r + 0.5 * r * (1.0 - v * r * r));
 }
 
-// Sum over a row of the chunks' terms; thread t of the row's has chunks t, t + TPR, ...  Two buffers in turn and one barrier:
+// Sum over a wave in the order of exchanges by halves (lanes 32 apart, then 16, ... 1): once lanes 8 apart agree, a rotation by 4
+// within 16 lanes is the exchange with the lane 4 apart, and so on.  Swaps and rotations are a fraction of the latency of
+// exchanges through LDS, which a row waits for twice.
+template <int ROTATE>
+__device__ inline float plus_rotated(float v)
+{
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x120 + ROTATE, 0xF, 0xF, true));
+}
+__device__ inline float wave_sum(float v)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    return plus_rotated<1>(plus_rotated<2>(plus_rotated<4>(plus_rotated<8>(v))));
+}
+
+// Sum over a row of the chunks' terms; thread t of the row's TPR has chunks t, t + TPR, ...  Two buffers in turn and one barrier:
 // a buffer is written again only after the barrier of the sum in between.
-template <int TPR, int U>
+template <int THREADS, int U>
 struct RowSum {
-    static constexpr int kRows = res_threads(TPR) / TPR, kPieces = TPR > kWave ? TPR / kWave * U : 1;
-    float (*terms)[kRows][kPieces][kWave];
+    static constexpr int kPieces = THREADS > kWave ? THREADS / kWave * U : 1;
+    float (*terms)[kPieces][kWave];
     int buf = 0;
     __device__ float operator()(const float* term)
     {
         const int lane = threadIdx.x & (kWave - 1);
         float s = 0.0f;
-        if constexpr (TPR == kWave) {
+        if constexpr (THREADS == kWave) {
 #pragma unroll
             for (int u = 0; u < U; ++u) s += term[u];
         } else {
-            const int wave = threadIdx.x % TPR / kWave, row = threadIdx.x / TPR;
+            const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
 #pragma unroll
-            for (int u = 0; u < U; ++u) terms[buf][row][wave + TPR / kWave * u][lane] = term[u];
+            for (int u = 0; u < U; ++u) terms[buf][wave + waves * u][lane] = term[u];
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) s += terms[buf][row][i][lane];
+#pragma unroll 8
+            for (int i = 0; i < waves * U; ++i) s += terms[buf][i][lane];
             buf ^= 1;
         }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, kWave);
-        return s;
+        return wave_sum(s);
     }
 };
 
-template <int TPR, int U, bool POST, bool PRE>
-__global__ __launch_bounds__(res_threads(TPR)) void residual_norm_kernel(const ResidualArgs p)
+template <int THREADS, int U, bool POST, bool PRE>
+__global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_kernel(const ResidualArgs p)
 {
-    constexpr int kRows = res_threads(TPR) / TPR, kWaves = res_threads(TPR) / kWave;
-    __shared__ float terms[2][RowSum<TPR, U>::kRows][RowSum<TPR, U>::kPieces][kWave];
-    __shared__ uint32_t red[kWaves];
-    RowSum<TPR, U> sum{terms};
-    const int t = threadIdx.x % TPR;
+    constexpr int kRows = THREADS == kWave ? kResWaveRows : 1;
+    __shared__ float terms[2][RowSum<THREADS, U>::kPieces][kWave];
+    __shared__ uint32_t red[res_threads(THREADS) / kWave];
+    RowSum<THREADS, U> sum{terms};
+    const int TPR = THREADS == kWave ? kWave : (int)blockDim.x, t = THREADS == kWave ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     uint32_t mag = 0;
     for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < p.M; m0 += (int64_t)gridDim.x * kRows) {
-        const int64_t m = m0 + threadIdx.x / TPR;
+        const int64_t m = m0 + (THREADS == kWave ? (int)threadIdx.x / kWave : 0);
         const bool live = m < p.M;
         uint4 x[U], y[U];
         bool in[U];
@@ -164,7 +192,7 @@ __global__ __launch_bounds__(res_threads(TPR)) void residual_norm_kernel(const R
         }
     }
     if (PRE && p.partial) {
-        const uint32_t mx = block_max_u32<kWaves>(pk_collapse(mag), red);
+        const uint32_t mx = waves_max(pk_collapse(mag), red);
         if (threadIdx.x == 0) p.partial[blockIdx.x] = mx;
     }
 }
@@ -178,6 +206,7 @@ struct ResidualGradArgs {
     const float *rstd_post, *rstd_pre;
     int64_t M, per_gate, units;
     int parts, dc;
+    bool once;  // loads past the caches
     float a, b, inv_d;
     uint16_t *dx, *dy;  // nullable
     int64_t lddx, lddy;
@@ -186,17 +215,17 @@ struct ResidualGradArgs {
 };
 
 // A block takes units: the rows part, part + parts, ... of one group of rows that share a gate's row, and leaves one row of
-// sums a gain.  The next row is on its way while this one is worked on (TPR < 1024, whose threads have the registers).
-template <int TPR, int U, bool POST, bool GATE, bool PRE>
-__global__ __launch_bounds__(res_threads(TPR), TPR > 256 ? 1 : 2) void residual_norm_bwd_kernel(const ResidualGradArgs p)
+// sums a gain.
+template <int THREADS, int U, bool POST, bool GATE, bool PRE>
+__global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_bwd_kernel(const ResidualGradArgs p)
 {
-    constexpr int kRows = res_threads(TPR) / TPR, kWaves = res_threads(TPR) / kWave;
-    constexpr bool AHEAD = TPR < 1024;
-    __shared__ float terms[2][RowSum<TPR, U>::kRows][RowSum<TPR, U>::kPieces][kWave];
-    __shared__ float share[kRows > 1 ? kRows : 1][kRows > 1 ? TPR * U * 8 : 1];
-    __shared__ uint32_t red[kWaves];
-    RowSum<TPR, U> sum{terms};
-    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    constexpr int kRows = THREADS == kWave ? kResWaveRows : 1;
+    __shared__ float terms[2][RowSum<THREADS, U>::kPieces][kWave];
+    __shared__ float share[kRows][kRows > 1 ? kWave * U * 8 : 1];
+    __shared__ uint32_t red[res_threads(THREADS) / kWave];
+    RowSum<THREADS, U> sum{terms};
+    const int TPR = THREADS == kWave ? kWave : (int)blockDim.x;
+    const int t = THREADS == kWave ? (int)threadIdx.x % kWave : (int)threadIdx.x, sub = THREADS == kWave ? (int)threadIdx.x / kWave : 0;
     uint32_t mag = 0;
     float acc_pre[U][8] = {}, acc_post[U][8] = {};
     struct Row {
@@ -210,15 +239,15 @@ __global__ __launch_bounds__(res_threads(TPR), TPR > 256 ? 1 : 2) void residual_
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) share[sub][(u * 8 + j) * TPR + t] = acc[u][j];
+                for (int j = 0; j < 8; ++j) share[sub][(u * 8 + j) * kWave + t] = acc[u][j];
             __syncthreads();
             if (sub) return;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    float s = share[0][(u * 8 + j) * TPR + t];
-                    for (int k = 1; k < kRows; ++k) s += share[k][(u * 8 + j) * TPR + t];
+                    float s = share[0][(u * 8 + j) * kWave + t];
+                    for (int k = 1; k < kRows; ++k) s += share[k][(u * 8 + j) * kWave + t];
                     acc[u][j] = s;
                 }
         }
@@ -236,32 +265,27 @@ __global__ __launch_bounds__(res_threads(TPR), TPR > 256 ? 1 : 2) void residual_
         const int64_t first = group * p.per_gate, rows = (p.per_gate - part + p.parts - 1) / p.parts;  // of this unit
         const uint4* gate = GATE ? p.gate + group * p.dc : nullptr;
         float acc_gate[U][8] = {};
-        auto request = [&](int64_t k) {
-            Row r;
+        for (int64_t k0 = 0; k0 < rows; k0 += kRows) {
+            const int64_t k = k0 + sub, m = first + part + k * p.parts;
             const bool live = k < rows;
-            const int64_t m = first + part + k * p.parts;
+            Row row;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int c = t + TPR * u;
-                const bool in = live && c < p.dc;
-                r.h[u] = r.y[u] = r.dh[u] = r.dn[u] = make_uint4(0, 0, 0, 0);
-                if (in) {
-                    if (PRE) r.h[u] = row_of(p.h, m, p.ldh)[c], r.dn[u] = row_of(p.dn, m, p.lddn)[c];
-                    if (POST || GATE) r.y[u] = row_of(p.y, m, p.ldy)[c];
-                    if (!PRE || p.dh) r.dh[u] = row_of(p.dh, m, p.lddh)[c];
+                row.h[u] = row.y[u] = row.dh[u] = row.dn[u] = make_uint4(0, 0, 0, 0);
+                if (!live || c >= p.dc) continue;
+                if (p.once) {
+                    if (PRE) row.h[u] = load_once(row_of(p.h, m, p.ldh) + c), row.dn[u] = load_once(row_of(p.dn, m, p.lddn) + c);
+                    if (POST || GATE) row.y[u] = load_once(row_of(p.y, m, p.ldy) + c);
+                    if (!PRE || p.dh) row.dh[u] = load_once(row_of(p.dh, m, p.lddh) + c);
+                } else {
+                    if (PRE) row.h[u] = row_of(p.h, m, p.ldh)[c], row.dn[u] = row_of(p.dn, m, p.lddn)[c];
+                    if (POST || GATE) row.y[u] = row_of(p.y, m, p.ldy)[c];
+                    if (!PRE || p.dh) row.dh[u] = row_of(p.dh, m, p.lddh)[c];
                 }
             }
-            r.r1 = POST && live ? p.rstd_post[m] : 0.0f;
-            r.r2 = PRE && live ? p.rstd_pre[m] : 0.0f;
-            return r;
-        };
-        Row row, next;
-        if constexpr (AHEAD) row = request(sub);
-        for (int64_t k0 = 0; k0 < rows; k0 += kRows) {
-            if constexpr (AHEAD) next = request(k0 + kRows + sub);
-            else row = request(k0 + sub);
-            const int64_t k = k0 + sub, m = first + part + k * p.parts;
-            const bool live = k < rows;
+            row.r1 = POST && live ? p.rstd_post[m] : 0.0f;
+            row.r2 = PRE && live ? p.rstd_pre[m] : 0.0f;
             float term[U], dt[U][8];
             if constexpr (PRE) {
 #pragma unroll
@@ -349,15 +373,13 @@ __global__ __launch_bounds__(res_threads(TPR), TPR > 256 ? 1 : 2) void residual_
                     }
                 }
             }
-            if constexpr (AHEAD) row = next;
         }
         if (GATE && p.part_gate) leave(acc_gate, p.part_gate + unit * p.dc * 8);
     }
     if (PRE && p.part_pre) leave(acc_pre, p.part_pre + (int64_t)blockIdx.x * p.dc * 8);
     if (POST && p.part_post) leave(acc_post, p.part_post + (int64_t)blockIdx.x * p.dc * 8);
     if (p.partial) {
-        __syncthreads();
-        const uint32_t mx = block_max_u32<kWaves>(pk_collapse(mag), red);
+        const uint32_t mx = waves_max(pk_collapse(mag), red);
         if (threadIdx.x == 0) p.partial[blockIdx.x] = mx;
     }
 }
@@ -417,19 +439,23 @@ __global__ __launch_bounds__(kResFinalCols* kResFinalGroups) void residual_final
 
 // ---- host ----------------------------------------------------------------------------------------
 
-// f(threads a row, chunks a thread): the fewest threads that hold a row of dc chunks with at most two chunks each; up to 1024
-// elements a row is a wave's own
+// f(upper bound of a block's threads, chunks a thread, threads): a row of dc chunks by as few waves as hold it with U chunks each
 template <class F>
-static void with_row_shape(int64_t dc, F&& f)
+static void with_row_shape(int64_t dc, int u, F&& f)
 {
     using std::integral_constant;
-    if (dc <= 64) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (dc <= 128) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    else if (dc <= 256) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-    else if (dc <= 512) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    else if (dc <= 1024) f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-    else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    const int threads = (int)((dc + u * kWave - 1) / (u * kWave)) * kWave;
+    const auto bounded = [&](auto U) {
+        if (threads <= 64) f(integral_constant<int, 64>{}, U, res_threads(64));
+        else if (threads <= 256) f(integral_constant<int, 256>{}, U, threads);
+        else if (threads <= 512) f(integral_constant<int, 512>{}, U, threads);
+        else f(integral_constant<int, 1024>{}, U, threads);
+    };
+    if (u == 1) bounded(integral_constant<int, 1>{});
+    else bounded(integral_constant<int, 2>{});
 }
+static int fwd_chunks(int64_t dc) { return dc <= 64 ? 1 : 2; }
+static int bwd_chunks(int64_t dc) { return dc <= 64 || (dc > 128 && dc <= 1024) ? 1 : 2; }
 
 // How the backward divides its rows: `parts` blocks share a group of rows with one gate row while there are fewer groups than
 // blocks, else a block takes whole groups.
@@ -439,12 +465,13 @@ struct ResidualPlan {
 };
 static ResidualPlan plan_bwd(int64_t M, int64_t D, int64_t gate_rows)
 {
-    const int64_t groups = gate_rows > 0 ? gate_rows : 1, per_gate = M / groups, slots = D <= 1024 ? 4 : 1;  // rows that a block takes at once
-    int64_t parts = kResBwdBlocks / groups, most = (per_gate + slots - 1) / slots;
+    const int64_t groups = gate_rows > 0 ? gate_rows : 1, per_gate = M / groups, slots = D / 8 <= 64 * bwd_chunks(D / 8) ? kResWaveRows : 1;  // rows that a block takes at once
+    const int blocks = D / 8 > 512 ? kResBwdBlocks / 2 : kResBwdBlocks;
+    int64_t parts = blocks / groups, most = (per_gate + slots - 1) / slots;
     if (parts > most) parts = most;
     if (parts < 1) parts = 1;
     const int64_t units = M > 0 ? groups * parts : 0;
-    return {per_gate, units, (int)parts, (int)(units < kResBwdBlocks ? units : kResBwdBlocks)};
+    return {per_gate, units, (int)parts, (int)(units < blocks ? units : blocks)};
 }
 
 static bool bad_pitch(int64_t ld, int64_t D) { return ld < D || (ld % 8); }
@@ -493,13 +520,13 @@ f8_status f8_residual_norm(const void* x_bf16, int64_t ldx, const void* y_bf16, 
                                 (const uint4*)g_pre_bf16, M, gate_rows > 0 ? M / gate_rows : M, (int)(D / 8), skip_scale, branch_scale, eps,
                                 1.0f / (float)D, 1.0 / (double)D, (uint16_t*)h_bf16, (uint16_t*)n_bf16, ldh, ldn, rstd_post, rstd_pre,
                                 amax_n ? (uint32_t*)workspace : nullptr};
-        with_row_shape(D / 8, [&](auto TPR, auto U) {
-            constexpr int kRows = res_threads(TPR()) / TPR();
+        with_row_shape(D / 8, fwd_chunks(D / 8), [&](auto T, auto U, int threads) {
+            constexpr int kRows = T() == kWave ? kResWaveRows : 1;
             const int64_t b = (M + kRows - 1) / kRows;
             nb = (int)(b < kResBlocks ? b : kResBlocks);
-            const auto kernel = g_post_bf16 ? (g_pre_bf16 ? residual_norm_kernel<TPR(), U(), true, true> : residual_norm_kernel<TPR(), U(), true, false>)
-                                            : (g_pre_bf16 ? residual_norm_kernel<TPR(), U(), false, true> : residual_norm_kernel<TPR(), U(), false, false>);
-            kernel<<<nb, res_threads(TPR()), 0, st>>>(a);
+            const auto kernel = g_post_bf16 ? (g_pre_bf16 ? residual_norm_kernel<T(), U(), true, true> : residual_norm_kernel<T(), U(), true, false>)
+                                            : (g_pre_bf16 ? residual_norm_kernel<T(), U(), false, true> : residual_norm_kernel<T(), U(), false, false>);
+            kernel<<<nb, threads, 0, st>>>(a);
         });
     }
     if (amax_n) amax_final((const uint32_t*)workspace, nb, amax_n, st);
@@ -534,15 +561,15 @@ f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf
     if (M > 0 && D > 0) {
         const ResidualGradArgs a = {(const uint16_t*)h_bf16, (const uint16_t*)y_bf16, (const uint16_t*)dh_bf16, (const uint16_t*)dn_bf16, ldh, ldy, lddh, lddn,
                                     (const uint4*)g_post_bf16, (const uint4*)gate_bf16, (const uint4*)g_pre_bf16, rstd_post, rstd_pre, M, plan.per_gate,
-                                    plan.units, plan.parts, (int)(D / 8), skip_scale, branch_scale, 1.0f / (float)D, (uint16_t*)dx_bf16, (uint16_t*)dy_bf16,
+                                    plan.units, plan.parts, (int)(D / 8), M * D >= kResOnce, skip_scale, branch_scale, 1.0f / (float)D, (uint16_t*)dx_bf16, (uint16_t*)dy_bf16,
                                     lddx, lddy, dg_pre ? sums : nullptr, dg_post ? sums + set : nullptr,
                                     dgate ? (direct ? dgate : sums + 2 * set) : nullptr, amax_dy ? maxima : nullptr};
-        with_row_shape(D / 8, [&](auto TPR, auto U) {
-            const auto kernel = post ? (gated ? (pre ? residual_norm_bwd_kernel<TPR(), U(), true, true, true> : residual_norm_bwd_kernel<TPR(), U(), true, true, false>)
-                                              : (pre ? residual_norm_bwd_kernel<TPR(), U(), true, false, true> : residual_norm_bwd_kernel<TPR(), U(), true, false, false>))
-                                     : (gated ? (pre ? residual_norm_bwd_kernel<TPR(), U(), false, true, true> : residual_norm_bwd_kernel<TPR(), U(), false, true, false>)
-                                              : (pre ? residual_norm_bwd_kernel<TPR(), U(), false, false, true> : residual_norm_bwd_kernel<TPR(), U(), false, false, false>));
-            kernel<<<plan.blocks, res_threads(TPR()), 0, st>>>(a);
+        with_row_shape(D / 8, bwd_chunks(D / 8), [&](auto T, auto U, int threads) {
+            const auto kernel = post ? (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), true, true, true> : residual_norm_bwd_kernel<T(), U(), true, true, false>)
+                                              : (pre ? residual_norm_bwd_kernel<T(), U(), true, false, true> : residual_norm_bwd_kernel<T(), U(), true, false, false>))
+                                     : (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), false, true, true> : residual_norm_bwd_kernel<T(), U(), false, true, false>)
+                                              : (pre ? residual_norm_bwd_kernel<T(), U(), false, false, true> : residual_norm_bwd_kernel<T(), U(), false, false, false>));
+            kernel<<<plan.blocks, threads, 0, st>>>(a);
         });
     }
     ResidualFinalArgs f = {};
