@@ -1,0 +1,189 @@
+"""The new operators as a model's end uses them: blocks with normalised, gated and scaled branches, and the output head behind
+them.  Every operator's outputs are compared with oracle/head_oracle.py on the tensors that it read in the run itself; the linears
+and the attention between them have tests of their own."""
+import numpy as np
+import pytest
+import torch
+
+import oracle as o
+from oracle import head_oracle as ho
+from paper_2410_06511_amd import f8
+from paper_2410_06511_amd.block import TransformerBlock
+from paper_2410_06511_amd.head import OutputHead
+from helpers import bits
+from test_gpu_layer import gen
+from test_gpu_residual import check_forward, check_backward
+import test_gpu_logits as tl
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+
+
+def weights(D, H, Hq, Hkv, hd, seed, post, gates):
+    w = {"g1": gen((D,), seed, 0.3) + 1, "g2": gen((D,), seed + 1, 0.3) + 1, "Wqkv": gen(((Hq + 2 * Hkv) * hd, D), seed + 2, 0.04),
+         "Wo": gen((D, D), seed + 3, 0.04), "W13": gen((2 * H, D), seed + 4, 0.04), "W2": gen((D, H), seed + 5, 0.04)}
+    if post:
+        w.update(p1=gen((D,), seed + 6, 0.3) + 1, p2=gen((D,), seed + 7, 0.3) + 1)
+    if gates:
+        w.update(a1=gen((gates, D), seed + 8, 0.5), a2=gen((gates, D), seed + 9, 0.5))
+    return {k: v.bfloat16().cuda() for k, v in w.items()}
+
+
+@pytest.mark.parametrize("scaling", ("dynamic", "delayed"))
+@pytest.mark.parametrize("post,gates,branch", [(True, 0, 1.0), (True, 2, 0.5), (False, 1, 1.0), (False, 0, 0.25)])
+def test_block_with_shaped_branches(post, gates, branch, scaling):
+    B, S, Hq, Hkv, hd, H = 2, 136, 4, 2, 128, 512
+    D, M = Hq * hd, B * S
+    w = weights(D, H, Hq, Hkv, hd, 100, post, gates)
+    x, dout = gen((M, D), 1).cuda(), gen((M, D), 2, 1e-2).cuda()
+    blk = TransformerBlock(B, S, D, H, Hq, Hkv, hd, EPS, scaling=scaling, post_norm=post, gate_rows=gates, branch_scale=branch)
+    for _ in range(2 if scaling == "delayed" else 1):
+        blk.forward(x, w)
+        blk.backward(x, w, dout)
+    torch.cuda.synchronize()
+    # the two residuals, forward: what they read is still there
+    s1 = dict(x=x, y=blk.yo, g_post=w.get("p1"), gate=w.get("a1"), g_pre=w["g2"], dh=dout, dn=blk.dhn)
+    r1 = dict(h=blk.h1, n=blk.hn, rstd_post=blk.rstd_p1, rstd_pre=blk.rstd2, amax_n=blk.a_hn if scaling == "dynamic" else None)
+    check_forward(s1, r1, 1.0, branch)
+    s2 = dict(x=blk.h1, y=blk.y2, g_post=w.get("p2"), gate=w.get("a2"), g_pre=None, dh=dout, dn=None)
+    r2 = dict(h=blk.out, n=None, rstd_post=blk.rstd_p2, rstd_pre=None, amax_n=None)
+    check_forward(s2, r2, 1.0, branch)
+    # and backward
+    amax = blk.a_dy if scaling == "dynamic" else torch.stack([blk.dyo.float().abs().max(), blk.dy2.float().abs().max()])
+    check_backward(s1, r1, dict(dx=blk.dh1, dy=blk.dyo, dg_post=blk.dp1, dgate=blk.da1, dg_pre=blk.dg2, amax_dy=amax[0:1]), 1.0, branch)
+    # (the stream's own gradient passes the second residual unchanged and is not written again)
+    check_backward(s2, r2, dict(dx=dout, dy=blk.dy2, dg_post=blk.dp2, dgate=blk.da2, amax_dy=amax[1:2]), 1.0, branch)
+    # the products that follow took those gradients: the same calls on their own
+    if scaling == "dynamic":
+        dhh, dW2, datt, dWo = (torch.empty_like(t) for t in (blk.dhh, blk.dW2, blk.datt, blk.dWo))
+        f8.linear_bwd(blk.d_2, blk.dy2, blk.s_2, dhh, dW2, blk.ws)
+        f8.linear_bwd(blk.d_o, blk.dyo, blk.s_o, datt, dWo, blk.ws)
+        torch.cuda.synchronize()
+        for a, b in ((dhh, blk.dhh), (dW2, blk.dW2), (datt, blk.datt), (dWo, blk.dWo)):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("scaling", ("dynamic", "delayed"))
+@pytest.mark.parametrize("recompute", (True, "selective"))
+def test_shaped_block_recomputes_its_own_bits(scaling, recompute):
+    B, S, Hq, Hkv, hd, H = 1, 272, 2, 1, 128, 512
+    D, M = Hq * hd, B * S
+    w = weights(D, H, Hq, Hkv, hd, 200, True, 1)
+    x, dout = gen((M, D), 11).cuda(), gen((M, D), 12, 1e-2).cuda()
+    kept, redo = (TransformerBlock(B, S, D, H, Hq, Hkv, hd, scaling=scaling, post_norm=True, gate_rows=1) for _ in range(2))
+    for _ in range(2):
+        kept.forward(x, w)
+        kept.backward(x, w, dout)
+        redo.forward(x, w)
+        for n in ("xn", "h1", "hn") + (("yo", "y2", "out", "att", "ab") if recompute is True else ()):
+            getattr(redo, n).fill_(5.0)
+        redo.backward(x, w, dout, recompute=recompute)
+        torch.cuda.synchronize()
+        for n in ("dx", "dWqkv", "dWo", "dW13", "dW2", "dg1", "dg2", "dp1", "dp2", "da1", "da2"):
+            assert torch.equal(getattr(kept, n).view(torch.uint8), getattr(redo, n).view(torch.uint8)), n
+
+
+def test_unshaped_block_is_what_it_was():
+    """Defaults leave the block's calls and buffers alone."""
+    blk = TransformerBlock(1, 128, 256, 256, 2, 1)
+    assert not blk.shaped and not any(hasattr(blk, n) for n in ("dyo", "dy2", "dp1", "res_ws"))
+
+
+@pytest.mark.parametrize("scaling", ("dynamic", "delayed"))
+@pytest.mark.parametrize("M,D,vocab", [(48, 256, 1000), (272, 512, 4099)])
+def test_head_losses_on_its_own_logits(M, D, vocab, scaling):
+    x, w = gen((M, D), 3).cuda(), {"g": (gen((D,), 4, 0.2) + 1).bfloat16().cuda()}
+    head = OutputHead(M, D, vocab, EPS, scale=0.8, scaling=scaling)
+    w["Wout"] = gen((head.width, D), 5, 0.1).cuda()
+    targets = tl.make_targets(M, vocab, 6)
+    tn = targets.cpu().numpy()
+    d_logp, d_entropy = torch.full((M,), -1.0 / M, device="cuda"), torch.full((M,), 0.1 / M, device="cuda")
+    steps = 2 if scaling == "delayed" else 1   # (the first delayed step casts with scales of 1)
+    for _ in range(steps):
+        head.forward(x, w, targets, entropy=True)
+        logits = head.logits.clone()
+        head.backward(x, w, targets, d_logp, d_entropy)
+    torch.cuda.synchronize()
+    # log probabilities and entropy of the logits that it had, and their gradient, which took their place
+    r = dict(stats=head.stats, logp=head.logp, entropy=head.entropy, top_ids=None, top_logp=None)
+    tl.check_forward(logits, vocab, r, 0.8, targets, 0)
+    zw = tl.wide(logits)[:, :vocab]
+    ref = ho.token_logprobs_bwd(zw, 0.8, tn, tl.f64(d_logp), tl.f64(d_entropy))
+    tl.check_gradient(zw, vocab, head.logits, head.a_dl, ref, 0.8, np.abs(tl.f64(d_logp)) * (tn >= 0), np.abs(tl.f64(d_entropy)))
+    assert not head.dW[vocab:].any()
+    # the projection took that gradient and its amax: the plain calls on their own give the same bits
+    if scaling == "dynamic":
+        dxn, dW = torch.empty_like(head.dxn), torch.empty_like(head.dW)
+        f8.linear_bwd(head.desc, head.logits, head.saved, dxn, dW, head.ws)
+        torch.cuda.synchronize()
+        assert torch.equal(dxn.view(torch.int16), head.dxn.view(torch.int16)) and torch.equal(dW.view(torch.int16), head.dW.view(torch.int16))
+    # distillation from a teacher that is another projection of the same stream
+    teacher = OutputHead(M, D, vocab, EPS)
+    wt = {"g": w["g"], "Wout": (w["Wout"] + gen((head.width, D), 7, 0.05).cuda())}
+    K = 32
+    ids, top = torch.empty((M, K), dtype=torch.int64, device="cuda"), torch.empty((M, K), device="cuda")
+    f8.token_logprobs(teacher.project(x, wt), vocab, teacher.stats, top_ids=ids, top_logp=top, workspace=torch.empty(
+        f8.logits_workspace_bytes(M, vocab, K), dtype=torch.uint8, device="cuda"))
+    d_loss = torch.full((M,), 1.0 / M, device="cuda")
+    for _ in range(steps):
+        head.forward_distill(x, w, ids, top, tail=True, targets=targets)
+        logits = head.logits.clone()
+        head.backward_distill(x, w, ids, top, d_loss, tail=True, targets=targets, d_logp=d_logp)
+    torch.cuda.synchronize()
+    zw = tl.wide(logits)[:, :vocab]
+    tl.check_distill(zw, ids.cpu().numpy(), top.cpu().numpy(), dict(loss=head.loss), head.logits, head.a_dl, 0.8, True, 1.0, tl.f64(d_loss), tn, tl.f64(d_logp))
+    assert torch.isfinite(head.dx.float()).all() and head.dx.float().abs().max() > 0
+
+
+def test_blocks_and_head_together_in_a_graph():
+    """Two shaped blocks and the head, forward and backward: replayed steps have the bits of eager ones, and the gradient of the
+    input agrees with a difference along it."""
+    B, S, Hq, Hkv, hd, H, vocab = 1, 128, 2, 1, 128, 512, 1003
+    D, M = Hq * hd, B * S
+    ws = [weights(D, H, Hq, Hkv, hd, 300 + 50 * i, True, 1) for i in range(2)]
+    blocks = [TransformerBlock(B, S, D, H, Hq, Hkv, hd, EPS, post_norm=True, gate_rows=1) for _ in range(2)]
+    head = OutputHead(M, D, vocab, EPS)
+    wh = {"g": torch.ones(D, dtype=torch.bfloat16, device="cuda"), "Wout": gen((head.width, D), 9, 0.05).cuda()}
+    x, targets = gen((M, D), 10).cuda(), tl.make_targets(M, vocab, 11)
+    d_logp = torch.full((M,), -1.0 / M, device="cuda")
+    grad = torch.empty_like(x)
+
+    def step():
+        h = blocks[0].forward(x, ws[0])
+        h = blocks[1].forward(h, ws[1])
+        head.forward(h, wh, targets)
+        d = head.backward(h, wh, targets, d_logp)
+        d = blocks[1].backward(blocks[0].out, ws[1], d)
+        grad.copy_(blocks[0].backward(x, ws[0], d))
+    outputs = lambda: [t.clone() for t in (head.logp, grad, head.dW, head.dg, blocks[0].dW2, blocks[0].dp1, blocks[1].da2, blocks[0].dg1)]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        x.copy_(gen((M, D), 20 + i).cuda())
+        graph.replay()
+        torch.cuda.synchronize()
+        got = outputs()
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, outputs()):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+    # The whole gradient against a difference along itself.  Float8 casts round every activation by up to 2^-4 of itself, some
+    # ten times in a row, at random: the slope along a direction of 32768 components averages them; a third is left as margin.
+    g = grad.float()
+    loss = lambda: -(head.logp.double().sum() / M).item()
+    x0 = x.float().clone()
+    length = g.norm()
+    h = 2.0 * x0.norm() / 100 / length
+    values = []
+    for sign in (+1, -1):
+        x.copy_((x0 + sign * h * g).bfloat16())
+        a = blocks[0].forward(x, ws[0])
+        head.forward(blocks[1].forward(a, ws[1]), wh, targets)
+        torch.cuda.synchronize()
+        values.append(loss())
+    slope = (values[0] - values[1]) / (2 * h * length).item()
+    assert abs(slope - length.item()) <= length.item() / 3, (slope, length.item())
