@@ -174,6 +174,38 @@ __device__ inline uint32_t wave_max_u32(uint32_t v)
     return v;
 }
 
+// op over the 64 lanes, in every lane: lanes 32 apart, then 16, ... 1 (once lanes 8 apart agree, a rotation by 4 within 16
+// lanes is the exchange with the lane 4 apart, and so on).  Swaps and rotations in registers: a sixth of the latency of
+// exchanges through LDS.  op must give the same bits with its operands exchanged; T is some 32-bit words.
+template <class T, class Op>
+__device__ inline T wave_all(T v, Op&& op)
+{
+    constexpr int N = sizeof(T) / 4;
+    struct Words {
+        uint32_t w[N];
+    };
+    const auto step = [&](auto&& pair) {
+        const Words x = __builtin_bit_cast(Words, v);
+        Words a, b;
+#pragma unroll
+        for (int i = 0; i < N; ++i) pair(x.w[i], a.w[i], b.w[i]);
+        v = op(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b));
+    };
+    step([](uint32_t x, uint32_t& a, uint32_t& b) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        a = r[0], b = r[1];
+    });
+    step([](uint32_t x, uint32_t& a, uint32_t& b) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        a = r[0], b = r[1];
+    });
+    step([](uint32_t x, uint32_t& a, uint32_t& b) { a = x, b = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xF, 0xF, true); });
+    step([](uint32_t x, uint32_t& a, uint32_t& b) { a = x, b = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xF, 0xF, true); });
+    step([](uint32_t x, uint32_t& a, uint32_t& b) { a = x, b = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xF, 0xF, true); });
+    step([](uint32_t x, uint32_t& a, uint32_t& b) { a = x, b = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xF, 0xF, true); });
+    return v;
+}
+
 // Max over a block of NW wavefronts; every thread gets the result.  `red` is
 // NW words of LDS.  Ends with a barrier, so `red` may be reused afterwards.
 template <int NW>

@@ -60,10 +60,7 @@ __device__ inline Stat join(const Stat& a, const Stat& b, float c)
 template <bool ENT>
 __device__ inline Stat wave_join(Stat v, float c)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1)
-        v = join<ENT>(v, {__shfl_xor(v.m, off, kWave), __shfl_xor(v.s, off, kWave), __shfl_xor(v.d, off, kWave)}, c);
-    return v;
+    return wave_all(v, [c](const Stat& a, const Stat& b) { return join<ENT>(a, b, c); });
 }
 
 // ---- order of logits -----------------------------------------------------------------------------
@@ -231,15 +228,10 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInput
         double sum = 0.0;
         float norm = 0.0f;
         if (!a.t.tail) {
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) {
-                const float o = __shfl_xor(top, off, kWave);
-                top = o > top || o != o ? o : top;
-            }
+            top = wave_all(top, [](float x, float y) { return x != x ? x : x > y ? x : y; });  // (a NaN stays)
 #pragma unroll
             for (int e = 0; e < E; ++e) sum += lq[e] == -INFINITY ? 0.0 : (double)expf(lq[e] - top);
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+            sum = wave_all(sum, [](double x, double y) { return x + y; });
             norm = sum == 0.0 ? 0.0f : top + logf((float)sum);
         }
         double loss = 0.0, mass = 0.0;
@@ -249,8 +241,8 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInput
             mass += q;
             if (q != 0.0f) loss += (double)q * (l - (none ? -INFINITY : (in.zk[e] - m) * a.scale - log_total));
         }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) loss += __shfl_xor(loss, off, kWave), mass += __shfl_xor(mass, off, kWave);
+        loss = wave_all(loss, [](double x, double y) { return x + y; });
+        mass = wave_all(mass, [](double x, double y) { return x + y; });
         float coef = sum == 0.0 ? 0.0f : 1.0f;
         if (a.t.tail) {
             const double left = 1.0 - mass, rest = none ? 0.0 : (double)v.s / total;
@@ -268,25 +260,53 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInput
     }
 }
 
+// Places of n keys (all different) among themselves, by counting: emit(place, key) for the first K.  Where there are threads
+// enough, 2 or 8 adjacent ones count for a key together.  keys has room for kRankPad more, which are set to 0 here (so that loads
+// need no condition and go ahead together: 175 keys 23 000 cycles with one, now 6 000).
+constexpr uint32_t kRankPad = 32;
+template <int THREADS, class Emit>
+__device__ inline void rank_keys(uint64_t* keys, uint32_t n, int K, Emit&& emit)
+{
+    if (threadIdx.x < kRankPad) keys[n + threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t lg = n <= THREADS / 8 ? 3 : n <= THREADS / 2 ? 1 : 0, part = threadIdx.x & ((1u << lg) - 1);
+    for (uint32_t i0 = 0; i0 < n; i0 += THREADS >> lg) {
+        const uint32_t i = i0 + (threadIdx.x >> lg);
+        const uint64_t key = i < n ? keys[i] : 0;
+        int rank = 0;
+        for (uint32_t j = part; j < n && rank < K; j += 4u << lg) {
+            uint64_t other[4];
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) other[k] = keys[j + (k << lg)];
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) rank += other[k] > key;
+        }
+        for (uint32_t off = 1; off < 1u << lg; off *= 2) rank += __shfl_xor(rank, off, kWave);
+        if (i < n && part == 0 && rank < K) emit(rank, key);
+    }
+}
+
 // Selection of a block's K largest elements.  A step's chunks of one thread (32 elements) leave their maximum in LDS, 2 bytes,
 // and every thread knows its own largest.  The K-th largest of these bounds the search: K elements reach it, so the K best do, and
 // they lie in steps whose maximum does.  Those are read again (about K, where the large elements are spread) and what reaches the
 // bound is ranked by counting.
 struct Select {
-    uint64_t cand[kLgCandidates];
+    uint64_t cand[kLgCandidates + kRankPad];
     uint16_t step[kLgCandidates];
     uint32_t best[kLgThreads];
     uint32_t bound, nstep, ncand;
 };
 
-// The largest value that at least K of the threads' maxima reach (every one of kLgThreads >= K has one, 0 if it saw nothing).
+// The largest value that at least K of the threads' maxima reach (every one of kLgThreads >= K has one, 0 if it saw nothing), or
+// the first found that exactly K do.
 __device__ inline uint32_t kth_best(const uint32_t* best, int K)
 {
     const int lane = threadIdx.x & (kWave - 1);
     uint32_t k[kLgWaves], hi = 0, lo = 0;
 #pragma unroll
     for (int i = 0; i < kLgWaves; ++i) k[i] = best[lane + kWave * i], hi = k[i] > hi ? k[i] : hi, lo = i == 0 || k[i] < lo ? k[i] : lo;
-    hi = wave_max_u32(hi), lo = ~wave_max_u32(~lo);
+    hi = wave_all(hi, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    lo = wave_all(lo, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
     while (lo < hi) {
         const uint32_t at = (lo + hi + 1) / 2;
         int n = 0;
@@ -294,6 +314,7 @@ __device__ inline uint32_t kth_best(const uint32_t* best, int K)
         for (int i = 0; i < kLgWaves; ++i) n += __popcll(__ballot(k[i] >= at));
         if (n >= K) lo = at;
         else hi = at - 1;
+        if (n == K) break;
     }
     return lo;
 }
@@ -327,6 +348,21 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
         const uint32_t at = atomicAdd(&S.ncand, 1u);
         if (at < (uint32_t)kLgCandidates) S.cand[at] = element_key(o, col);
     };
+    auto put_reaching = [&](int c) {  // what of a chunk reaches the bound, with one step of the counter
+        const uint4 v = row[c];
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            hits |= (uint32_t)(order16(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu) >= bound && c * 8 + j < V) << j;
+        if (!hits) return;
+        uint32_t at = atomicAdd(&S.ncand, (uint32_t)__popc(hits));
+        for (; hits && at < (uint32_t)kLgCandidates; hits &= hits - 1, ++at) {
+            const int j = __ffs(hits) - 1;
+            const uint32_t pair = j < 4 ? (j < 2 ? v.x : v.y) : j < 6 ? v.z : v.w;
+            S.cand[at] = element_key(order16(j & 1 ? pair >> 16 : pair & 0xFFFFu), (uint32_t)(c * 8 + j));
+        }
+    };
     if (best >= bound)
         for (int i = 0; i < steps; ++i)
             if (smax[i * kLgThreads + tid] >= bound && c0 + i * kLgUnroll * kLgThreads + tid < c1) {
@@ -338,7 +374,7 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
     if (nstep <= (uint32_t)kLgCandidates) {
         for (uint32_t i = tid; i < nstep * kLgUnroll; i += kLgThreads) {
             const int st = S.step[i / kLgUnroll], c = c0 + (st / kLgThreads * kLgUnroll + (int)(i % kLgUnroll)) * kLgThreads + st % kLgThreads;
-            if (c < c1) each_element(row, c, V, [&](uint32_t o, uint32_t col) { if (o >= bound) put(o, col); });
+            if (c < c1) put_reaching(c);
         }
         __syncthreads();
     }
@@ -394,13 +430,7 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
             n = S.ncand;
         }
     }
-    for (uint32_t i = tid; i < n; i += kLgThreads) {
-        const uint64_t key = S.cand[i];
-        int rank = 0;
-#pragma unroll 8
-        for (uint32_t j = 0; j < n; ++j) rank += S.cand[j] > key;
-        if (rank < K) emit(rank, key);
-    }
+    rank_keys<kLgThreads>(S.cand, n, K, emit);
 }
 
 // One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.
@@ -509,7 +539,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
 template <bool ENT, bool LIST>
 __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs a)
 {
-    extern __shared__ uint64_t cand[];  // [nseg * top]
+    extern __shared__ uint64_t cand[];  // [nseg * top + kRankPad]
     __shared__ uint32_t n;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const float c2 = a.scale * kLog2e;
@@ -531,11 +561,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
         for (int u = 0; u < AHEAD; ++u) mine[u] = tid + u * kLgThreads < keys ? lists[tid + u * kLgThreads] : 0;
         v = wave_join<ENT>(v, c2);
         if (keys) {
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) {
-                const uint64_t o = __shfl_xor(least, off, kWave);
-                least = o < least ? o : least;
-            }
+            least = wave_all(least, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
             if (tid == 0) n = 0;
             __syncthreads();
 #pragma unroll
@@ -547,17 +573,10 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
             }
             __syncthreads();
             const float log_total = logf(v.s);
-            for (uint32_t i = tid; i < n; i += kLgThreads) {
-                const uint64_t key = cand[i];
-                int rank = 0;
-                for (uint32_t j = 0; j < n && rank < a.top; j += 8)
-#pragma unroll
-                    for (uint32_t k = j; k < j + 8; ++k) rank += k < n && cand[k] > key;
-                if (rank < a.top) {
-                    a.top_ids[row * a.top + rank] = key_column(key);
-                    a.top_logp[row * a.top + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
-                }
-            }
+            rank_keys<kLgThreads>(cand, n, a.top, [&](int rank, uint64_t key) {
+                a.top_ids[row * a.top + rank] = key_column(key);
+                a.top_logp[row * a.top + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
+            });
         }
         if (tid / kWave == kLgWaves - 1) finish_row<LIST>(a, row, in, v);  // (while the first waves rank)
         __syncthreads();
@@ -686,19 +705,18 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
 
 // ---- host ---------------------------------------------------------------------------------------------
 
-// Into how many pieces of how many chunks rows are cut: enough blocks for the chip where there are few rows, no piece shorter
-// than one chunk a thread.
+// Into how many pieces of how many chunks rows are cut: enough blocks for the chip where there are few rows, pieces of `least`
+// chunks at least.
 struct Split {
     int nseg, seg_chunks;
 };
-static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted, int threads)
+static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted, int least)
 {
-    const int64_t chunks = (cols + 7) / 8;
+    const int64_t chunks = (cols + 7) / 8, must = (cols + kLgSegCols - 1) / kLgSegCols;
     int64_t n = M > 0 ? blocks_wanted / M : 1;
-    if (n > chunks / threads) n = chunks / threads;
+    if (n > chunks / least) n = chunks / least;
     if (n > kLgMaxSeg) n = kLgMaxSeg;
-    const int64_t least = (cols + kLgSegCols - 1) / kLgSegCols;
-    if (n < least) n = least;
+    if (n < must) n = must;
     if (n < 1) n = 1;
     const int64_t per = (chunks + n - 1) / n;
     return {(int)((chunks + per - 1) / per), (int)per};
@@ -708,7 +726,7 @@ constexpr int64_t kLgOnce = (int64_t)1 << 29, kLgGradOnce = (int64_t)1 << 27;
 
 static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
 {
-    const Split s = split_rows(M, V, kLgBlocksWanted, kLgThreads);
+    const Split s = split_rows(M, V, kLgBlocksWanted, kLgUnroll * kLgThreads);
     return s.nseg > 1 ? (size_t)M * s.nseg * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
 }
 
@@ -732,7 +750,7 @@ template <bool LIST>
 static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_t st)
 {
     if (a.M == 0) return F8_OK;
-    const Split s = split_rows(a.M, a.V, kLgBlocksWanted, kLgThreads);
+    const Split s = split_rows(a.M, a.V, kLgBlocksWanted, kLgUnroll * kLgThreads);
     a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
     if (a.nseg > 1) {
         if (!ws || ws_bytes < logits_part_bytes(a.M, a.V, a.top)) return F8_ERR_WORKSPACE;
@@ -757,7 +775,7 @@ static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_
     if (a.nseg > 1) {
         const unsigned rows = (unsigned)(a.M < (1 << 20) ? a.M : (1 << 20));
         const auto kernel = a.entropy ? logits_join_kernel<true, LIST> : logits_join_kernel<false, LIST>;
-        kernel<<<rows, kLgThreads, (size_t)a.nseg * a.top * sizeof(uint64_t), st>>>(a);
+        kernel<<<rows, kLgThreads, ((size_t)a.nseg * a.top + kRankPad) * sizeof(uint64_t), st>>>(a);
     }
     return last_launch_status();
 }
@@ -769,7 +787,7 @@ static f8_status launch_grad(GradArgs& a, float* amax, void* ws, hipStream_t st)
     if (a.M > 0) {
         Split s = split_rows(a.M, a.cols, kLgGradBlocks / 2, 1024);
         const bool wide = s.seg_chunks >= kLgGradUnroll * 1024 && a.M * s.nseg >= kLgGradBlocks;
-        if (!wide) s = split_rows(a.M, a.cols, LIST ? kLgGradBlocks / 2 : kLgGradBlocks, 512);
+        if (!wide) s = LIST ? split_rows(a.M, a.cols, kLgGradBlocks / 4, 512) : split_rows(a.M, a.cols, kLgGradBlocks, kLgGradUnroll * 512);
         a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
         a.partial = amax ? (uint32_t*)ws : nullptr;
         const int64_t units = a.M * a.nseg;

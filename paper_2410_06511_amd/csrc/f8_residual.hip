@@ -69,21 +69,10 @@ __device__ inline float rsqrt_exact(double v)
     return (float)(r + 0.5 * r * (1.0 - v * r * r));
 }
 
-// Sum over a wave in the order of exchanges by halves (lanes 32 apart, then 16, ... 1): once lanes 8 apart agree, a rotation by 4
-// within 16 lanes is the exchange with the lane 4 apart, and so on.  Swaps and rotations are a fraction of the latency of
-// exchanges through LDS, which a row waits for twice.
-template <int ROTATE>
-__device__ inline float plus_rotated(float v)
-{
-    return v + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x120 + ROTATE, 0xF, 0xF, true));
-}
+// Sum over a wave in f8_rmsnorm's order; a row waits for it up to twice.
 __device__ inline float wave_sum(float v)
 {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
-    return plus_rotated<1>(plus_rotated<2>(plus_rotated<4>(plus_rotated<8>(v))));
+    return wave_all(v, [](float a, float b) { return a + b; });
 }
 
 // Sum over a row of the chunks' terms; thread t of the row's TPR has chunks t, t + TPR, ...  Two buffers in turn and one barrier:
