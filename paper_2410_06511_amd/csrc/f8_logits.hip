@@ -730,10 +730,12 @@ static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
     return s.nseg > 1 ? (size_t)M * s.nseg * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
 }
 
+static bool bad_scale(float scale) { return !(scale > 0.0f) || !(scale * kLog2e <= FLT_MAX); }
+
 static f8_status check_logits(const void* logits, int64_t ld, int64_t M, int64_t V, float scale, const void* stats)
 {
     if (M != 0 && (!logits || !stats)) return F8_ERR_NULL;  // (without rows there is nothing that pointers point to)
-    if (M < 0 || M > 0x7FFFFFFF || V < 1 || V > kLgMaxCols || ld < V || (ld % 8) || ld > 0x7FFFFFFF || !(scale > 0.0f) || !(scale <= FLT_MAX)) return F8_ERR_SHAPE;
+    if (M < 0 || M > 0x7FFFFFFF || V < 1 || V > kLgMaxCols || ld < V || (ld % 8) || ld > 0x7FFFFFFF || bad_scale(scale)) return F8_ERR_SHAPE;
     if (!aligned16(logits)) return F8_ERR_ALIGN;
     return F8_OK;
 }
@@ -742,7 +744,7 @@ static f8_status check_teacher(int64_t M, const int64_t* ids, const float* logp,
 {
     if (M != 0 && (!ids || !logp)) return F8_ERR_NULL;
     if (tail != 0 && tail != 1) return F8_ERR_ENUM;
-    if (K < 1 || K > kLgMaxTop || !(scale > 0.0f) || !(scale <= FLT_MAX) || (tail && scale != 1.0f)) return F8_ERR_SHAPE;
+    if (K < 1 || K > kLgMaxTop || bad_scale(scale) || (tail && scale != 1.0f)) return F8_ERR_SHAPE;
     return F8_OK;
 }
 

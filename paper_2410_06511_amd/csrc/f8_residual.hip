@@ -61,12 +61,12 @@ __device__ inline uint32_t waves_max(uint32_t v, uint32_t* red)
     return threadIdx.x < kWave ? wave_max_u32(threadIdx.x < blockDim.x / kWave ? red[threadIdx.x] : 0) : 0;
 }
 
-// 1 / sqrt(v) rounded once: the instruction and one Newton step in fp64.  (The norm of the branch; the one after the sum has
-// f8_rmsnorm's arithmetic and bits.)
+// 1 / sqrt(v) rounded once: the fp64 instruction (some 2^-26 off) and one Newton step.  (The norm of the branch; the one after
+// the sum has f8_rmsnorm's arithmetic and bits.)
 __device__ inline float rsqrt_exact(double v)
 {
-    const double r = (double)__builtin_amdgcn_rsqf((float)v);
-    return (float)(r + 0.5 * r * (1.0 - v * r * r));
+    const double r = __builtin_amdgcn_rsq(v);
+    return (float)(r > 0.0 && r < __builtin_inf() ? r + 0.5 * r * (1.0 - v * r * r) : r);
 }
 
 // Sum over a wave in f8_rmsnorm's order; a row waits for it up to twice.
@@ -467,8 +467,8 @@ static bool bad_pitch(int64_t ld, int64_t D) { return ld < D || (ld % 8); }
 
 static f8_status check_residual(int64_t M, int64_t D, const void* gate, int64_t gate_rows, float a, float b)
 {
-    if (M < 0 || M > 0x7FFFFFFF || D < 0 || D > kResMaxD || (D % 8) || gate_rows < 0 || (gate != nullptr) != (gate_rows > 0) ||
-        (gate_rows > 0 && M % gate_rows) || gate_rows > 65535 - 2 || !(a - a == 0.0f) || !(b - b == 0.0f))
+    if (M < 0 || M > 0x7FFFFFFF || D < 0 || D > kResMaxD || (D % 8) || gate_rows < 0 || gate_rows * D > 0x7FFFFFFFFLL ||
+        (gate != nullptr) != (gate_rows > 0) || (gate_rows > 0 && M % gate_rows) || !(a - a == 0.0f) || !(b - b == 0.0f))
         return F8_ERR_SHAPE;
     return F8_OK;
 }
@@ -565,8 +565,12 @@ f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf
     if (dg_pre) f.part[f.sets] = sums, f.out[f.sets++] = dg_pre;
     if (dg_post) f.part[f.sets] = sums + set, f.out[f.sets++] = dg_post;
     f.strips = plan.blocks, f.parts = plan.parts, f.part_gate = sums + 2 * set, f.dgate = dgate, f.D = D;
-    if (M == 0) f.parts = 0;
-    const int64_t gate_sets = dgate && (!direct || M == 0) ? gate_rows : 0;
+    const int64_t gate_sets = dgate && !direct ? gate_rows : 0;  // (fewer than blocks)
+    if (M == 0 && dgate && D > 0) {  // no rows: zeros
+        ResidualFinalArgs z = {};
+        z.dgate = dgate, z.D = gate_rows * D;
+        residual_final_kernel<<<(unsigned)((z.D + kResFinalCols - 1) / kResFinalCols), kResFinalCols * kResFinalGroups, 0, st>>>(z);
+    }
     if (f.sets + gate_sets > 0 && D > 0) {
         if (amax_dy) f.partial = maxima, f.npartial = plan.blocks, f.amax = amax_dy;
         residual_final_kernel<<<dim3((unsigned)((D + kResFinalCols - 1) / kResFinalCols), (unsigned)(f.sets + gate_sets)), kResFinalCols * kResFinalGroups, 0, st>>>(f);

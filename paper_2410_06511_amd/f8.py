@@ -490,46 +490,65 @@ def sdpa_bwd_rows(q, k, v, o, do, lse, B, S, Hq, Hkv, hd, dq, dk, dv, delta, wor
 # ---- residual sum with the norms around it; logits, loss and back -----------------------
 
 F8_ERR_SHAPE = 2
+_BF16, _F32, _I64 = torch.bfloat16, torch.float32, torch.int64
 
 
 def _refuse(name, t, dtype, shape):
-    raise F8Error(F8_ERR_SHAPE, f"{name}: a GPU tensor of {dtype} and shape {shape} with adjacent elements is wanted; "
+    raise F8Error(F8_ERR_SHAPE, f"{name}: a tensor on the current GPU of {dtype} and shape {shape} with adjacent elements is wanted; "
                                 f"got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
 
 
-# What the library cannot see of an argument: type, shape, strides and where it lies.  (In line and in this order because a
-# call of one token takes no longer than its arguments' checks.)
+# What the library cannot see of an argument: type, shape, strides and where it lies.  (A call of one token takes no longer than
+# the look at its arguments, so the usual case comes first and costs five attributes.)
 
-def _packed(name, t, dtype, shape):
+def _current():
+    """Number of the current device (one that no tensor has, if there is none)."""
+    try:
+        return torch.cuda.current_device() if _device is None else _device()
+    except (RuntimeError, AssertionError):
+        return -2
+
+
+def _packed(name, t, dtype, shape, dev):
     """The address of a packed tensor."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        _refuse(name, t, dtype, shape)
-    return t.data_ptr()
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(name, t, dtype, shape)
 
 
-def _rows(name, t, shape):
+def _rows(name, t, shape, dev):
     """Address and row pitch of a bf16 matrix (any pitch that fits, if it has less than two rows)."""
     if t is None:
         return None, 0
-    ld, step = t.stride()
-    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != shape or (step != 1 and shape[1] > 1):
-        _refuse(name, t, torch.bfloat16, shape)
-    return t.data_ptr(), ld if shape[0] > 1 else (max(ld, shape[1]) + 7) // 8 * 8
+    if t.dtype is _BF16 and t.get_device() == dev and t.shape == shape:
+        ld, step = t.stride()
+        if step == 1 or shape[1] <= 1:
+            return t.data_ptr(), ld if shape[0] > 1 else (max(ld, shape[1]) + 7) // 8 * 8
+    _refuse(name, t, _BF16, shape)
+
+
+def _room(ws, dev):
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        _refuse("workspace", ws, ws.dtype, tuple(ws.shape))
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def residual_norm(x, y, h, n=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, eps=1e-5, rstd_post=None, rstd_pre=None,
                   amax_n=None, workspace=None, stream=None):
     """h = skip_scale x + branch_scale gate norm(y) g_post; n = norm(h) g_pre.  gate: [gate_rows, D]."""
     shape = M, D = x.shape
-    bf, f32, gr = torch.bfloat16, torch.float32, 0 if gate is None else gate.shape[0]
-    (xp, ldx), (yp, ldy), (hp, ldh), (np_, ldn) = _rows("x", x, shape), _rows("y", y, shape), _rows("h", h, shape), _rows("n", n, shape)
-    wp, wb = _ws(workspace)
-    _check(lib().f8_residual_norm(xp, ldx, yp, ldy, M, D, _packed("g_post", g_post, bf, (D,)), _packed("gate", gate, bf, (gr, D)), gr,
-                                  _packed("g_pre", g_pre, bf, (D,)), skip_scale, branch_scale, eps, hp, ldh, np_, ldn,
-                                  _packed("rstd_post", rstd_post, f32, (M,)), _packed("rstd_pre", rstd_pre, f32, (M,)),
-                                  _packed("amax_n", amax_n, f32, (1,)), wp, wb, _stream(stream)))
+    gr, of_d, of_m, dev = 0 if gate is None else gate.shape[0], (D,), (M,), _current()
+    (xp, ldx), (yp, ldy), (hp, ldh), (np_, ldn) = _rows("x", x, shape, dev), _rows("y", y, shape, dev), _rows("h", h, shape, dev), _rows("n", n, shape, dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_residual_norm(xp, ldx, yp, ldy, M, D, _packed("g_post", g_post, _BF16, of_d, dev), _packed("gate", gate, _BF16, (gr, D), dev), gr,
+                                  _packed("g_pre", g_pre, _BF16, of_d, dev), skip_scale, branch_scale, eps, hp, ldh, np_, ldn,
+                                  _packed("rstd_post", rstd_post, _F32, of_m, dev), _packed("rstd_pre", rstd_pre, _F32, of_m, dev),
+                                  _packed("amax_n", amax_n, _F32, (1,), dev), wp, wb, _stream(stream)))
 
 
 def residual_norm_bwd_workspace_bytes(M, D, gate_rows=0):
@@ -539,16 +558,18 @@ def residual_norm_bwd_workspace_bytes(M, D, gate_rows=0):
 def residual_norm_bwd(y, dx, dy, h=None, dh=None, dn=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, rstd_post=None,
                       rstd_pre=None, dg_post=None, dgate=None, dg_pre=None, amax_dy=None, workspace=None, stream=None):
     """y may be None without g_post and gate; dx or dy may be None."""
+    if dh is None and dn is None:
+        raise F8Error(1, "residual_norm_bwd: a gradient of h or of n is wanted")
     shape = M, D = (dn if dh is None else dh).shape
-    bf, f32, gr = torch.bfloat16, torch.float32, 0 if gate is None else gate.shape[0]
-    (hp, ldh), (yp, ldy), (dhp, lddh), (dnp, lddn) = _rows("h", h, shape), _rows("y", y, shape), _rows("dh", dh, shape), _rows("dn", dn, shape)
-    (dxp, lddx), (dyp, lddy) = _rows("dx", dx, shape), _rows("dy", dy, shape)
-    wp, wb = _ws(workspace)
-    _check(lib().f8_residual_norm_bwd(hp, ldh, yp, ldy, dhp, lddh, dnp, lddn, M, D, _packed("g_post", g_post, bf, (D,)), _packed("gate", gate, bf, (gr, D)), gr,
-                                      _packed("g_pre", g_pre, bf, (D,)), _packed("rstd_post", rstd_post, f32, (M,)),
-                                      _packed("rstd_pre", rstd_pre, f32, (M,)), skip_scale, branch_scale, dxp, lddx, dyp, lddy,
-                                      _packed("dg_post", dg_post, f32, (D,)), _packed("dgate", dgate, f32, (gr, D)), _packed("dg_pre", dg_pre, f32, (D,)),
-                                      _packed("amax_dy", amax_dy, f32, (1,)), wp, wb, _stream(stream)))
+    gr, of_d, of_m, dev = 0 if gate is None else gate.shape[0], (D,), (M,), _current()
+    (hp, ldh), (yp, ldy), (dhp, lddh), (dnp, lddn) = _rows("h", h, shape, dev), _rows("y", y, shape, dev), _rows("dh", dh, shape, dev), _rows("dn", dn, shape, dev)
+    (dxp, lddx), (dyp, lddy) = _rows("dx", dx, shape, dev), _rows("dy", dy, shape, dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_residual_norm_bwd(hp, ldh, yp, ldy, dhp, lddh, dnp, lddn, M, D, _packed("g_post", g_post, _BF16, of_d, dev), _packed("gate", gate, _BF16, (gr, D), dev), gr,
+                                      _packed("g_pre", g_pre, _BF16, of_d, dev), _packed("rstd_post", rstd_post, _F32, of_m, dev),
+                                      _packed("rstd_pre", rstd_pre, _F32, of_m, dev), skip_scale, branch_scale, dxp, lddx, dyp, lddy,
+                                      _packed("dg_post", dg_post, _F32, of_d, dev), _packed("dgate", dgate, _F32, (gr, D), dev), _packed("dg_pre", dg_pre, _F32, of_d, dev),
+                                      _packed("amax_dy", amax_dy, _F32, (1,), dev), wp, wb, _stream(stream)))
 
 
 def logits_workspace_bytes(M, vocab, top_k=0):
@@ -558,14 +579,14 @@ def logits_workspace_bytes(M, vocab, top_k=0):
 def token_logprobs(logits, vocab, stats, targets=None, logp=None, entropy=None, top_ids=None, top_logp=None, scale=1.0, workspace=None, stream=None):
     """logits: [M, N], the first `vocab` columns are the vocabulary; stats [M, 2]; top_ids, top_logp [M, k]."""
     M, N = logits.shape
-    wp, wb = _ws(workspace)
-    i64, f32 = torch.int64, torch.float32
+    of_m, dev = (M,), _current()
+    wp, wb = _room(workspace, dev)
     k = 0 if top_ids is None else top_ids.shape[1]
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_token_logprobs(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("targets", targets, i64, (M,)), _packed("stats", stats, f32, (M, 2)),
-                                   _packed("logp", logp, f32, (M,)), _packed("entropy", entropy, f32, (M,)), k, _packed("top_ids", top_ids, i64, (M, k)),
-                                   _packed("top_logp", top_logp, f32, (M, k)), wp, wb, _stream(stream)))
+    _check(lib().f8_token_logprobs(*_rows("logits", logits, (M, N), dev), M, vocab, scale, _packed("targets", targets, _I64, of_m, dev), _packed("stats", stats, _F32, (M, 2), dev),
+                                   _packed("logp", logp, _F32, of_m, dev), _packed("entropy", entropy, _F32, of_m, dev), k, _packed("top_ids", top_ids, _I64, (M, k), dev),
+                                   _packed("top_logp", top_logp, _F32, (M, k), dev), wp, wb, _stream(stream)))
 
 
 def token_logprobs_bwd(logits, vocab, stats, dlogits, targets=None, entropy=None, d_logp=None, d_entropy=None, scale=1.0, amax_d=None, workspace=None,
@@ -573,13 +594,13 @@ def token_logprobs_bwd(logits, vocab, stats, dlogits, targets=None, entropy=None
     """dlogits: [M, at least vocab columns]; may be logits itself."""
     M, N = logits.shape
     cols = dlogits.shape[1]
-    wp, wb = _ws(workspace)
-    f32 = torch.float32
+    of_m, dev = (M,), _current()
+    wp, wb = _room(workspace, dev)
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_token_logprobs_bwd(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("targets", targets, torch.int64, (M,)),
-                                       _packed("stats", stats, f32, (M, 2)), _packed("entropy", entropy, f32, (M,)), _packed("d_logp", d_logp, f32, (M,)),
-                                       _packed("d_entropy", d_entropy, f32, (M,)), *_rows("dlogits", dlogits, (M, cols)), cols, _packed("amax_d", amax_d, f32, (1,)), wp, wb,
+    _check(lib().f8_token_logprobs_bwd(*_rows("logits", logits, (M, N), dev), M, vocab, scale, _packed("targets", targets, _I64, of_m, dev),
+                                       _packed("stats", stats, _F32, (M, 2), dev), _packed("entropy", entropy, _F32, of_m, dev), _packed("d_logp", d_logp, _F32, of_m, dev),
+                                       _packed("d_entropy", d_entropy, _F32, of_m, dev), *_rows("dlogits", dlogits, (M, cols), dev), cols, _packed("amax_d", amax_d, _F32, (1,), dev), wp, wb,
                                        _stream(stream)))
 
 
@@ -588,13 +609,13 @@ def distill(logits, vocab, teacher_ids, teacher_logp, stats, loss, targets=None,
     """teacher_ids, teacher_logp: [M, K]; stats [M, 4]."""
     M, N = logits.shape
     K = teacher_ids.shape[1]
-    wp, wb = _ws(workspace)
-    i64, f32 = torch.int64, torch.float32
+    of_m, dev = (M,), _current()
+    wp, wb = _room(workspace, dev)
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_distill(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("teacher_ids", teacher_ids, i64, (M, K)),
-                            _packed("teacher_logp", teacher_logp, f32, (M, K)), K, int(bool(tail)), teacher_scale, _packed("targets", targets, i64, (M,)),
-                            _packed("stats", stats, f32, (M, 4)), _packed("loss", loss, f32, (M,)), _packed("logp", logp, f32, (M,)), wp, wb, _stream(stream)))
+    _check(lib().f8_distill(*_rows("logits", logits, (M, N), dev), M, vocab, scale, _packed("teacher_ids", teacher_ids, _I64, (M, K), dev),
+                            _packed("teacher_logp", teacher_logp, _F32, (M, K), dev), K, int(bool(tail)), teacher_scale, _packed("targets", targets, _I64, of_m, dev),
+                            _packed("stats", stats, _F32, (M, 4), dev), _packed("loss", loss, _F32, of_m, dev), _packed("logp", logp, _F32, of_m, dev), wp, wb, _stream(stream)))
 
 
 def distill_bwd(logits, vocab, teacher_ids, teacher_logp, stats, dlogits, d_loss, targets=None, d_logp=None, tail=False, teacher_scale=1.0, scale=1.0,
@@ -602,14 +623,14 @@ def distill_bwd(logits, vocab, teacher_ids, teacher_logp, stats, dlogits, d_loss
     """dlogits: [M, at least vocab columns]; may be logits itself."""
     M, N = logits.shape
     K, cols = teacher_ids.shape[1], dlogits.shape[1]
-    wp, wb = _ws(workspace)
-    i64, f32 = torch.int64, torch.float32
+    of_m, dev = (M,), _current()
+    wp, wb = _room(workspace, dev)
     if vocab > N:
         raise F8Error(F8_ERR_SHAPE, f"a vocabulary of {vocab} in {N} columns")
-    _check(lib().f8_distill_bwd(*_rows("logits", logits, (M, N)), M, vocab, scale, _packed("teacher_ids", teacher_ids, i64, (M, K)),
-                                _packed("teacher_logp", teacher_logp, f32, (M, K)), K, int(bool(tail)), teacher_scale, _packed("targets", targets, i64, (M,)),
-                                _packed("stats", stats, f32, (M, 4)), _packed("d_loss", d_loss, f32, (M,)), _packed("d_logp", d_logp, f32, (M,)),
-                                *_rows("dlogits", dlogits, (M, cols)), cols, _packed("amax_d", amax_d, f32, (1,)), wp, wb, _stream(stream)))
+    _check(lib().f8_distill_bwd(*_rows("logits", logits, (M, N), dev), M, vocab, scale, _packed("teacher_ids", teacher_ids, _I64, (M, K), dev),
+                                _packed("teacher_logp", teacher_logp, _F32, (M, K), dev), K, int(bool(tail)), teacher_scale, _packed("targets", targets, _I64, of_m, dev),
+                                _packed("stats", stats, _F32, (M, 4), dev), _packed("d_loss", d_loss, _F32, of_m, dev), _packed("d_logp", d_logp, _F32, of_m, dev),
+                                *_rows("dlogits", dlogits, (M, cols), dev), cols, _packed("amax_d", amax_d, _F32, (1,), dev), wp, wb, _stream(stream)))
 
 
 # ---- measuring helpers ---------------------------------------------------------------

@@ -57,7 +57,7 @@ DISTILL = dict(z=FAKE, ld=104, M=3, V=100, scale=1.0, ids=FAKE, t=FAKE, K=8, tai
 DISTILL_BWD = dict(z=FAKE, ld=104, M=3, V=100, scale=1.0, ids=FAKE, t=FAKE, K=8, tail=0, ts=1.0, targets=FAKE, stats=FAKE, d_loss=FAKE, d_logp=FAKE, dz=FAKE,
                    ldd=104, cols=104, amax=FAKE, ws=FAKE, wb=8192, stream=None)
 LOGITS = [(NULL, dict(z=None)), (NULL, dict(stats=None)), (SHAPE, dict(M=-1)), (SHAPE, dict(M=1 << 31)), (SHAPE, dict(V=0)), (SHAPE, dict(V=(1 << 22) + 1, ld=1 << 23)),
-          (SHAPE, dict(ld=96)), (SHAPE, dict(ld=101)), (SHAPE, dict(scale=0.0)), (SHAPE, dict(scale=-1.0)), (SHAPE, dict(scale=INF)), (SHAPE, dict(scale=NAN)),
+          (SHAPE, dict(ld=96)), (SHAPE, dict(ld=101)), (SHAPE, dict(scale=0.0)), (SHAPE, dict(scale=-1.0)), (SHAPE, dict(scale=INF)), (SHAPE, dict(scale=NAN)), (SHAPE, dict(scale=3e38)),
           (ALIGN, dict(z=FAKE + 8))]
 TEACHER = [(NULL, dict(ids=None)), (NULL, dict(t=None)), (SHAPE, dict(K=0)), (SHAPE, dict(K=129)), (ENUM, dict(tail=2)), (SHAPE, dict(ts=0.0)),
            (SHAPE, dict(ts=NAN)), (SHAPE, dict(tail=1, ts=0.5))]
@@ -103,13 +103,31 @@ def test_binding_refuses_what_the_library_cannot_see():
     """Wrong types, shapes, strides, and tensors that are not on a GPU, are refused before the library is called."""
     bf, M, D, V = torch.bfloat16, 4, 64, 100
     t = lambda *s, dtype=bf: torch.zeros(s, dtype=dtype)
-    with pytest.raises(f8.F8Error, match="x: a GPU tensor"):
+    with pytest.raises(f8.F8Error, match="x: a tensor on the current GPU"):
         f8.residual_norm(t(M, D), t(M, D), t(M, D))
-    with pytest.raises(f8.F8Error, match="logits: a GPU tensor"):
+    with pytest.raises(f8.F8Error, match="logits: a tensor on the current GPU"):
         f8.token_logprobs(t(M, 104), V, t(M, 2, dtype=torch.float32))
     with pytest.raises(f8.F8Error, match="a vocabulary of 105 in 104 columns"):
         f8.token_logprobs(t(M, 104), 105, t(M, 2, dtype=torch.float32))
+    with pytest.raises(f8.F8Error, match="a gradient of h or of n"):
+        f8.residual_norm_bwd(None, t(M, D), None)
     with pytest.raises(f8.F8Error, match="got torch.float32"):
         f8.residual_norm_bwd(None, t(M, D, dtype=torch.float32), None, dh=t(M, D, dtype=torch.float32))
-    with pytest.raises(f8.F8Error, match="logits: a GPU tensor"):
+    with pytest.raises(f8.F8Error, match="logits: a tensor on the current GPU"):
         f8.distill(t(M, 104), V, t(M, 3, dtype=torch.int64), t(M, 3, dtype=torch.float32), t(M, 4, dtype=torch.float32), t(M, dtype=torch.float32))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The library works on the current device: a tensor of another one (stand-ins that say so) is refused."""
+    class Elsewhere:
+        dtype, shape, device = torch.bfloat16, (4, 64), "cuda:1"
+        def get_device(self): return 1
+        def stride(self): return (64, 1)
+        def is_contiguous(self): return True
+        def data_ptr(self): return FAKE
+    monkeypatch.setattr(f8, "_device", lambda: 0)
+    with pytest.raises(f8.F8Error, match="on cuda:1"):
+        f8.residual_norm(Elsewhere(), Elsewhere(), Elsewhere())
+    monkeypatch.setattr(f8, "_device", lambda: 1)
+    assert f8._rows("x", Elsewhere(), (4, 64), f8._current()) == (FAKE, 64)
+    assert f8._packed("x", Elsewhere(), torch.bfloat16, (4, 64), f8._current()) == FAKE
