@@ -49,6 +49,10 @@ def parse():
     ap.add_argument("--recompute", nargs="?", const="full", default=None, choices=["full", "selective"],
                     help="llama8b_layer: activation checkpointing: run the forward again inside the backward (full), "
                          "or only its cheap bf16 operations, keeping the outputs of the products and of the attention (selective)")
+    ap.add_argument("--vocab", type=int, default=0,
+                    help="llama8b_layer: an output head (final norm, Float8 projection to so many tokens, their log probabilities) follows the block, "
+                         "forward and backward, and the block's gradient comes from it")
+    ap.add_argument("--post-norm", action="store_true", help="llama8b_layer: both branches are normalised before they join the residual stream")
     ap.add_argument("--keep-weights", action="store_true",
                     help="dynamic scaling: quantise the weights once before the timed steps and keep their codes "
                          "(micro-batches of one optimizer step); the default recasts them on every forward")
@@ -854,11 +858,24 @@ def layer_main(args, w):
                "Wo": wl.randn_bf16((D, D), 0.02, 0, generator=g).cuda(),
                "W13": wl.randn_bf16((2 * H, D), 0.02, 0, generator=g).cuda(),
                "W2": wl.randn_bf16((D, H), 0.02, 0, generator=g).cuda()}
-    blk = TransformerBlock(B, S, D, H, Hq, Hkv, hd, scaling=args.scaling)
+    if args.post_norm:
+        weights.update(p1=torch.ones(D, dtype=torch.bfloat16, device="cuda"), p2=torch.ones(D, dtype=torch.bfloat16, device="cuda"))
+    blk = TransformerBlock(B, S, D, H, Hq, Hkv, hd, scaling=args.scaling, post_norm=args.post_norm)
     stream = torch.cuda.current_stream()
+    head = None
+    if args.vocab:
+        from paper_2410_06511_amd.head import OutputHead
+        head = OutputHead(M, D, args.vocab, scaling=args.scaling)
+        dout = head.dx
+        weights_head = {"g": torch.ones(D, dtype=torch.bfloat16, device="cuda"), "Wout": wl.randn_bf16((head.width, D), 0.02, 0, generator=g).cuda()}
+        tokens = torch.randint(0, args.vocab, (M,), generator=g).cuda()
+        d_logp = torch.full((M,), -1.0 / M, device="cuda")
 
     def step():
         blk.forward(x, weights, stream)
+        if head:
+            head.forward(blk.out, weights_head, tokens, stream=stream)
+            head.backward(blk.out, weights_head, tokens, d_logp, stream=stream)
         blk.backward(x, weights, dout, stream, recompute={"full": True, "selective": "selective", None: False}[args.recompute])
 
     for _ in range(args.warmup):
@@ -869,10 +886,13 @@ def layer_main(args, w):
         step()
     torch.cuda.synchronize()
     ms_per_step = (time.perf_counter() - t0) * 1e3 / args.steps
-    flops_step = sum(l.flops for l in w.linears)
+    flops_step = sum(l.flops for l in w.linears) + (6 * M * D * head.width if head else 0)
     tflops = flops_step / (ms_per_step * 1e-3) / 1e12
 
-    calls = blk.forward_stages(x, weights, stream, joined=True) + blk.backward_stages(x, weights, dout, stream, joined=True)  # those of step()
+    calls = blk.forward_stages(x, weights, stream, joined=True)  # those of step()
+    if head:
+        calls += head.forward_stages(blk.out, weights_head, tokens, stream=stream) + head.backward_stages(blk.out, weights_head, tokens, d_logp, stream=stream)
+    calls += blk.backward_stages(x, weights, dout, stream, joined=True)
     reps = max(3, min(args.steps, 10))
     evs = [[(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in calls] for _ in range(reps)]
     for r in range(reps):
@@ -929,7 +949,9 @@ def layer_main(args, w):
         "dtype": "fp8 (e4m3) x fp8 -> fp32 accumulate -> bf16 (linears); bf16 x bf16 -> fp32 (attention)", "data": "synthetic",
         "config": {"workload": f"{w.key}: one Llama 3.1 8B transformer block, {B} x {S} tokens, hidden {D}, FFN {H}, "
                                f"{Hq} query / {Hkv} key-value heads of {hd}: rmsnorm -> wq|wk|wv -> rope -> causal attention -> wo -> "
-                               "+x -> rmsnorm -> w1|w3 -> silu(a)*b -> w2 -> +h, and the backward of every stage",
+                               "+x -> rmsnorm -> w1|w3 -> silu(a)*b -> w2 -> +h, and the backward of every stage"
+                               + (", both branches normalised" if args.post_norm else "")
+                               + (f"; then final norm, Float8 projection to {args.vocab} tokens and their log probabilities, and back" if head else ""),
                    "scaling_granularity": "tensorwise", "scaling_strategy": args.scaling, "grad_format": "e4m3",
                    "chained": True, "recompute_in_backward": args.recompute or "none", "flops_per_step": flops_step,
                    "attention_flops_per_step_not_counted": att_flops},

@@ -5,7 +5,9 @@
 // and distillation from a teacher's listed entries (id_k, q_k), with p_rest, q_rest the masses outside the list:
 //   loss = sum_k q_k (log q_k - log p_k) [+ q_rest (log q_rest - log p_rest)]
 //   dz_j = scale * (g (c p_j - q_j) + the given token's term above),  c = 1 for listed j, 1 [- q_rest / p_rest] for the others.
-// Bound by memory: one read of the logits forward (2 bytes an element), one read and one write backward (4 bytes).
+// Bound by memory: one read of the logits forward (2 bytes an element), one read and one write backward (4 bytes).  8192 x 131072
+// forward 317 us (6.8 TB/s), backward 788 (5.5); beside the loads stand about 9 instructions and an exponential an element, some
+// two thirds of what a compute unit can issue at that rate.
 // Softmax statistics are kept as (largest logit, log of the sum of exp(z - z_max)): a difference of two bf16 values is exact in
 // fp32 where their ratio is below 2^16, so that p keeps its precision however large the logits are, which one number lse would not.
 #include <float.h>
@@ -17,6 +19,8 @@
 
 namespace f8 {
 
+// A block of 256 threads holds little enough that several share a compute unit and hide each other's selection, joins and ends
+// (8192 x 32768 with 32 alternatives 110 us, with 512 threads 128); four loads a thread (two 116, eight 122).
 constexpr int kLgThreads = 256;         // of a block of the forward
 constexpr int kLgWaves = kLgThreads / kWave;
 constexpr int kLgGradUnroll = 4;
@@ -26,7 +30,7 @@ constexpr int kLgMaxSeg = 32;           // blocks that share a row, at most
 constexpr int64_t kLgMaxCols = (int64_t)kLgSegCols * kLgMaxSeg;
 constexpr int kLgMaxTop = 128;          // alternatives, and entries of a teacher's list
 constexpr int kLgCandidates = 1024;     // elements that the selection ranks at once
-constexpr int kLgGradBlocks = 2048;     // of the gradient: one partial maximum each
+constexpr int kLgGradBlocks = 2048;     // of the gradient: one partial maximum each (1024: 8192 x 131072 832 -> 867 us)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint32_t kNegInf2 = 0xFF80FF80u;
 static_assert((size_t)kLgGradBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial maximum per block fits the minimum workspace");
@@ -721,7 +725,13 @@ static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted, int leas
     const int64_t per = (chunks + n - 1) / n;
     return {(int)((chunks + per - 1) / per), (int)per};
 }
+// The forward shares rows among blocks below two blocks a compute unit (more pieces cost more in the join than they bring: us with
+// 512 / 1024 / 2048 blocks, 300 x 50001 with 64 alternatives 23 / 30 / 38, 512 x 50001 without 17.6 / 20.2 / 22.7), in pieces of a
+// full step (of a chunk a thread at least: 100 x 8000 with 20 alternatives 14.8, so 9.5; 16 x 32768 16.2, so 13.3).
 constexpr int64_t kLgBlocksWanted = 512;
+// Loads past the caches.  Forward: from 1 GiB on, of which the backward would find little (8192 x 131072 357 -> 317 us, the backward
+// unchanged; 2048 x 131072 102 -> 93, but its backward 188 -> 205).  Backward, the last to read: from 256 MiB on (4096 x 32768
+// 85 -> 80, 2000 x 131072 with a teacher 211 -> 180; but 512 x 50001 21.9 -> 23.0).
 constexpr int64_t kLgOnce = (int64_t)1 << 29, kLgGradOnce = (int64_t)1 << 27;
 
 static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
@@ -787,6 +797,9 @@ static f8_status launch_grad(GradArgs& a, float* amax, void* ws, hipStream_t st)
 {
     int nb = 0;
     if (a.M > 0) {
+        // Blocks of 1024 threads where there are many long rows (8192 x 131072 819 -> 788 us, 4096 x 131072 with a teacher 419 ->
+        // 397; few rows lose: 300 x 131072 36 -> 41, 777 x 50001 44 -> 52), else of 512, in pieces of a full step, or with a teacher,
+        // whose list every piece sets up, of a quarter of the blocks (64 x 131072 with 64 entries 19.5 -> 12.7, 300 x 50001 23 -> 18).
         Split s = split_rows(a.M, a.cols, kLgGradBlocks / 2, 1024);
         const bool wide = s.seg_chunks >= kLgGradUnroll * 1024 && a.M * s.nseg >= kLgGradBlocks;
         if (!wide) s = LIST ? split_rows(a.M, a.cols, kLgGradBlocks / 4, 512) : split_rows(a.M, a.cols, kLgGradBlocks, kLgGradUnroll * 512);

@@ -3,7 +3,8 @@
 //   t = dh + r2 g_pre dn - h r2^3 mean(h g_pre dn),  dx = a t,  v = b gate t,  dy = r1 g_post v - y r1^3 mean(y g_post v) (or v),
 //   dgate = sum over its rows of b t u,  dg_post = sum v y r1,  dg_pre = sum dn h r2.
 // Bound by memory: 8 bytes an element forward (x, y -> h, n), 12 backward (h, y, dh, dn -> dx, dy); as separate calls the sum,
-// the gate and each norm read and write their tensors again.
+// the gate and each norm read and write their tensors again.  16384 x 8192 with both norms and gates: forward 185 us (5.8 TB/s),
+// backward 330 (4.9); 8192 x 4096 with the norm after the sum only: 47 (5.7) and 64 (5.2).
 // A row is held in registers by TPR threads, U chunks of 16 bytes each, so that every tensor is read once although a norm needs
 // its row twice.  Sums over a row are taken in f8_rmsnorm's order (chunks 64 apart one after the other, then lanes by halves), so
 // that the plain residual and norm have the bits of f8_add followed by f8_rmsnorm.  Sums over rows have a fixed order too.
@@ -16,7 +17,12 @@ namespace f8 {
 
 constexpr int64_t kResMaxD = 16384;
 constexpr int kResBlocks = 2048;     // of the forward: one partial maximum each
-constexpr int kResBwdBlocks = 512;   // of the backward: a partial row of each gain's sums each; half as many of more than 512 threads
+// Blocks of the backward, each of which leaves a partial row of every gain's sums (4096 x 4096 with 256 / 512 blocks 58 / 53 us,
+// 768 71); half as many above 4096 elements a row, where a block's waves fill a compute unit (16384 x 8192 371 -> 341 us, 300 x 8192
+// 26 -> 22).
+constexpr int kResBwdBlocks = 512;
+// Elements from which the backward loads past the caches (16384 x 8192 348 -> 326 us, 8192 x 5120 126 -> 118; 4096 x 4096 52 -> 53,
+// 2001 x 2816 26 -> 27).
 constexpr int64_t kResOnce = (int64_t)1 << 25;
 static_assert((size_t)kResBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial per block fits the minimum workspace");
 
@@ -444,6 +450,10 @@ static void with_row_shape(int64_t dc, int u, F&& f)
     else bounded(integral_constant<int, 2>{});
 }
 static int fwd_chunks(int64_t dc) { return dc <= 64 ? 1 : 2; }
+// The backward holds four rows and up to three rows of sums.  One chunk a thread leaves registers for enough waves up to 8192
+// elements (16384 x 8192 394 -> 371 us, 8192 x 2048 59 -> 50), but a row of 520 to 1024 elements is better a wave's own, without
+// barriers (8192 x 1024 45 -> 30).  Waves hide the loads better than loads ahead of the row, which take their registers (4096 x 4096
+// 74 -> 53).
 static int bwd_chunks(int64_t dc) { return dc <= 64 || (dc > 128 && dc <= 1024) ? 1 : 2; }
 
 // How the backward divides its rows: `parts` blocks share a group of rows with one gate row while there are fewer groups than

@@ -35,47 +35,78 @@ class OutputHead:
         self.dxn, self.dx = torch.empty((M, D), **bf), torch.empty((M, D), **bf)
         self.dg, self.dW = torch.empty(D, **f32), torch.empty((N, D), **bf)
 
-    def project(self, x, w, stream=None):
-        """w: dict with g [D] and Wout [width, D] (bf16).  Returns the logits [M, width]."""
-        s, amax = self, self.state is None
-        f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, s.a_xn if amax else None, s.ws, stream)
-        if amax:
-            f8.linear_fwd_chained(s.desc, s.xn, s.a_xn, w["Wout"], s.logits, None, s.saved, s.ws, stream)
+    def projection_stages(self, x, w, stream=None):
+        """w: dict with g [D] and Wout [width, D] (bf16).  [(name, call, flops, algorithmic bytes)] in execution order, as the block's."""
+        s, M, D = self, self.M, self.D
+        if s.state is None:
+            norm = lambda: f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, s.a_xn, s.ws, stream)
+            linear = lambda: f8.linear_fwd_chained(s.desc, s.xn, s.a_xn, w["Wout"], s.logits, None, s.saved, s.ws, stream)
         else:
-            f8.linear_fwd_scaled(s.desc, s.state, s.xn, w["Wout"], s.logits, s.saved, s.ws, stream)
-        return s.logits
+            norm = lambda: f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, None, None, stream)
+            linear = lambda: f8.linear_fwd_scaled(s.desc, s.state, s.xn, w["Wout"], s.logits, s.saved, s.ws, stream)
+        return [("final rmsnorm", norm, 0, 4 * M * D), ("linear Wout fwd", linear, 2 * M * D * s.width, 0)]
+
+    def _backward_stages(self, x, w, loss, stream):
+        s, M, D = self, self.M, self.D
+        if s.state is None:
+            linear = lambda: f8.linear_bwd_chained(s.desc, s.logits, s.a_dl, s.saved, s.dxn, None, s.dW, s.ws, stream)
+        else:
+            linear = lambda: f8.linear_bwd_scaled(s.desc, s.state, s.logits, s.saved, s.dxn, s.dW, s.ws, stream)
+        return [loss, ("linear Wout bwd", linear, 4 * M * D * s.width, 0),
+                ("final rmsnorm bwd", lambda: f8.rmsnorm_bwd(x, w["g"], s.rstd, s.dxn, s.dx, s.dg, s.ws, stream), 0, 6 * M * D)]
+
+    def forward_stages(self, x, w, targets, entropy=False, stream=None):
+        s = self
+        return self.projection_stages(x, w, stream) + [
+            ("token log probabilities", lambda: f8.token_logprobs(s.logits, s.vocab, s.stats, targets, s.logp, s.entropy if entropy else None,
+                                                                  scale=s.scale, workspace=s.logits_ws, stream=stream), 0, 2 * s.M * s.vocab)]
+
+    def backward_stages(self, x, w, targets, d_logp, d_entropy=None, stream=None):
+        s = self
+        return self._backward_stages(x, w, (
+            "token log probabilities bwd", lambda: f8.token_logprobs_bwd(s.logits, s.vocab, s.stats, s.logits, targets,
+                                                                         None if d_entropy is None else s.entropy, d_logp, d_entropy, s.scale, s.a_dl,
+                                                                         s.ws, stream), 0, 4 * s.M * s.width), stream)
+
+    def distill_forward_stages(self, x, w, teacher_ids, teacher_logp, tail=False, teacher_scale=1.0, targets=None, stream=None):
+        s = self
+        return self.projection_stages(x, w, stream) + [
+            ("distillation", lambda: f8.distill(s.logits, s.vocab, teacher_ids, teacher_logp, s.kd_stats, s.loss, targets,
+                                                None if targets is None else s.logp, tail, teacher_scale, s.scale, s.logits_ws, stream),
+             0, 2 * s.M * s.vocab)]
+
+    def distill_backward_stages(self, x, w, teacher_ids, teacher_logp, d_loss, tail=False, teacher_scale=1.0, targets=None, d_logp=None, stream=None):
+        s = self
+        return self._backward_stages(x, w, (
+            "distillation bwd", lambda: f8.distill_bwd(s.logits, s.vocab, teacher_ids, teacher_logp, s.kd_stats, s.logits, d_loss, targets, d_logp, tail,
+                                                       teacher_scale, s.scale, s.a_dl, s.ws, stream), 0, 4 * s.M * s.width), stream)
+
+    @staticmethod
+    def _run(stages):
+        for _, call, _, _ in stages:
+            call()
+
+    def project(self, x, w, stream=None):
+        """The logits [M, width]."""
+        self._run(self.projection_stages(x, w, stream))
+        return self.logits
 
     def forward(self, x, w, targets, entropy=False, stream=None):
         """Log probabilities of the targets [M] (int64; negative: no token); with entropy the distributions' too, in .entropy."""
-        self.project(x, w, stream)
-        f8.token_logprobs(self.logits, self.vocab, self.stats, targets, self.logp, self.entropy if entropy else None, scale=self.scale,
-                          workspace=self.logits_ws, stream=stream)
+        self._run(self.forward_stages(x, w, targets, entropy, stream))
         return self.logp
 
     def backward(self, x, w, targets, d_logp, d_entropy=None, stream=None):
         """Gradient of x, from those of .logp and .entropy [M] (next-token training: d_logp = -1 / tokens)."""
-        f8.token_logprobs_bwd(self.logits, self.vocab, self.stats, self.logits, targets, None if d_entropy is None else self.entropy, d_logp, d_entropy,
-                              self.scale, self.a_dl, self.ws, stream)
-        return self._backward(x, w, stream)
+        self._run(self.backward_stages(x, w, targets, d_logp, d_entropy, stream))
+        return self.dx
 
     def forward_distill(self, x, w, teacher_ids, teacher_logp, tail=False, teacher_scale=1.0, targets=None, stream=None):
         """Divergence from the teacher's entries [M, K] (f8.token_logprobs of its logits gives them); with targets their log
         probabilities too, in .logp."""
-        self.project(x, w, stream)
-        f8.distill(self.logits, self.vocab, teacher_ids, teacher_logp, self.kd_stats, self.loss, targets, None if targets is None else self.logp, tail,
-                   teacher_scale, self.scale, self.logits_ws, stream)
+        self._run(self.distill_forward_stages(x, w, teacher_ids, teacher_logp, tail, teacher_scale, targets, stream))
         return self.loss
 
     def backward_distill(self, x, w, teacher_ids, teacher_logp, d_loss, tail=False, teacher_scale=1.0, targets=None, d_logp=None, stream=None):
-        f8.distill_bwd(self.logits, self.vocab, teacher_ids, teacher_logp, self.kd_stats, self.logits, d_loss, targets, d_logp, tail, teacher_scale,
-                       self.scale, self.a_dl, self.ws, stream)
-        return self._backward(x, w, stream)
-
-    def _backward(self, x, w, stream):
-        s = self
-        if s.state is None:
-            f8.linear_bwd_chained(s.desc, s.logits, s.a_dl, s.saved, s.dxn, None, s.dW, s.ws, stream)
-        else:
-            f8.linear_bwd_scaled(s.desc, s.state, s.logits, s.saved, s.dxn, s.dW, s.ws, stream)
-        f8.rmsnorm_bwd(x, w["g"], s.rstd, s.dxn, s.dx, s.dg, s.ws, stream)
-        return s.dx
+        self._run(self.distill_backward_stages(x, w, teacher_ids, teacher_logp, d_loss, tail, teacher_scale, targets, d_logp, stream))
+        return self.dx
