@@ -201,7 +201,6 @@ struct ResidualGradArgs {
     const float *rstd_post, *rstd_pre;
     int64_t M, per_gate, units;
     int parts, dc;
-    bool once;  // loads past the caches
     float a, b, inv_d;
     uint16_t *dx, *dy;  // nullable
     int64_t lddx, lddy;
@@ -211,7 +210,7 @@ struct ResidualGradArgs {
 
 // A block takes units: the rows part, part + parts, ... of one group of rows that share a gate's row, and leaves one row of
 // sums a gain.
-template <int THREADS, int U, bool POST, bool GATE, bool PRE>
+template <int THREADS, int U, bool POST, bool GATE, bool PRE, bool ONCE>
 __global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_bwd_kernel(const ResidualGradArgs p)
 {
     constexpr int kRows = THREADS == kWave ? kResWaveRows : 1;
@@ -269,15 +268,10 @@ __global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_bwd_kernel
                 const int c = t + TPR * u;
                 row.h[u] = row.y[u] = row.dh[u] = row.dn[u] = make_uint4(0, 0, 0, 0);
                 if (!live || c >= p.dc) continue;
-                if (p.once) {
-                    if (PRE) row.h[u] = load_once(row_of(p.h, m, p.ldh) + c), row.dn[u] = load_once(row_of(p.dn, m, p.lddn) + c);
-                    if (POST || GATE) row.y[u] = load_once(row_of(p.y, m, p.ldy) + c);
-                    if (!PRE || p.dh) row.dh[u] = load_once(row_of(p.dh, m, p.lddh) + c);
-                } else {
-                    if (PRE) row.h[u] = row_of(p.h, m, p.ldh)[c], row.dn[u] = row_of(p.dn, m, p.lddn)[c];
-                    if (POST || GATE) row.y[u] = row_of(p.y, m, p.ldy)[c];
-                    if (!PRE || p.dh) row.dh[u] = row_of(p.dh, m, p.lddh)[c];
-                }
+                const auto load = [&](const uint16_t* t, int64_t ld) { return ONCE ? load_once(row_of(t, m, ld) + c) : row_of(t, m, ld)[c]; };
+                if (PRE) row.h[u] = load(p.h, p.ldh), row.dn[u] = load(p.dn, p.lddn);
+                if (POST || GATE) row.y[u] = load(p.y, p.ldy);
+                if (!PRE || p.dh) row.dh[u] = load(p.dh, p.lddh);
             }
             row.r1 = POST && live ? p.rstd_post[m] : 0.0f;
             row.r2 = PRE && live ? p.rstd_pre[m] : 0.0f;
@@ -560,14 +554,18 @@ f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf
     if (M > 0 && D > 0) {
         const ResidualGradArgs a = {(const uint16_t*)h_bf16, (const uint16_t*)y_bf16, (const uint16_t*)dh_bf16, (const uint16_t*)dn_bf16, ldh, ldy, lddh, lddn,
                                     (const uint4*)g_post_bf16, (const uint4*)gate_bf16, (const uint4*)g_pre_bf16, rstd_post, rstd_pre, M, plan.per_gate,
-                                    plan.units, plan.parts, (int)(D / 8), M * D >= kResOnce, skip_scale, branch_scale, 1.0f / (float)D, (uint16_t*)dx_bf16, (uint16_t*)dy_bf16,
+                                    plan.units, plan.parts, (int)(D / 8), skip_scale, branch_scale, 1.0f / (float)D, (uint16_t*)dx_bf16, (uint16_t*)dy_bf16,
                                     lddx, lddy, dg_pre ? sums : nullptr, dg_post ? sums + set : nullptr,
                                     dgate ? (direct ? dgate : sums + 2 * set) : nullptr, amax_dy ? maxima : nullptr};
         with_row_shape(D / 8, bwd_chunks(D / 8), [&](auto T, auto U, int threads) {
-            const auto kernel = post ? (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), true, true, true> : residual_norm_bwd_kernel<T(), U(), true, true, false>)
-                                              : (pre ? residual_norm_bwd_kernel<T(), U(), true, false, true> : residual_norm_bwd_kernel<T(), U(), true, false, false>))
-                                     : (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), false, true, true> : residual_norm_bwd_kernel<T(), U(), false, true, false>)
-                                              : (pre ? residual_norm_bwd_kernel<T(), U(), false, false, true> : residual_norm_bwd_kernel<T(), U(), false, false, false>));
+            const auto pick = [&](auto ONCE) {
+                constexpr bool O = ONCE();
+                return post ? (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), true, true, true, O> : residual_norm_bwd_kernel<T(), U(), true, true, false, O>)
+                                     : (pre ? residual_norm_bwd_kernel<T(), U(), true, false, true, O> : residual_norm_bwd_kernel<T(), U(), true, false, false, O>))
+                            : (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), false, true, true, O> : residual_norm_bwd_kernel<T(), U(), false, true, false, O>)
+                                     : (pre ? residual_norm_bwd_kernel<T(), U(), false, false, true, O> : residual_norm_bwd_kernel<T(), U(), false, false, false, O>));
+            };
+            const auto kernel = M * D >= kResOnce ? pick(std::true_type{}) : pick(std::false_type{});
             kernel<<<plan.blocks, threads, 0, st>>>(a);
         });
     }
