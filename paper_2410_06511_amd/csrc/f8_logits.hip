@@ -511,7 +511,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
                 for (int j = 0; j < 8; ++j) {
                     const float l = (z[u][j] - v.m) * c2, e = exp2_hw(l);
                     v.s += e;
-                    if constexpr (ENT) v.d += e * fmaxf(l, kFar);
+                    if constexpr (ENT) v.d = __builtin_fmaf(e, fmaxf(l, kFar), v.d);
                 }
         }
         v = wave_join<ENT>(v, c2);
