@@ -20,7 +20,7 @@
 namespace f8 {
 
 // A block of 256 threads holds little enough that several share a compute unit and hide each other's selection, joins and ends
-// (8192 x 32768 with 32 alternatives 110 us, with 512 threads 128); four loads a thread (two 116, eight 122).
+// (8192 x 32768 with 32 alternatives 111 us, with 512 threads 137); four loads a thread (two 116, eight 122).
 constexpr int kLgThreads = 256;         // of a block of the forward
 constexpr int kLgWaves = kLgThreads / kWave;
 constexpr int kLgGradUnroll = 4;

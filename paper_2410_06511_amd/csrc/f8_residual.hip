@@ -3,8 +3,8 @@
 //   t = dh + r2 g_pre dn - h r2^3 mean(h g_pre dn),  dx = a t,  v = b gate t,  dy = r1 g_post v - y r1^3 mean(y g_post v) (or v),
 //   dgate = sum over its rows of b t u,  dg_post = sum v y r1,  dg_pre = sum dn h r2.
 // Bound by memory: 8 bytes an element forward (x, y -> h, n), 12 backward (h, y, dh, dn -> dx, dy); as separate calls the sum,
-// the gate and each norm read and write their tensors again.  16384 x 8192 with both norms and gates: forward 185 us (5.8 TB/s),
-// backward 330 (4.9); 8192 x 4096 with the norm after the sum only: 47 (5.7) and 64 (5.2).
+// the gate and each norm read and write their tensors again.  16384 x 8192 with both norms and gates: forward 190 us (5.6 TB/s),
+// backward 321 and 7 for its sums (4.9); 8192 x 4096 with the norm after the sum only: 44 (6.1), 57 and 5 (5.4).
 // A row is held in registers by TPR threads, U chunks of 16 bytes each, so that every tensor is read once although a norm needs
 // its row twice.  Sums over a row are taken in f8_rmsnorm's order (chunks 64 apart one after the other, then lanes by halves), so
 // that the plain residual and norm have the bits of f8_add followed by f8_rmsnorm.  Sums over rows have a fixed order too.
@@ -446,7 +446,8 @@ static void with_row_shape(int64_t dc, int u, F&& f)
 static int fwd_chunks(int64_t dc) { return dc <= 64 ? 1 : 2; }
 // The backward holds four rows and up to three rows of sums.  One chunk a thread leaves registers for enough waves up to 8192
 // elements (16384 x 8192 394 -> 371 us, 8192 x 2048 59 -> 50), but a row of 520 to 1024 elements is better a wave's own, without
-// barriers (8192 x 1024 45 -> 30).  Waves hide the loads better than loads ahead of the row, which take their registers (4096 x 4096
+// barriers (8192 x 1024 45 -> 30); with a norm of the branch the two are within 6 % between 2816 and 4096 (2001 x 2816 26.9 -> 25.8,
+// 8192 x 2816 66 -> 70).  Waves hide the loads better than loads ahead of the row, which take their registers (4096 x 4096
 // 74 -> 53).
 static int bwd_chunks(int64_t dc) { return dc <= 64 || (dc > 128 && dc <= 1024) ? 1 : 2; }
 
