@@ -113,6 +113,11 @@ def _teacher_row(ids, t, tail, teacher_scale):
     return ids, np.exp(t) if tail else np.exp(t - t.max()) / np.exp(t - t.max()).sum()
 
 
+def _has_term(ids, cols, tail):
+    """whether a row has entries (tail), or weights to share out"""
+    return (ids >= 0).any() if tail else len(cols) > 0
+
+
 def _rest(listed, p, q):
     q_rest = 1.0 - q.sum()
     return (0.0 if q_rest < 2.0 ** -20 else q_rest), p[~listed].sum()
@@ -125,6 +130,8 @@ def distill(z, ids, t, scale=1.0, tail=False, teacher_scale=1.0):
     for r in range(M):
         _, _, lp, p = _softmax_row(z[r], scale)
         cols, q = _teacher_row(ids[r], t[r], tail, teacher_scale)
+        if not _has_term(ids[r], cols, tail):
+            continue
         loss[r] = sum(w * (np.log(w) - lp[c]) for c, w in zip(cols, q) if w > 0)
         if tail:
             listed = np.zeros(V, dtype=bool)
@@ -145,13 +152,14 @@ def distill_bwd(z, ids, t, d_loss, scale=1.0, tail=False, teacher_scale=1.0, tar
         cols, q = _teacher_row(ids[r], t[r], tail, teacher_scale)
         listed = np.zeros(V, dtype=bool)
         listed[ids[r][ids[r] >= 0]] = True
-        coef = 1.0 if len(cols) else 0.0
+        coef = 1.0
         if tail:
             q_rest, p_rest = _rest(listed, p, q)
             coef = 1.0 - q_rest / p_rest if p_rest > 0 else 0.0
-        row = np.where(listed, p, coef * p)
-        np.add.at(row, cols, -q)
-        dz[r] = d_loss[r] * row
+        if _has_term(ids[r], cols, tail):
+            row = np.where(listed, p, coef * p)
+            np.add.at(row, cols, -q)
+            dz[r] = d_loss[r] * row
         if targets is not None and targets[r] >= 0:
             dz[r] -= d_logp[r] * p
             dz[r, targets[r]] += d_logp[r]

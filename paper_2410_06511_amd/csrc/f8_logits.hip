@@ -247,16 +247,21 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInput
         }
         loss = wave_all(loss, [](double x, double y) { return x + y; });
         mass = wave_all(mass, [](double x, double y) { return x + y; });
-        float coef = sum == 0.0 ? 0.0f : 1.0f;
+        float coef = 1.0f;
         if (a.t.tail) {
             const double left = 1.0 - mass, rest = none ? 0.0 : (double)v.s / total;
             const float q_rest = left < kNoRest ? 0.0f : (float)left;  // (a NaN stays)
-            coef = rest > 0.0 ? (float)(1.0 - (double)q_rest / rest) : 0.0f;
-            if (q_rest != 0.0f) loss += (double)q_rest * (logf(q_rest) - (rest > 0.0 ? logf((float)rest) : -INFINITY));
+            coef = rest == 0.0 ? 0.0f : (float)(1.0 - (double)q_rest / rest);
+            if (q_rest != 0.0f) loss += (double)q_rest * (logf(q_rest) - logf((float)rest));
             if (mass != mass) coef = NAN;
         }
         if (none) coef = 0.0f;
-        if (__any(in.wrong)) loss = coef = NAN;
+        // without entries (or weights to share out) there is no term, whatever the logits: marked for the backward by norm = -inf
+        bool some = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) some |= in.has[e];
+        if (a.t.tail ? !__any(some) : sum == 0.0) loss = coef = 0.0f, norm = -INFINITY;
+        if (__any(in.wrong)) loss = coef = NAN, norm = 0.0f;
         if (lane == 0) {
             a.loss[row] = (float)loss;
             a.stats[row * 4 + 2] = coef, a.stats[row * 4 + 3] = norm;
@@ -628,7 +633,7 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
         }
         float g = 0.0f;
         if constexpr (LIST) {
-            g = a.d_loss[rowi] * a.scale;
+            g = st[3] == -INFINITY ? 0.0f : a.d_loss[rowi] * a.scale;  // (a row without entries has no term)
             if (g != 0.0f) A += g * st[2];
             AL = g - dlp;
         }

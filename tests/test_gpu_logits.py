@@ -417,6 +417,45 @@ def test_distill_masked_students_and_lists(M):
                           dz[4:].float().abs().max().reshape(1), 1.0, tail, 1.0, np.ones(M - 4), None, None)
 
 
+@pytest.mark.parametrize("M", (5, 560))
+@pytest.mark.parametrize("tail", (False, True))
+def test_rows_without_entries_have_no_term_whatever_their_logits(M, tail):
+    """Masked rows and rows of what memory held, as behind the last sequence; a weight with no row to fall on is no gradient."""
+    V, K = 2050, 6
+    z = make_logits(M, V, 11)
+    z[0], z[1], z[2, 7] = float("-inf"), float("nan"), float("inf")
+    ids = torch.full((M, K), -1, dtype=torch.int64, device="cuda")
+    t = torch.full((M, K), -2.0, device="cuda")
+    if not tail:  # entries that all weigh nothing
+        ids[3], t[3] = torch.arange(K, device="cuda"), float("-inf")
+    r = distill_forward(z, V, ids, t, 1.0, tail, 1.0)
+    dz, am = distill_backward(z, V, ids, t, r, torch.ones(M, device="cuda"), 1.0, tail, 1.0)
+    torch.cuda.synchronize()
+    assert not r["loss"].any() and not dz.any() and am.item() == 0.0
+
+
+@pytest.mark.parametrize("M", (5, 560))
+@pytest.mark.parametrize("tail", (False, True))
+def test_nan_and_infinity_in_a_row_with_entries(M, tail):
+    """Also where the teacher gives its entries no weight, so that only the rest's class has a term; other rows stay finite."""
+    V, K = 2050, 6
+    z = make_logits(M, V, 12)
+    z[:, K:V] = z[:, K:V].clamp(-5, 5)
+    z[1, 100], z[2, 3] = float("nan"), float("inf")
+    ids = torch.arange(K, device="cuda").repeat(M, 1)
+    t = torch.full((M, K), -2.5, device="cuda")
+    if tail:
+        z[3, 200], t[3] = float("inf"), float("-inf")
+    r = distill_forward(z, V, ids, t, 1.0, tail, 1.0)
+    dz, _ = distill_backward(z, V, ids, t, r, torch.ones(M, device="cuda"), 1.0, tail, 1.0)
+    torch.cuda.synchronize()
+    bad = [1, 2, 3] if tail else [1, 2]
+    fine = [i for i in range(M) if i not in bad]
+    assert r["loss"][bad].isnan().all() and dz[bad, :V].isnan().all(dim=1).all()
+    masked = torch.isinf(z[fine, :V][:, :K]).any(dim=1)  # (a listed token that the student masks: infinite)
+    assert torch.isfinite(r["loss"][fine][~masked]).all() and torch.isfinite(dz[fine].float()).all()
+
+
 def test_a_teachers_own_pass_feeds_the_student():
     """top_ids and top_logp of one call are the lists of the other; a student that is the teacher has nothing to learn."""
     M, V, K = 12, 4000, 32

@@ -117,3 +117,13 @@ def test_distillation_is_zero_where_the_student_agrees():
     none = np.full((1, 3), -1)
     assert ho.distill(z, none, np.zeros((1, 3)))[0] == 0 and not ho.distill_bwd(z, none, np.zeros((1, 3)), np.ones(1)).any()
     assert abs(ho.distill(z, none, np.zeros((1, 3)), tail=True)[0]) < 1e-14
+
+
+def test_rows_without_entries_have_no_term():
+    """The loss is constant there: also with every logit masked, and (without a tail) with entries that all weigh nothing."""
+    z = np.random.default_rng(5).normal(size=(3, 9))
+    z[1] = -np.inf
+    none, zero = np.full((3, 4), -1), np.tile(np.arange(4), (3, 1))
+    for ids, t, tail in ((none, np.zeros((3, 4)), False), (none, np.zeros((3, 4)), True), (zero, np.full((3, 4), -np.inf), False)):
+        assert not ho.distill(z, ids, t, 0.7, tail).any()
+        assert not ho.distill_bwd(z, ids, t, np.ones(3), 0.7, tail).any()
