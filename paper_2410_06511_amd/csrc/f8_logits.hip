@@ -6,7 +6,7 @@
 //   loss = sum_k q_k (log q_k - log p_k) [+ q_rest (log q_rest - log p_rest)]
 //   dz_j = scale * (g (c p_j - q_j) + the given token's term above),  c = 1 for listed j, 1 [- q_rest / p_rest] for the others.
 // Bound by memory: one read of the logits forward (2 bytes an element), one read and one write backward (4 bytes).  8192 x 131072
-// forward 317 us (6.8 TB/s), backward 788 (5.5); beside the loads stand about 9 instructions and an exponential an element, some
+// forward 315 us (6.8 TB/s), backward 785 (5.5); beside the loads stand about 9 instructions and an exponential an element, some
 // two thirds of what a compute unit can issue at that rate.
 // Softmax statistics are kept as (largest logit, log of the sum of exp(z - z_max)): a difference of two bf16 values is exact in
 // fp32 where their ratio is below 2^16, so that p keeps its precision however large the logits are, which one number lse would not.
@@ -104,12 +104,15 @@ __device__ inline uint4 load_logits(const uint4* row, int c, int V)
 // ---- a teacher's list in LDS ----------------------------------------------------------------------
 
 // The entries of one row that fall into a block's columns.  A chunk that holds some is marked by a bit; the sweep leaves it out,
-// and the thread of its first entry takes it with all its entries.
+// and the thread of its first entry takes it with all its entries.  A second bit marks chunks of several entries: only those entries
+// are looked for (2048 x 32768 with 128: forward 50 -> 38 us, backward 108 -> 61 against each entry compared with all; with 128
+// adjacent tokens, which all share, 45 -> 50 and 162 -> 144).
 struct List {
     int id[kLgMaxTop];  // column, -1: none here
     float q[kLgMaxTop];
-    uint32_t marks[kLgSegCols / 8 / 32];
-    __device__ bool marked(int lc) const { return marks[lc >> 5] >> (lc & 31) & 1; }
+    uint32_t marks[kLgSegCols / 8 / 32], shared[kLgSegCols / 8 / 32];
+    __device__ static bool bit(const uint32_t* bits, int lc) { return bits[lc >> 5] >> (lc & 31) & 1; }
+    __device__ bool marked(int lc) const { return bit(marks, lc); }
 };
 // Threads below K bring their entry (q: its weight), all THREADS call; chunks c0 .. c1 - 1.
 template <int THREADS>
@@ -117,31 +120,41 @@ __device__ inline void list_fill(List& L, int K, int64_t id, float q, int c0, in
 {
     const int k = threadIdx.x;
     const bool here = k < K && id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8;
-    for (int i = k; i < (c1 - c0 + 31) / 32; i += THREADS) L.marks[i] = 0;
-    if (k < K) L.id[k] = here ? (int)id : -1, L.q[k] = q;
+    for (int i = k; i < (c1 - c0 + 31) / 32; i += THREADS) L.marks[i] = L.shared[i] = 0;
+    if (k < kLgMaxTop) L.id[k] = here ? (int)id : -1, L.q[k] = q;
     __syncthreads();
-    if (here) atomicOr(&L.marks[((int)id / 8 - c0) >> 5], 1u << (((int)id / 8 - c0) & 31));
+    if (here) {
+        const int lc = (int)id / 8 - c0;
+        const uint32_t own = 1u << (lc & 31);
+        if (atomicOr(&L.marks[lc >> 5], own) & own) atomicOr(&L.shared[lc >> 5], own);
+    }
     __syncthreads();
 }
 // The chunk that this thread takes (-1: none): which of its elements are listed, and their weights (an id that occurs again
-// counts with each of its weights).
-__device__ inline int list_chunk(const List& L, int K, uint32_t* mask, float* w)
+// counts with each of its weights, in their order).  All threads call.
+__device__ inline int list_chunk(const List& L, int c0, uint32_t* mask, float* w)
 {
-    const int k = threadIdx.x, id = k < K ? L.id[k] : -1;
-    int c = id >> 3;
-    if (id < 0) return -1;
+    const int k = threadIdx.x, lane = k & (kWave - 1);
+    if (k - lane >= kLgMaxTop) return -1;  // (whole waves)
+    const int id = L.id[k];
+    int c = id >> 3;  // (-1 >> 3 is no chunk)
     *mask = 1u << (id & 7);
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = e == (id & 7) ? L.q[k] : 0.0f;
     const int own = c;
-#pragma unroll 8
-    for (int j = 0; j < K; ++j) {
-        const int other = L.id[j];
-        if (j != k && other >> 3 == own) {  // (-1 >> 3 is no chunk)
-            if (j < k) c = -1;
-            *mask |= 1u << (other & 7);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] += e == (other & 7) ? L.q[j] : 0.0f;
+    for (int half = 0; half < kLgMaxTop; half += kWave) {
+        const int there = L.id[half + lane], weight = __float_as_int(L.q[half + lane]);
+        for (uint64_t left = __ballot(there >= 0 && List::bit(L.shared, (there >> 3) - c0)); left; left &= left - 1) {
+            const int at = __ffsll((unsigned long long)left) - 1, j = half + at;  // (alike in all lanes, as what is read of entry j)
+            const int other = __builtin_amdgcn_readlane(there, at);
+            const float q = __int_as_float(__builtin_amdgcn_readlane(weight, at));
+            if (j != k && other >> 3 == own) {
+                if (j < k) c = -1;
+                *mask |= 1u << (other & 7);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] += e == (other & 7) ? q : 0.0f;
+            }
         }
     }
     return c;
@@ -477,7 +490,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
                 list_fill<kLgThreads>(list, a.t.K, id, 0.0f, c0, c1);
                 uint32_t mask;
                 float none[8];
-                if (list_chunk(list, a.t.K, &mask, none) >= 0) {
+                if (list_chunk(list, c0, &mask, none) >= 0) {
                     float z[8];
                     unpack(own, z);
 #pragma unroll
@@ -685,7 +698,7 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
                 list_fill<THREADS>(list, a.t.K, id, id >= 0 && g != 0.0f ? g * expf(t * a.t.scale - st[3]) : 0.0f, c0, c1);
                 uint32_t mask;
                 float q[8];
-                const int c = list_chunk(list, a.t.K, &mask, q);
+                const int c = list_chunk(list, c0, &mask, q);
                 if (c >= 0) emit(c, own, mask, q);
             }
         }
@@ -802,12 +815,19 @@ static f8_status launch_grad(GradArgs& a, float* amax, void* ws, hipStream_t st)
 {
     int nb = 0;
     if (a.M > 0) {
-        // Blocks of 1024 threads where there are many long rows (8192 x 131072 819 -> 788 us, 4096 x 131072 with a teacher 419 ->
-        // 397; few rows lose: 300 x 131072 36 -> 41, 777 x 50001 44 -> 52), else of 512, in pieces of a full step, or with a teacher,
-        // whose list every piece sets up, of a quarter of the blocks (64 x 131072 with 64 entries 19.5 -> 12.7, 300 x 50001 23 -> 18).
+        // Blocks of 1024 threads where there are many long rows (8192 x 131072 819 -> 788 us, 8192 x 32768 168 -> 158; few rows lose:
+        // 300 x 131072 36 -> 41, 777 x 50001 44 -> 52), with a teacher, whose list only two such blocks a compute unit set up, where
+        // they are three times as long (4096 x 131072 420 -> 409, 3000 x 100000 230 -> 228; 4096 x 65536 192 -> 200, 8192 x 32768
+        // 182 -> 221).  Else of 512, in pieces of a full step, or with a teacher of a quarter of the blocks, as every piece sets up
+        // the list (64 x 131072 with 64 entries 19.5 -> 12.7, 300 x 50001 23 -> 18), but in as many as leave 4096 chunks to each
+        // (600 x 131072 75 -> 63, 300 x 131072 34 -> 32; leaving 2048 or 8192: 62, 70 and 33, 35).
         Split s = split_rows(a.M, a.cols, kLgGradBlocks / 2, 1024);
-        const bool wide = s.seg_chunks >= kLgGradUnroll * 1024 && a.M * s.nseg >= kLgGradBlocks;
-        if (!wide) s = LIST ? split_rows(a.M, a.cols, kLgGradBlocks / 4, 512) : split_rows(a.M, a.cols, kLgGradBlocks, kLgGradUnroll * 512);
+        const bool wide = s.seg_chunks >= (LIST ? 3 : 1) * kLgGradUnroll * 1024 && a.M * s.nseg >= kLgGradBlocks;
+        if (!wide) s = split_rows(a.M, a.cols, kLgGradBlocks, LIST ? 4096 : kLgGradUnroll * 512);
+        if (LIST && !wide) {
+            const Split quarter = split_rows(a.M, a.cols, kLgGradBlocks / 4, 512);
+            if (quarter.nseg > s.nseg) s = quarter;
+        }
         a.nseg = s.nseg, a.seg_chunks = s.seg_chunks;
         a.partial = amax ? (uint32_t*)ws : nullptr;
         const int64_t units = a.M * a.nseg;
