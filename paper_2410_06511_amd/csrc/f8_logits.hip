@@ -103,61 +103,80 @@ __device__ inline uint4 load_logits(const uint4* row, int c, int V)
 
 // ---- a teacher's list in LDS ----------------------------------------------------------------------
 
-// The entries of one row that fall into a block's columns.  A chunk that holds some is marked by a bit; the sweep leaves it out,
-// and the thread of its first entry takes it with all its entries.  A second bit marks chunks of several entries: only those entries
-// are looked for (2048 x 32768 with 128: forward 50 -> 38 us, backward 108 -> 61 against each entry compared with all; with 128
-// adjacent tokens, which all share, 45 -> 50 and 162 -> 144).
+// The entries of one row that fall into a block's columns.  A chunk that holds some has a slot, the number of one of them; there its
+// entries leave which elements they are and their weights.  The sweep leaves these chunks out, and the thread whose entry is the
+// first element takes it: the same one whichever entry gave the slot its number, so that sums keep their order.
+// (2048 x 32768 with 128 entries: forward 38 us, backward 53; adjacent tokens 32 and 47, 45 and 162 with a search among all entries.)
+constexpr uint8_t kNoSlot = 0xFF;
+template <bool WEIGHTS>
 struct List {
-    int id[kLgMaxTop];  // column, -1: none here
-    float q[kLgMaxTop];
-    uint32_t marks[kLgSegCols / 8 / 32], shared[kLgSegCols / 8 / 32];
-    __device__ static bool bit(const uint32_t* bits, int lc) { return bits[lc >> 5] >> (lc & 31) & 1; }
-    __device__ bool marked(int lc) const { return bit(marks, lc); }
+    alignas(16) uint8_t slot[kLgSegCols / 8];
+    alignas(16) float w[WEIGHTS ? kLgMaxTop : 1][8];  // by slot and element
+    uint32_t mask[kLgMaxTop];                         // by slot
+    int id[kLgMaxTop];                                // column, -1: none here
+    float q[WEIGHTS ? kLgMaxTop : 1];
+    uint32_t again;  // an id occurs twice
+    __device__ bool marked(int lc) const { return slot[lc] != kNoSlot; }
 };
+static_assert(kLgMaxTop <= kNoSlot, "entries are numbered in a byte");
 // Threads below K bring their entry (q: its weight), all THREADS call; chunks c0 .. c1 - 1.
-template <int THREADS>
-__device__ inline void list_fill(List& L, int K, int64_t id, float q, int c0, int c1)
+template <int THREADS, bool WEIGHTS>
+__device__ inline void list_fill(List<WEIGHTS>& L, int K, int64_t id, float q, int c0, int c1)
 {
     const int k = threadIdx.x;
     const bool here = k < K && id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8;
-    for (int i = k; i < (c1 - c0 + 31) / 32; i += THREADS) L.marks[i] = L.shared[i] = 0;
-    if (k < kLgMaxTop) L.id[k] = here ? (int)id : -1, L.q[k] = q;
+    const int lc = here ? (int)(id >> 3) - c0 : 0, e = (int)(id & 7);
+    for (int i = k; i < (c1 - c0 + 15) / 16; i += THREADS) reinterpret_cast<uint4*>(L.slot)[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+    if (k < kLgMaxTop) {
+        L.id[k] = here ? (int)id : -1, L.mask[k] = 0;
+        if constexpr (WEIGHTS) {
+            L.q[k] = q;
+            reinterpret_cast<float4*>(L.w[k])[0] = reinterpret_cast<float4*>(L.w[k])[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+    }
+    if (k == 0) L.again = 0;
+    __syncthreads();
+    if (here) L.slot[lc] = (uint8_t)k;  // (one of the chunk's entries stays)
     __syncthreads();
     if (here) {
-        const int lc = (int)id / 8 - c0;
-        const uint32_t own = 1u << (lc & 31);
-        if (atomicOr(&L.marks[lc >> 5], own) & own) atomicOr(&L.shared[lc >> 5], own);
+        const int s = L.slot[lc];
+        if (atomicOr(&L.mask[s], 1u << e) >> e & 1) L.again = 1;
+        else if constexpr (WEIGHTS) L.w[s][e] = q;
     }
     __syncthreads();
 }
 // The chunk that this thread takes (-1: none): which of its elements are listed, and their weights (an id that occurs again
-// counts with each of its weights, in their order).  All threads call.
-__device__ inline int list_chunk(const List& L, int c0, uint32_t* mask, float* w)
+// counts with each of its weights, in their order).
+template <bool WEIGHTS>
+__device__ inline int list_chunk(const List<WEIGHTS>& L, int K, int c0, uint32_t* mask, float* w)
 {
-    const int k = threadIdx.x, lane = k & (kWave - 1);
-    if (k - lane >= kLgMaxTop) return -1;  // (whole waves)
-    const int id = L.id[k];
-    int c = id >> 3;  // (-1 >> 3 is no chunk)
-    *mask = 1u << (id & 7);
+    const int k = threadIdx.x, id = k < K ? L.id[k] : -1;
+    if (id < 0) return -1;
+    const int s = L.slot[(id >> 3) - c0];
+    *mask = L.mask[s];
+    bool first = (id & 7) == __ffs(*mask) - 1;
+    if constexpr (WEIGHTS) {
+        const float4 a = reinterpret_cast<const float4*>(L.w[s])[0], b = reinterpret_cast<const float4*>(L.w[s])[1];
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+    if (L.again) {
+        if constexpr (WEIGHTS) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = e == (id & 7) ? L.q[k] : 0.0f;
-    const int own = c;
+            for (int e = 0; e < 8; ++e) w[e] = 0.0f;
+        }
+#pragma unroll 8
+        for (int j = 0; j < K; ++j) {
+            const int other = L.id[j];
+            if (other == id && j < k) first = false;
+            if constexpr (WEIGHTS) {
+                if (other >> 3 == id >> 3) {
 #pragma unroll
-    for (int half = 0; half < kLgMaxTop; half += kWave) {
-        const int there = L.id[half + lane], weight = __float_as_int(L.q[half + lane]);
-        for (uint64_t left = __ballot(there >= 0 && List::bit(L.shared, (there >> 3) - c0)); left; left &= left - 1) {
-            const int at = __ffsll((unsigned long long)left) - 1, j = half + at;  // (alike in all lanes, as what is read of entry j)
-            const int other = __builtin_amdgcn_readlane(there, at);
-            const float q = __int_as_float(__builtin_amdgcn_readlane(weight, at));
-            if (j != k && other >> 3 == own) {
-                if (j < k) c = -1;
-                *mask |= 1u << (other & 7);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] += e == (other & 7) ? q : 0.0f;
+                    for (int e = 0; e < 8; ++e) w[e] += e == (other & 7) ? L.q[j] : 0.0f;
+                }
             }
         }
     }
-    return c;
+    return first ? id >> 3 : -1;
 }
 
 // ---- forward ---------------------------------------------------------------------------------------
@@ -455,14 +474,15 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
     rank_keys<kLgThreads>(S.cand, n, K, emit);
 }
 
-// One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.
-template <bool ENT, bool TOP, bool LIST, bool ONCE>
+// One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.  LIST: with a teacher, TAIL: whose
+// remainder is a class of its own, so that the sums inside and outside the list are apart.
+template <bool ENT, bool TOP, bool LIST, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs a)
 {
     extern __shared__ uint16_t smax[];
     __shared__ Stat wave_stat[kLgWaves];
     __shared__ std::conditional_t<TOP, Select, int> sel;
-    __shared__ std::conditional_t<LIST, List, int> list;
+    __shared__ std::conditional_t<TAIL, List<false>, int> list;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int chunks = (a.V + 7) / 8;
     const float c2 = a.scale * kLog2e;
@@ -480,37 +500,33 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
             for (int u = 0; u < kLgUnroll; ++u)
                 w[u] = c + u * kLgThreads < c1 ? load_logits<ONCE>(row, c + u * kLgThreads, a.V) : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
         };
-        const bool marks = LIST && a.t.tail;
-        if constexpr (LIST) {
-            if (marks) {
-                const int64_t id = tid < a.t.K ? a.t.ids[rowi * a.t.K + tid] : -1;
-                uint4 own = make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
-                if (id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8) own = load_logits<false>(row, (int)(id >> 3), a.V);
-                request(c0 + tid);
-                list_fill<kLgThreads>(list, a.t.K, id, 0.0f, c0, c1);
-                uint32_t mask;
-                float none[8];
-                if (list_chunk(list, c0, &mask, none) >= 0) {
-                    float z[8];
-                    unpack(own, z);
+        if constexpr (TAIL) {
+            const int64_t id = tid < a.t.K ? a.t.ids[rowi * a.t.K + tid] : -1;
+            uint4 own = make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+            if (id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8) own = load_logits<false>(row, (int)(id >> 3), a.V);
+            request(c0 + tid);
+            list_fill<kLgThreads>(list, a.t.K, id, 0.0f, c0, c1);
+            uint32_t mask;
+            if (list_chunk(list, a.t.K, c0, &mask, nullptr) >= 0) {
+                float z[8];
+                unpack(own, z);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v.m = fmaxf(v.m, z[j]);
+                for (int j = 0; j < 8; ++j) v.m = fmaxf(v.m, z[j]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float e = exp2_hw((z[j] - v.m) * c2);
-                        (mask >> j & 1 ? v.d : v.s) += e;
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const float e = exp2_hw((z[j] - v.m) * c2);
+                    (mask >> j & 1 ? v.d : v.s) += e;
                 }
             }
         }
         for (int c = c0 + tid, step = 0; c < c1; c += kLgUnroll * kLgThreads, ++step) {
-            if (!marks || step > 0) request(c);
+            if (!TAIL || step > 0) request(c);
             float z[kLgUnroll][8], m = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kLgUnroll; ++u) {
                 unpack(w[u], z[u]);
-                if constexpr (LIST)
-                    if (marks && c + u * kLgThreads < c1 && list.marked(c + u * kLgThreads - c0)) {
+                if constexpr (TAIL)
+                    if (c + u * kLgThreads < c1 && list.marked(c + u * kLgThreads - c0)) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) z[u][j] = -INFINITY;
                     }
@@ -624,7 +640,7 @@ template <int THREADS, bool ENT, bool LIST, bool ONCE>
 __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
 {
     __shared__ uint32_t red[THREADS / kWave];
-    __shared__ std::conditional_t<LIST, List, int> list;
+    __shared__ std::conditional_t<LIST, List<true>, int> list;
     const int tid = threadIdx.x;
     const int chunks = a.cols / 8, read = (a.V + 7) / 8;
     const float c2 = a.scale * kLog2e;
@@ -698,7 +714,7 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
                 list_fill<THREADS>(list, a.t.K, id, id >= 0 && g != 0.0f ? g * expf(t * a.t.scale - st[3]) : 0.0f, c0, c1);
                 uint32_t mask;
                 float q[8];
-                const int c = list_chunk(list, c0, &mask, q);
+                const int c = list_chunk(list, a.t.K, c0, &mask, q);
                 if (c >= 0) emit(c, own, mask, q);
             }
         }
@@ -794,12 +810,13 @@ static f8_status launch_stats(StatArgs& a, void* ws, size_t ws_bytes, hipStream_
     constexpr int kStep = kLgUnroll * kLgThreads;
     const size_t lds = a.top ? (size_t)(a.seg_chunks + kStep - 1) / kStep * kLgThreads * sizeof(uint16_t) : 0;
     if constexpr (LIST) {
-        const auto kernel = once ? logits_stat_kernel<false, false, true, true> : logits_stat_kernel<false, false, true, false>;
+        const auto kernel = a.t.tail ? (once ? logits_stat_kernel<false, false, true, true, true> : logits_stat_kernel<false, false, true, true, false>)
+                                     : (once ? logits_stat_kernel<false, false, true, false, true> : logits_stat_kernel<false, false, true, false, false>);
         kernel<<<blocks, kLgThreads, lds, st>>>(a);
     } else {
-        const auto kernel = a.top ? (a.entropy ? logits_stat_kernel<true, true, false, false> : logits_stat_kernel<false, true, false, false>)
-                            : once ? (a.entropy ? logits_stat_kernel<true, false, false, true> : logits_stat_kernel<false, false, false, true>)
-                                   : (a.entropy ? logits_stat_kernel<true, false, false, false> : logits_stat_kernel<false, false, false, false>);
+        const auto kernel = a.top ? (a.entropy ? logits_stat_kernel<true, true, false, false, false> : logits_stat_kernel<false, true, false, false, false>)
+                            : once ? (a.entropy ? logits_stat_kernel<true, false, false, false, true> : logits_stat_kernel<false, false, false, false, true>)
+                                   : (a.entropy ? logits_stat_kernel<true, false, false, false, false> : logits_stat_kernel<false, false, false, false, false>);
         kernel<<<blocks, kLgThreads, lds, st>>>(a);
     }
     if (a.nseg > 1) {

@@ -390,6 +390,30 @@ def test_distill_against_the_oracle(M, V, K, tail):
             assert (np.abs(f64(r["logp"]) - f64(lone["logp"])) <= 4 * dl + 12 * U * np.abs(f64(lone["logp"]))).all()
 
 
+@pytest.mark.parametrize("M,V,K", [(6, 1000, 100), (6, 40001, 128), (520, 2001, 128)])
+@pytest.mark.parametrize("tail", (False, True))
+def test_lists_of_adjacent_and_repeated_tokens(M, V, K, tail):
+    """Entries that share their chunk with others: adjacent tokens in any order, across the ends of chunks and pieces of a row; an
+    id three times, of which two in one half of the list."""
+    g = np.random.default_rng(V)
+    z = make_logits(M, V, K)
+    zw = wide(z)[:, :V]
+    at = np.linspace(0, V - K, M).astype(int)
+    ids = np.stack([a + g.permutation(K) for a in at]).astype(np.int64)
+    ids[1::2, 5], ids[1::2, K - 1] = ids[1::2, 2], ids[1::2, 2]
+    t = np.log(g.dirichlet(np.ones(K), size=M) * 0.8 + 1e-6).astype(np.float32)
+    d_loss = g.normal(size=M).astype(np.float32)
+    di, dt, dv = torch.from_numpy(ids).cuda(), torch.from_numpy(t).cuda(), torch.from_numpy(d_loss).cuda()
+    r = distill_forward(z, V, di, dt, 0.7, tail, 1.0)
+    dz, am = distill_backward(z, V, di, dt, r, dv, 0.7, tail, 1.0)
+    torch.cuda.synchronize()
+    check_distill(zw, ids, t, r, dz, am, 0.7, tail, 1.0, d_loss.astype(np.float64), None, None)
+    for _ in range(5):
+        r2 = distill_forward(z, V, di, dt, 0.7, tail, 1.0)
+        dz2, am2 = distill_backward(z, V, di, dt, r2, dv, 0.7, tail, 1.0)
+        assert torch.equal(r["loss"], r2["loss"]) and torch.equal(r["stats"], r2["stats"]) and torch.equal(dz, dz2) and torch.equal(am, am2)
+
+
 @pytest.mark.parametrize("M", (4, 560))
 def test_distill_masked_students_and_lists(M):
     """A student row with nothing left; listed tokens that the student masks; the whole vocabulary listed; ids beyond it."""
