@@ -436,6 +436,7 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
                     }
         __syncthreads();
         n = S.ncand;
+        __syncthreads();  // (every wave has the count before the first adds to it: the way on is one for the whole block)
         if (n <= kLgCandidates - kPiece) {
             for (int c = c0; c < c1 && n < (uint32_t)K; c += kWave) {
                 if (tid < kWave && c + tid < c1) each_element(row, c + tid, V, [&](uint32_t o, uint32_t col) { if (o == bound) put(o, col); });

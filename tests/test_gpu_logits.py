@@ -559,3 +559,25 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert all(torch.equal(a[n], b[n]) for n in ("stats", "entropy", "top_ids", "top_logp"))
+
+
+@pytest.mark.parametrize("V,copies", [(2051, 700), (20003, 600), (60000, 2), (131072, 520)])
+def test_equals_beyond_the_room_of_the_selection(V, copies):
+    """Rows with more elements at the selection's bound than it has room for, which are then taken from the row's front while the
+    block counts them: every wave has to see the same count.  Each copy of a row (a block each, or a row of several blocks) takes
+    the same columns, in every pass."""
+    k = 128
+    at = np.arange(V)
+    g = np.random.default_rng(V)
+    above = g.permutation(V)
+    rows = np.stack([np.zeros(V), np.where(at % 2 == 0, 1.0, -1.0), np.floor(g.random(V) * 3), np.where(at < V - 1500, -np.inf, 2.0),
+                     *(np.where(np.isin(at, above[:n]), 4.0 + at % 5, 1.0) for n in (1, 64, 127))])
+    n = len(rows)
+    z = torch.full((n * copies, (V + 15) // 16 * 16), float("nan"), dtype=torch.bfloat16, device="cuda")
+    z[:, :V] = torch.from_numpy(rows.astype(np.float32)).to(torch.bfloat16).cuda().repeat_interleave(copies, dim=0)
+    want = torch.from_numpy(np.stack([np.argsort(-wide(z[i * copies:i * copies + 1])[0, :V], kind="stable")[:k] for i in range(n)])).cuda()
+    for _ in range(4):
+        r = forward(z, V, 1.0, None, k, entropy=False)
+        torch.cuda.synchronize()
+        assert torch.equal(r["top_ids"], want.repeat_interleave(copies, dim=0))
+        assert torch.equal(r["top_logp"], r["top_logp"][::copies].repeat_interleave(copies, dim=0))
