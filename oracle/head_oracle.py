@@ -118,9 +118,15 @@ def _has_term(ids, cols, tail):
     return (ids >= 0).any() if tail else len(cols) > 0
 
 
-def _rest(listed, p, q):
-    q_rest = 1.0 - q.sum()
-    return (0.0 if q_rest < 2.0 ** -20 else q_rest), p[~listed].sum()
+def _rest(listed, lp, q):
+    """(q_rest, log p_rest, softmax outside the list): from the logs, so that a rest far below the list keeps its value"""
+    q_rest, rest = 1.0 - q.sum(), lp[~listed]
+    q_rest = 0.0 if q_rest < 2.0 ** -20 else q_rest
+    top = rest.max() if rest.size else -np.inf
+    if top == -np.inf:
+        return q_rest, -np.inf, np.zeros_like(rest)
+    e = np.exp(rest - top)
+    return q_rest, top + np.log(e.sum()), e / e.sum()
 
 
 def distill(z, ids, t, scale=1.0, tail=False, teacher_scale=1.0):
@@ -136,9 +142,9 @@ def distill(z, ids, t, scale=1.0, tail=False, teacher_scale=1.0):
         if tail:
             listed = np.zeros(V, dtype=bool)
             listed[ids[r][ids[r] >= 0]] = True
-            q_rest, p_rest = _rest(listed, p, q)
+            q_rest, log_rest, _ = _rest(listed, lp, q)
             if q_rest > 0:
-                loss[r] += q_rest * (np.log(q_rest) - (np.log(p_rest) if p_rest > 0 else -np.inf))
+                loss[r] += q_rest * (np.log(q_rest) - log_rest)
     return loss
 
 
@@ -146,18 +152,17 @@ def distill_bwd(z, ids, t, d_loss, scale=1.0, tail=False, teacher_scale=1.0, tar
     M, V = z.shape
     dz = np.zeros((M, V))
     for r in range(M):
-        m, _, _, p = _softmax_row(z[r], scale)
+        m, _, lp, p = _softmax_row(z[r], scale)
         if m == -np.inf:
             continue
         cols, q = _teacher_row(ids[r], t[r], tail, teacher_scale)
         listed = np.zeros(V, dtype=bool)
         listed[ids[r][ids[r] >= 0]] = True
-        coef = 1.0
+        row = p.copy()
         if tail:
-            q_rest, p_rest = _rest(listed, p, q)
-            coef = 1.0 - q_rest / p_rest if p_rest > 0 else 0.0
+            q_rest, _, outside = _rest(listed, lp, q)
+            row[~listed] -= q_rest * outside
         if _has_term(ids[r], cols, tail):
-            row = np.where(listed, p, coef * p)
             np.add.at(row, cols, -q)
             dz[r] = d_loss[r] * row
         if targets is not None and targets[r] >= 0:

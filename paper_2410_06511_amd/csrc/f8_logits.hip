@@ -4,7 +4,8 @@
 //   dz_j = scale * (dlogp (1[j = t] - p_j) - dH p_j (log p_j + H))
 // and distillation from a teacher's listed entries (id_k, q_k), with p_rest, q_rest the masses outside the list:
 //   loss = sum_k q_k (log q_k - log p_k) [+ q_rest (log q_rest - log p_rest)]
-//   dz_j = scale * (g (c p_j - q_j) + the given token's term above),  c = 1 for listed j, 1 [- q_rest / p_rest] for the others.
+//   dz_j = scale * (g (p_j - q_j) + the given token's term above) [for j outside the list q_j = q_rest s_j, where s is the softmax
+//   of the logits outside the list alone].
 // Bound by memory: one read of the logits forward (2 bytes an element), one read and one write backward (4 bytes).  8192 x 131072
 // forward 315 us (6.8 TB/s), backward 785 (5.5); beside the loads stand about 9 instructions and an exponential an element, some
 // two thirds of what a compute unit can issue at that rate.
@@ -41,7 +42,7 @@ __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // ---- statistics of a softmax, joined over lanes, waves and blocks -------------------------------
 
 // m: largest logit seen (-FLT_MAX: none but -inf), s = sum e, e = exp(scale (z - m)); c = scale * log2(e);
-// d: sum e log2(e) (ENT), or a second sum of e (a teacher's listed entries).
+// d: sum e log2(e) (ENT).
 // Exponents end at kFar, where e is 0: differences of masked values (-inf, the type's lowest) would make 0 * inf.
 constexpr float kFar = -1000.0f;
 struct Stat {
@@ -52,14 +53,14 @@ template <bool ENT>
 __device__ inline Stat raised(const Stat& v, float m, float c)
 {
     const float g = fmaxf((v.m - m) * c, kFar), f = exp2_hw(g);
-    return {m, v.s * f, f * (ENT ? v.d + v.s * g : v.d)};
+    return {m, v.s * f, ENT ? f * (v.d + v.s * g) : 0.0f};
 }
 template <bool ENT>
 __device__ inline Stat join(const Stat& a, const Stat& b, float c)
 {
     const float m = fmaxf(a.m, b.m);
     const Stat x = raised<ENT>(a, m, c), y = raised<ENT>(b, m, c);
-    return {m, x.s + y.s, x.d + y.d};
+    return {m, x.s + y.s, ENT ? x.d + y.d : 0.0f};
 }
 template <bool ENT>
 __device__ inline Stat wave_join(Stat v, float c)
@@ -198,7 +199,7 @@ struct StatArgs {
     float* top_logp;
     TeacherArgs t;
     float* loss;
-    float4* part;        // per block of a shared row: (m, s, d, -)
+    float4* part;        // per block of a shared row: (m, s, d, -), or (m, s) outside and inside the list
     uint64_t* part_top;  // and its elements
 };
 
@@ -238,15 +239,19 @@ __device__ inline RowInputs row_inputs(const StatArgs& a, int64_t row)
 }
 
 // What a row's outputs are, from its statistics; called by the same whole wave.
-// With a teacher whose remainder is a class of its own v.s is the sum outside the list and v.d the list's.
+// With a teacher whose remainder is a class of its own v is of the logits outside the list and `listed` of those in it, each with its
+// own largest: the remainder's log probability and gradient are finite however far below the list its logits lie.  The backward
+// takes them as (largest outside the list, log of the sum of exponentials there over q_rest) in the row's last two numbers, the
+// second +inf where there is nothing to subtract, -inf where the row has no term.
 template <bool LIST>
-__device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInputs& in, Stat v)
+__device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInputs& in, Stat v, Stat listed)
 {
     const int lane = threadIdx.x & (kWave - 1);
     constexpr int E = RowInputs::E;
-    const float total = LIST ? v.s + v.d : v.s;
+    const Stat all = LIST && a.t.tail ? join<false>(v, listed, a.scale * kLog2e) : v;
+    const float total = all.s;
     const bool none = total == 0.0f;  // every logit is -inf
-    const float m = none ? -INFINITY : v.m, log_total = none ? -INFINITY : logf(total);
+    const float m = none ? -INFINITY : all.m, log_total = none ? -INFINITY : logf(total);
     if (lane == 0) {
         float* s = a.stats + row * (LIST ? 4 : 2);
         s[0] = m, s[1] = log_total;
@@ -279,21 +284,21 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInput
         }
         loss = wave_all(loss, [](double x, double y) { return x + y; });
         mass = wave_all(mass, [](double x, double y) { return x + y; });
-        float coef = 1.0f;
+        float coef = none ? 0.0f : 1.0f;
         if (a.t.tail) {
-            const double left = 1.0 - mass, rest = none ? 0.0 : (double)v.s / total;
+            const double left = 1.0 - mass;
             const float q_rest = left < kNoRest ? 0.0f : (float)left;  // (a NaN stays)
-            coef = rest == 0.0 ? 0.0f : (float)(1.0 - (double)q_rest / rest);
-            if (q_rest != 0.0f) loss += (double)q_rest * (logf(q_rest) - logf((float)rest));
-            if (mass != mass) coef = NAN;
+            const bool rest = v.s != 0.0f;
+            const double log_rest = rest ? logf((float)((double)v.s / total)) + ((double)v.m - m) * a.scale : -INFINITY;
+            if (q_rest != 0.0f) loss += (double)q_rest * (logf(q_rest) - log_rest);
+            coef = v.m, norm = mass != mass ? NAN : rest && q_rest != 0.0f ? logf((float)((double)v.s / q_rest)) : INFINITY;
         }
-        if (none) coef = 0.0f;
         // without entries (or weights to share out) there is no term, whatever the logits: marked for the backward by norm = -inf
         bool some = false;
 #pragma unroll
         for (int e = 0; e < E; ++e) some |= in.has[e];
         if (a.t.tail ? !__any(some) : sum == 0.0) loss = coef = 0.0f, norm = -INFINITY;
-        if (__any(in.wrong)) loss = coef = NAN, norm = 0.0f;
+        if (__any(in.wrong)) loss = coef = NAN, norm = a.t.tail ? NAN : 0.0f;
         if (lane == 0) {
             a.loss[row] = (float)loss;
             a.stats[row * 4 + 2] = coef, a.stats[row * 4 + 3] = norm;
@@ -476,12 +481,12 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
 }
 
 // One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.  LIST: with a teacher, TAIL: whose
-// remainder is a class of its own, so that the sums inside and outside the list are apart.
+// remainder is a class of its own, so that the statistics inside and outside the list are apart.
 template <bool ENT, bool TOP, bool LIST, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs a)
 {
     extern __shared__ uint16_t smax[];
-    __shared__ Stat wave_stat[kLgWaves];
+    __shared__ Stat wave_stat[kLgWaves], wave_listed[TAIL ? kLgWaves : 1];
     __shared__ std::conditional_t<TOP, Select, int> sel;
     __shared__ std::conditional_t<TAIL, List<false>, int> list;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         const int64_t rowi = unit / a.nseg;
         const int seg = (int)(unit - rowi * a.nseg), c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
         const uint4* row = reinterpret_cast<const uint4*>(a.logits + rowi * a.ld);
-        Stat v = {-FLT_MAX, 0.0f, 0.0f};
+        Stat v = {-FLT_MAX, 0.0f, 0.0f}, listed = v;
         uint32_t best = 0;
         RowInputs in;
         if (a.nseg == 1 && wave == kLgWaves - 1) in = row_inputs<LIST>(a, rowi);
@@ -512,11 +517,15 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
                 float z[8];
                 unpack(own, z);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v.m = fmaxf(v.m, z[j]);
+                for (int j = 0; j < 8; ++j) {
+                    const bool on = mask >> j & 1;
+                    v.m = fmaxf(v.m, on ? -FLT_MAX : z[j]), listed.m = fmaxf(listed.m, on ? z[j] : -FLT_MAX);
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float e = exp2_hw((z[j] - v.m) * c2);
-                    (mask >> j & 1 ? v.d : v.s) += e;
+                    const bool on = mask >> j & 1;
+                    const float e = exp2_hw((z[j] - (on ? listed.m : v.m)) * c2);
+                    v.s += on ? 0.0f : e, listed.s += on ? e : 0.0f;
                 }
             }
         }
@@ -551,12 +560,21 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         }
         v = wave_join<ENT>(v, c2);
         if (lane == 0) wave_stat[wave] = v;
+        if constexpr (TAIL) {
+            listed = wave_join<false>(listed, c2);
+            if (lane == 0) wave_listed[wave] = listed;
+        }
         __syncthreads();
         v = wave_stat[0];
 #pragma unroll
         for (int i = 1; i < kLgWaves; ++i) v = join<ENT>(v, wave_stat[i], c2);
+        if constexpr (TAIL) {
+            listed = wave_listed[0];
+#pragma unroll
+            for (int i = 1; i < kLgWaves; ++i) listed = join<false>(listed, wave_listed[i], c2);
+        }
         if (a.nseg > 1) {
-            if (tid == 0) a.part[unit] = make_float4(v.m, v.s, v.d, 0.0f);
+            if (tid == 0) a.part[unit] = TAIL ? make_float4(v.m, v.s, listed.m, listed.s) : make_float4(v.m, v.s, v.d, 0.0f);
         }
         if constexpr (TOP) {
             const float log_total = logf(v.s);
@@ -569,7 +587,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
                 }
             });
         }
-        if (a.nseg == 1 && wave == kLgWaves - 1) finish_row<LIST>(a, rowi, in, v);  // (while the first waves rank)
+        if (a.nseg == 1 && wave == kLgWaves - 1) finish_row<LIST>(a, rowi, in, v, listed);  // (while the first waves rank)
         __syncthreads();  // LDS is used again
     }
 }
@@ -589,16 +607,18 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
         RowInputs in;
         if (tid / kWave == kLgWaves - 1) in = row_inputs<LIST>(a, row);
         uint64_t mine[AHEAD], least = ~(uint64_t)0;
-        Stat v = {-FLT_MAX, 0.0f, 0.0f};
+        Stat v = {-FLT_MAX, 0.0f, 0.0f}, listed = v;
         if (lane < a.nseg) {
             const float4 p = a.part[row * a.nseg + lane];
             v = {p.x, p.y, p.z};
+            if (LIST && a.t.tail) listed = {p.z, p.w, 0.0f};
             // a key that K of the pieces' elements reach: the least of the pieces' (K / nseg)-th
             if (keys) least = lists[lane * a.top + (a.top + a.nseg - 1) / a.nseg - 1];
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) mine[u] = tid + u * kLgThreads < keys ? lists[tid + u * kLgThreads] : 0;
         v = wave_join<ENT>(v, c2);
+        if (LIST && a.t.tail) listed = wave_join<false>(listed, c2);
         if (keys) {
             least = wave_all(least, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
             if (tid == 0) n = 0;
@@ -617,7 +637,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_join_kernel(const StatArgs 
                 a.top_logp[row * a.top + rank] = v.s == 0.0f ? -INFINITY : (order_value((uint32_t)(key >> 32)) - v.m) * a.scale - log_total;
             });
         }
-        if (tid / kWave == kLgWaves - 1) finish_row<LIST>(a, row, in, v);  // (while the first waves rank)
+        if (tid / kWave == kLgWaves - 1) finish_row<LIST>(a, row, in, v, listed);  // (while the first waves rank)
         __syncthreads();
     }
 }
@@ -655,8 +675,8 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
         const float m = st[0], log2_total = st[1] * kLog2e;
         const int64_t target = a.targets ? a.targets[rowi] : -1;
         const float dlp = target < 0 || !a.d_logp ? 0.0f : target >= a.V ? NAN : a.d_logp[rowi] * a.scale;
-        // dz = p (A + B log2 p), + dlp at the given token; of listed entries p AL - their weight
-        float A = -dlp, B = 0.0f, AL = 0.0f;
+        // dz = w (A + B log2 w), + dlp at the given token, w = exp2((z - mw) c2 - lw) = p; of listed entries p AL - their weight
+        float A = -dlp, B = 0.0f, AL = 0.0f, mw = m, lw = log2_total;
         if constexpr (ENT) {
             const float dh = a.d_entropy[rowi] * a.scale;
             if (dh != 0.0f) A -= dh * a.entropy[rowi], B = -dh * kLn2;
@@ -664,8 +684,18 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
         float g = 0.0f;
         if constexpr (LIST) {
             g = st[3] == -INFINITY ? 0.0f : a.d_loss[rowi] * a.scale;  // (a row without entries has no term)
-            if (g != 0.0f) A += g * st[2];
             AL = g - dlp;
+            if (g != 0.0f) {
+                if (!a.t.tail) {
+                    A += g * st[2];
+                } else if (st[3] == INFINITY) {
+                    A = AL;
+                } else {  // w is the rest's weight on this element, r = p / w = p_rest / q_rest (at most 2^20)
+                    mw = st[2], lw = st[3] * kLog2e;
+                    const float r = exp2_hw(__builtin_fmaf(mw - m, c2, lw) - log2_total);
+                    A = g * (r - 1.0f) - dlp * r;
+                }
+            }
         }
         // nothing to hand back: no weight, or no logit that a change could move
         const bool zero = (A == 0.0f && B == 0.0f && dlp == 0.0f && g == 0.0f) || st[1] == -INFINITY;
@@ -675,9 +705,9 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
             unpack(w, z);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float l2 = __builtin_fmaf(z[j] - m, c2, -log2_total), p = exp2_hw(l2);
-                z[j] = ENT ? p * __builtin_fmaf(B, fmaxf(l2, kFar), A) : p * A;
-                if (LIST && q) z[j] = mask >> j & 1 ? p * AL - q[j] : z[j];
+                const bool on = LIST && q && (mask >> j & 1);
+                const float l2 = __builtin_fmaf(z[j] - (on ? m : mw), c2, -(on ? log2_total : lw)), w = exp2_hw(l2);
+                z[j] = ENT ? w * __builtin_fmaf(B, fmaxf(l2, kFar), A) : on ? w * AL - q[j] : w * A;
             }
             if (cu == (int)(target >> 3)) {
 #pragma unroll
@@ -712,7 +742,8 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
                     if (id >= (int64_t)c0 * 8 && id < (int64_t)c1 * 8) own = load_logits<false>(row, (int)(id >> 3), a.V);
                 }
                 request(c0 + tid);
-                list_fill<THREADS>(list, a.t.K, id, id >= 0 && g != 0.0f ? g * expf(t * a.t.scale - st[3]) : 0.0f, c0, c1);
+                const float norm = a.t.tail ? 0.0f : st[3];
+                list_fill<THREADS>(list, a.t.K, id, id >= 0 && g != 0.0f ? g * expf(t * a.t.scale - norm) : 0.0f, c0, c1);
                 uint32_t mask;
                 float q[8];
                 const int c = list_chunk(list, a.t.K, c0, &mask, q);

@@ -581,3 +581,77 @@ def test_equals_beyond_the_room_of_the_selection(V, copies):
         torch.cuda.synchronize()
         assert torch.equal(r["top_ids"], want.repeat_interleave(copies, dim=0))
         assert torch.equal(r["top_logp"], r["top_logp"][::copies].repeat_interleave(copies, dim=0))
+
+
+@pytest.mark.parametrize("V,copies", [(1000, 60), (9001, 60), (40001, 1), (140001, 1)])
+@pytest.mark.parametrize("scale", (1.0, 4.0))
+@pytest.mark.parametrize("weight", (1.0, 300.0))
+def test_a_rest_far_below_the_list(V, copies, scale, weight):
+    """The teacher's remainder has weight where the student puts next to nothing outside the list, or the list lies far below the
+    rest: the loss and the gradient are the definition's, however far the two are apart (one exponential of the distance is 0 in
+    fp32 from 104 nats on).  Tolerances as above, with the logits outside the list seen from their own largest: every weight there
+    is off by a factor of fw, the log of their sum by dl_rest; the distance to the list is taken in fp64 for the loss, and as the
+    weights' exponents, off by 4 u of itself, for the gradient."""
+    g = np.random.default_rng(V)
+    gaps = np.array([0.0, 80.0, 86.9, 87.4, 88.8, 103.5, 105.0, 250.0, 500.0, 1e4, -40.0, -300.0]) / scale
+    n, K = len(gaps) + 4, 24
+    ids = np.stack([np.sort(g.permutation(V)[:K]) for _ in range(n)]).astype(np.int64)
+    listed = np.zeros((n, V), dtype=bool)
+    np.put_along_axis(listed, ids, True, axis=1)
+    rows = g.normal(size=(n, V)) * 2
+    rows[:len(gaps)] -= np.where(listed[:len(gaps)], 0.0, gaps[:, None])
+    lowest, part, one, whole = range(len(gaps), n)
+    rows[lowest][~listed[lowest]] = LOWEST                                     # all of the rest masked by the lowest value
+    rows[part] -= np.where(listed[part], 0.0, 300.0)
+    rows[part][~listed[part] & (np.arange(V) % 3 != 0)] = LOWEST               # most of it
+    rows[one][~listed[one]] = -np.inf
+    rows[one][np.flatnonzero(~listed[one])[V // 2]] = -300.0                   # one left outside the list
+    rows[whole] -= np.where(listed[whole], 300.0, np.where(np.arange(V) % 2 == 0, 0.0, 300.0))
+    t = np.log(g.dirichlet(np.ones(K), size=n) * g.uniform(0.5, 0.95, size=(n, 1))).astype(np.float32)
+    z = torch.full((n, (V + 15) // 16 * 16), float("nan"), dtype=torch.bfloat16)
+    z[:, :V] = torch.from_numpy(rows.astype(np.float32)).to(torch.bfloat16)
+    zw = wide(z)[:, :V]
+    targets = np.where(np.arange(n) % 3 == 0, ids[:, 5], np.where(np.arange(n) % 3 == 1, (ids[:, 0] + 1) % V, -1))
+    d_loss, d_logp = (weight * g.normal(size=n)).astype(np.float32), g.normal(size=n).astype(np.float32)
+    again = lambda a: torch.from_numpy(np.tile(a, (copies,) + (1,) * (a.ndim - 1))).cuda()
+    zc, args = z.repeat(copies, 1).cuda(), [again(a) for a in (ids, t)]
+    tg, dv, dw = again(targets), again(d_loss), again(d_logp)
+    r = distill_forward(zc, V, *args, scale, True, 1.0, tg)
+    dz, am = distill_backward(zc, V, *args, r, dv, scale, True, 1.0, tg, dw)
+    torch.cuda.synchronize()
+    for v in (*r.values(), dz):  # every copy alike
+        assert torch.equal(v, v[:n].repeat((copies,) + (1,) * (v.dim() - 1)))
+
+    dl, fp, p, nl = errors(zw, scale)
+    ref = ho.distill(zw, ids, t.astype(np.float64), scale, True)
+    q = np.exp(t.astype(np.float64))
+    q_rest = 1 - q.sum(axis=1)
+    dq = 4 * U * (np.abs(t).max(axis=1) + 4) + 8 * U
+    dr = q.sum(axis=1) * dq + 4 * U
+    rest = np.where(listed, -np.inf, zw)
+    dl_rest, fw, w, nl_rest = errors(rest, scale)
+    logs = nl.min(axis=1) + nl_rest.min(axis=1) + np.abs(np.log(q_rest))      # magnitudes of the logs of sums and masses, together
+    apart = scale * np.abs(zw.max(axis=1) - rest.max(axis=1))
+    nlk, fk = np.take_along_axis(nl, ids, axis=1), np.take_along_axis(fp, ids, axis=1)
+    fk = np.maximum(fk, 4 * U * nlk)    # (errors() ends its exponents at 800)
+    bound = ((q * (2 * dq[:, None] * (1 + np.abs(t) + nlk) + 2 * fk + 4 * U * nlk)).sum(axis=1) + 2 * dl + 2 * dl_rest + dr * (2 + logs + apart)
+             + q_rest * 8 * U * (1 + logs) + 4 * U * np.abs(ref))
+    got = f64(r["loss"][:n])
+    with np.errstate(over="ignore"):
+        dead = ref.astype(np.float32) == np.inf   # (the lowest value, scaled)
+    assert np.array_equal(got == np.inf, dead)
+    assert (np.abs(got - ref) <= bound)[~dead].all(), (got, ref, bound)
+
+    rd = ho.distill_bwd(zw, ids, t.astype(np.float64), d_loss.astype(np.float64), scale, True, 1.0, targets, d_logp.astype(np.float64))
+    got = wide(dz[:n])
+    assert np.isfinite(got).all() and not got[:, V:].any()
+    gl, gt = np.abs(d_loss.astype(np.float64))[:, None], (np.abs(d_logp.astype(np.float64)) * (targets >= 0))[:, None]
+    qs = np.zeros((n, V))
+    np.put_along_axis(qs, ids, q, axis=1)
+    # p outside the list is its weight there times r = p_rest / q_rest, an exponential of a sum of four terms
+    fr = (4 * U * np.minimum(apart, 800) + dl + dl_rest + 8 * U * (1 + logs) + dr / q_rest)[:, None]
+    bound = HALF * np.abs(rd) + scale * np.where(listed, p * (gl + gt) * (fp + 16 * U) + gl * qs * (dq[:, None] + 8 * U),
+                                                 gl * w * q_rest[:, None] * (fw + (dr / q_rest + 8 * U * (1 + logs))[:, None]) + p * (gl + gt) * (fp + fw + fr + 16 * U))
+    bad = np.abs(got[:, :V] - rd) > bound + 1e-37 * (1 + weight)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4])
+    assert am.item() == np.abs(got).max()

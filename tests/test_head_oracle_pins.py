@@ -127,3 +127,28 @@ def test_rows_without_entries_have_no_term():
     for ids, t, tail in ((none, np.zeros((3, 4)), False), (none, np.zeros((3, 4)), True), (zero, np.full((3, 4), -np.inf), False)):
         assert not ho.distill(z, ids, t, 0.7, tail).any()
         assert not ho.distill_bwd(z, ids, t, np.ones(3), 0.7, tail).any()
+
+
+@pytest.mark.parametrize("gap", (0.0, 90.0, 2000.0, 1e30))
+def test_a_rest_far_below_the_list_keeps_its_loss_and_gradient(gap):
+    """What lies outside the list, as a class of its own, against autograd of the loss written with log sums: also where its
+    probability is below every number that fp64 has."""
+    r = rng(6)
+    z = r.normal(size=(1, 19))
+    ids, t = np.array([[3, 7, 11]]), np.log(np.array([[0.3, 0.2, 0.1]]))
+    listed = np.isin(np.arange(19), ids)
+    z[0, ~listed] -= gap
+    scale = 0.7
+    zt = torch.tensor(z[0], requires_grad=True)
+    total = torch.logsumexp(scale * zt, dim=0)
+    rest = scale * zt[torch.tensor(~listed)]
+    top = rest.max().detach()   # (torch.logsumexp's gradient is exp(rest - result), which loses log 16 of the result beside 1e30)
+    log_rest = top + (rest - top).exp().sum().log() - total
+    q = torch.tensor(np.exp(t[0]))
+    left = 1 - q.sum()
+    loss = (q * (q.log() - (scale * zt[torch.tensor(ids[0])] - total))).sum() + left * (left.log() - log_rest)
+    loss.backward()
+    assert abs(ho.distill(z, ids, t, scale, True)[0] - loss.item()) <= 1e-13 * (1 + gap)
+    dz = ho.distill_bwd(z, ids, t, np.ones(1), scale, True)[0]
+    assert np.isfinite(dz).all() and abs(dz[~listed].sum()) > (0.1 if gap else 0.0)
+    assert np.abs(dz - zt.grad.numpy()).max() <= 1e-12
