@@ -24,6 +24,11 @@ import torch
 from . import f8
 
 
+def _bf16(t):
+    """t as f8.residual_norm wants it: bf16 values that are kept in another type of 16 bits are accepted by every other call."""
+    return t if t.dtype is torch.bfloat16 else t.view(torch.bfloat16)
+
+
 class TransformerBlock:
     def __init__(self, B, S, D, H, Hq, Hkv, hd=128, eps=1e-5, theta=500000.0, grad_format=f8.E4M3, device="cuda",
                  scaling="dynamic", history_len=16, post_norm=False, gate_rows=0, branch_scale=1.0):
@@ -128,7 +133,7 @@ class TransformerBlock:
                 return [("residual 1", lambda: f8.add(x, s.yo, s.h1, stream), 0, 6 * M * D),
                         ("rmsnorm 2", lambda: f8.rmsnorm(s.h1, w["g2"], s.eps, s.hn, s.rstd2, a_hn, ws, stream), 0, 4 * M * D)]
             (p1, r1), a1 = (w["p1"], s.rstd_p1) if s.post_norm else (None, None), w["a1"] if s.gate_rows else None
-            return [("rmsnorm 2", lambda: f8.residual_norm(x, s.yo, s.h1, s.hn, p1, a1, w["g2"], 1.0, s.branch_scale, s.eps, r1, s.rstd2, a_hn, ws, stream),
+            return [("rmsnorm 2", lambda: f8.residual_norm(_bf16(x), s.yo, s.h1, s.hn, p1, a1, _bf16(w["g2"]).reshape(D), 1.0, s.branch_scale, s.eps, r1, s.rstd2, a_hn, ws, stream),
                      0, 8 * M * D)]
         if self.shaped:
             (p2, r2), a2 = (w["p2"], s.rstd_p2) if s.post_norm else (None, None), w["a2"] if s.gate_rows else None
@@ -258,7 +263,7 @@ class TransformerBlock:
                                                                    dg_post=s.dp2, dgate=s.da2, amax_dy=a_y[1], workspace=s.res_ws, stream=stream),
                     0, 6 * M * D)] + ffn
             norm_2 = ("rmsnorm 2 bwd + residual",
-                      lambda: f8.residual_norm_bwd(s.yo, s.dh1, s.dyo, h=s.h1, dh=dout, dn=s.dhn, g_post=p1, gate=a1, g_pre=w["g2"],
+                      lambda: f8.residual_norm_bwd(s.yo, s.dh1, s.dyo, h=s.h1, dh=dout, dn=s.dhn, g_post=p1, gate=a1, g_pre=_bf16(w["g2"]).reshape(D),
                                                    branch_scale=s.branch_scale, rstd_post=r1, rstd_pre=s.rstd2, dg_post=s.dp1, dgate=s.da1, dg_pre=s.dg2,
                                                    amax_dy=a_y[0], workspace=s.res_ws, stream=stream), 0, 12 * M * D)
         else:

@@ -187,3 +187,25 @@ def test_blocks_and_head_together_in_a_graph():
         values.append(loss())
     slope = (values[0] - values[1]) / (2 * h * length).item()
     assert abs(slope - length.item()) <= length.item() / 3, (slope, length.item())
+
+
+@pytest.mark.parametrize("scaling", ("dynamic", "delayed"))
+@pytest.mark.parametrize("post", (False, True))
+def test_gains_of_any_shape_and_bits_of_any_type(scaling, post):
+    """A block takes gains as [D] and as [1, D], and inputs and gains as bf16 or as its bits in another type, alike."""
+    B, S, Hq, Hkv, hd, H = 1, 128, 2, 1, 128, 512
+    D, M = Hq * hd, B * S
+    w = weights(D, H, Hq, Hkv, hd, 400, post, 0)
+    x, dout = gen((M, D), 31).cuda(), gen((M, D), 32, 1e-2).cuda()
+    results = []
+    for g, as_bits in (((D,), False), ((1, D), False), ((D, 1), False), ((D,), True)):
+        blk = TransformerBlock(B, S, D, H, Hq, Hkv, hd, EPS, scaling=scaling, post_norm=post)
+        kind = (lambda t: t.view(torch.int16)) if as_bits else (lambda t: t)
+        given = dict(w, g1=kind(w["g1"].reshape(g)), g2=kind(w["g2"].reshape(g)))
+        for _ in range(2):
+            out = blk.forward(kind(x), given).clone()
+            dx = blk.backward(kind(x), given, dout).clone()
+        torch.cuda.synchronize()
+        results.append((out, blk.h1.clone(), dx, blk.dg1, blk.dg2))
+    for r in results[1:]:
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(r, results[0]))
