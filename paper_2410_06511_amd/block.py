@@ -17,6 +17,7 @@ post_norm, gate_rows and branch_scale give blocks whose branches are normalised,
 stream:
     h1 = x + branch_scale * a1 * rmsnorm(wo ..., p1),   out = h1 + branch_scale * a2 * rmsnorm(w2 ..., p2)
 """
+import math
 from functools import cached_property
 
 import torch
@@ -33,10 +34,15 @@ class TransformerBlock:
     def __init__(self, B, S, D, H, Hq, Hkv, hd=128, eps=1e-5, theta=500000.0, grad_format=f8.E4M3, device="cuda",
                  scaling="dynamic", history_len=16, post_norm=False, gate_rows=0, branch_scale=1.0):
         """post_norm: the weights have p1, p2 [D], the gains of the norms after the two branches.  gate_rows: they have a1, a2
-        [gate_rows, D] (1: a gate per channel, B: one per sequence).  Gradients: dp1, dp2, da1, da2."""
+        [gate_rows, D] (1: a gate per channel, B: one per sequence; a divisor of B * S).  Gradients: dp1, dp2, da1, da2.  With any
+        of the three D is at most 16384."""
         assert D == Hq * hd and scaling in ("dynamic", "delayed")
         self.post_norm, self.gate_rows, self.branch_scale = post_norm, gate_rows, branch_scale
         self.shaped = bool(post_norm or gate_rows or branch_scale != 1.0)  # a branch that is more than its last product
+        if self.shaped:  # what f8.residual_norm takes
+            assert D <= 16384, f"a branch with a norm, a gate or a scale holds rows of up to 16384 elements, not {D}"
+            assert gate_rows >= 0 and (not gate_rows or B * S % gate_rows == 0), f"{gate_rows} rows of a gate do not divide {B * S} tokens"
+            assert math.isfinite(branch_scale), f"a branch's scale of {branch_scale}"
         self.delayed, self.gfmt = scaling == "delayed", grad_format
         if self.delayed:
             self.st_qkv, self.st_o, self.st_13, self.st_2 = (f8.ScalingState(f8.DELAYED, history_len, device) for _ in range(4))

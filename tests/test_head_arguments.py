@@ -131,3 +131,16 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     monkeypatch.setattr(f8, "_device", lambda: 1)
     assert f8._rows("x", Elsewhere(), (4, 64), f8._current()) == (FAKE, 64)
     assert f8._packed("x", Elsewhere(), torch.bfloat16, (4, 64), f8._current()) == FAKE
+
+
+@pytest.mark.parametrize("change,message", [
+    (dict(D=16512, Hq=129, Hkv=129, post_norm=True), "up to 16384"), (dict(D=16512, Hq=129, Hkv=129, gate_rows=1), "up to 16384"),
+    (dict(D=16512, Hq=129, Hkv=129, branch_scale=0.5), "up to 16384"), (dict(gate_rows=3), "do not divide"), (dict(gate_rows=-1), "do not divide"),
+    (dict(gate_rows=64), "do not divide"), (dict(branch_scale=INF), "scale"), (dict(branch_scale=NAN), "scale")])
+def test_a_block_refuses_branches_that_its_calls_would(change, message):
+    """At its making, before it takes memory, and not at the first call."""
+    from paper_2410_06511_amd.block import TransformerBlock
+    args = dict(B=2, S=16, D=256, H=256, Hq=2, Hkv=1)
+    args.update(change)
+    with pytest.raises(AssertionError, match=message):
+        TransformerBlock(**args)
