@@ -249,9 +249,9 @@ __global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_bwd_kernel
         for (int u = 0; u < U; ++u) {
             const int c = t + TPR * u;
             if (c >= p.dc) continue;
-            float4* o = reinterpret_cast<float4*>(out + (int64_t)c * 8);
-            o[0] = make_float4(acc[u][0], acc[u][1], acc[u][2], acc[u][3]);
-            o[1] = make_float4(acc[u][4], acc[u][5], acc[u][6], acc[u][7]);
+            float* o = out + (int64_t)c * 8;  // (a caller's dgate lies on any word)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = acc[u][j];
         }
     };
     for (int64_t unit = blockIdx.x; unit < p.units; unit += gridDim.x) {

@@ -295,3 +295,22 @@ def test_gradient_against_differences():
             down[of][at] -= 1e-5
             # h was rounded to bf16 on the GPU: 2^-8 of the terms of t in each, twice, and the result's own rounding
             assert abs((total(up) - total(down)) / 2e-5 - wide(g[name])[at]) <= 4 * HALF * scale, (name, at)
+
+
+@pytest.mark.parametrize("M,D,gates", [(12, 520, 12), (40, 4096, 2), (2600, 64, 1300), (1100, 256, 1100)])
+def test_gradients_on_any_word(M, D, gates):
+    """The fp32 results need no more than their own alignment."""
+    s = make(M, D, True, gates, True, 13)
+    r = run_forward(s, M, D, 1.0, 0.5)
+    want = run_backward(s, r, M, D, 1.0, 0.5)
+    ws = torch.empty(f8.residual_norm_bwd_workspace_bytes(M, D, gates), dtype=torch.uint8, device="cuda")
+    for at in (1, 2, 3):
+        flat = torch.full((gates * D + 2 * D + M * 2 + 8 * at + 40,), 5.0, device="cuda")
+        dgate, rest = flat[at:at + gates * D].view(gates, D), flat[at + gates * D:]
+        dg_post, dg_pre, rstds = rest[1:1 + D], rest[1 + D:1 + 2 * D], rest[1 + 2 * D:1 + 2 * D + 2 * M]
+        rstds[:M], rstds[M:] = r["rstd_post"], r["rstd_pre"]
+        f8.residual_norm_bwd(s["y"], torch.empty_like(s["y"]), None, h=r["h"], dh=s["dh"], dn=s["dn"], g_post=s["g_post"], gate=s["gate"], g_pre=s["g_pre"],
+                             branch_scale=0.5, rstd_post=rstds[:M], rstd_pre=rstds[M:], dg_post=dg_post, dgate=dgate, dg_pre=dg_pre, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(dgate, want["dgate"]) and torch.equal(dg_post, want["dg_post"]) and torch.equal(dg_pre, want["dg_pre"])
+        assert (flat[:at] == 5.0).all() and rest[0].item() == 5.0 and (rest[1 + 2 * D + 2 * M:] == 5.0).all()
