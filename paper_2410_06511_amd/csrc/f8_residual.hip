@@ -472,7 +472,7 @@ static bool bad_pitch(int64_t ld, int64_t D) { return ld < D || (ld % 8); }
 
 static f8_status check_residual(int64_t M, int64_t D, const void* gate, int64_t gate_rows, float a, float b)
 {
-    if (M < 0 || M > 0x7FFFFFFF || D < 0 || D > kResMaxD || (D % 8) || gate_rows < 0 || gate_rows * D > 0x7FFFFFFFFLL ||
+    if (M < 0 || M > 0x7FFFFFFF || D < 0 || D > kResMaxD || (D % 8) || gate_rows < 0 || gate_rows > 0x7FFFFFFF || gate_rows * D > 0x7FFFFFFFFLL ||
         (gate != nullptr) != (gate_rows > 0) || (gate_rows > 0 && M % gate_rows) || !(a - a == 0.0f) || !(b - b == 0.0f))
         return F8_ERR_SHAPE;
     return F8_OK;

@@ -144,3 +144,12 @@ def test_a_block_refuses_branches_that_its_calls_would(change, message):
     args.update(change)
     with pytest.raises(AssertionError, match=message):
         TransformerBlock(**args)
+
+
+@pytest.mark.parametrize("D,gate_rows", [(16, 1 << 60), (16, (1 << 60) + 1), (16384, 1 << 50), (8, (1 << 61) + 8), (0, (1 << 31) + 1)])
+def test_gates_whose_size_no_number_holds(D, gate_rows):
+    """Without rows every number of gate rows divides them; what the gate then takes must not be counted past 64 bits."""
+    shape = dict(M=0, D=D, gate_rows=gate_rows)
+    assert call("f8_residual_norm", FORWARD, **shape, ldx=16384, ldy=16384, ldh=16384, ldn=16384) == SHAPE
+    assert call("f8_residual_norm_bwd", BACKWARD, **shape, ldh=16384, ldy=16384, lddh=16384, lddn=16384, lddx=16384, lddy=16384) == SHAPE
+    assert f8.residual_norm_bwd_workspace_bytes(0, D, gate_rows) == 8192
