@@ -655,3 +655,75 @@ def test_a_rest_far_below_the_list(V, copies, scale, weight):
     bad = np.abs(got[:, :V] - rd) > bound + 1e-37 * (1 + weight)
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4])
     assert am.item() == np.abs(got).max()
+
+
+# ---- the kernels of large tensors -------------------------------------------------------------------
+
+def large_logits(M, V, seed):
+    torch.manual_seed(seed)
+    z = torch.full((M, (V + 15) // 16 * 16), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for rows in z.split(1024):
+        rows[:, :V] = torch.randn((len(rows), V), device="cuda") * 3
+    return z
+
+
+def parts_of(M, n=300):
+    """Calls of n rows, whose rows are cut for the forward as those of all and which load through the caches."""
+    return [slice(i, i + n) for i in range(0, M - n, n)] + [slice(M - n, M)]
+
+
+# The forward loads past the caches from 2^29 elements on; the gradient from 2^27 on, in blocks of 1024 threads where there are 2048 rows
+# or pieces of rows as long as those blocks' steps: with both, of many long rows; one of the two alone in the last two cases.
+@pytest.mark.parametrize("M,V", [(4200, 131071), (2700, 50001), (2100, 32768), (600, 262144)])
+@pytest.mark.parametrize("entropy", (False, True))
+def test_large_logits_have_the_bits_of_their_rows(M, V, entropy):
+    z = large_logits(M, V, 31)
+    targets = torch.randint(-1, V, (M,), device="cuda")
+    d_logp, d_entropy = torch.randn(M, device="cuda"), torch.randn(M, device="cuda") if entropy else None
+    r = forward(z, V, 0.8, targets, 0, entropy)
+    dz, am = backward(z, V, r, 0.8, targets, d_logp, d_entropy)
+    torch.cuda.synchronize()
+    for rows in parts_of(M):
+        at = lambda t: None if t is None else t[rows]
+        pr = forward(z[rows], V, 0.8, targets[rows], 0, entropy)
+        pz, _ = backward(z[rows], V, pr, 0.8, targets[rows], d_logp[rows], at(d_entropy))
+        torch.cuda.synchronize()
+        assert torch.equal(pz, dz[rows]) and all(v is None or torch.equal(v, r[k][rows]) for k, v in pr.items())
+    assert am.item() == max(t.float().abs().max().item() for t in dz.split(1024))
+    few = {k: v[:3] if v is not None else None for k, v in r.items()}
+    check_forward(z[:3], V, few, 0.8, targets[:3], 0)
+    zw, t = wide(z[:3])[:, :V], targets[:3].cpu().numpy()
+    wl, wh = np.abs(f64(d_logp[:3])) * (t >= 0), f64(d_entropy[:3]) if entropy else None
+    check_gradient(zw, V, dz[:3], None, ho.token_logprobs_bwd(zw, 0.8, t, f64(d_logp[:3]), wh), 0.8, wl, np.abs(wh) if entropy else None)
+    backward(z, V, r, 0.8, targets, d_logp, d_entropy, out=z)   # in place
+    torch.cuda.synchronize()
+    assert torch.equal(z, dz)
+
+
+# With a teacher blocks of 1024 threads take rows of 98304 columns and more.
+@pytest.mark.parametrize("M,V,K", [(4200, 131071, 64), (2100, 98304, 128), (2700, 50001, 100)])
+@pytest.mark.parametrize("tail", (False, True))
+def test_distill_of_large_logits_has_the_bits_of_its_rows(M, V, K, tail):
+    scale, ts = 0.7, 1.0 if tail else 1.4
+    z = large_logits(M, V, 32)
+    ids = torch.randint(0, V, (M, K), device="cuda")
+    ids[:, K // 2:] = torch.sort(torch.rand((M, V // 64), device="cuda"), dim=1).indices[:, :K - K // 2] + 17   # some close together
+    ids[::5, K - 3:], ids[1::5, 4] = -1, ids[1::5, 1]
+    t = torch.log_softmax(torch.randn((M, K), device="cuda"), dim=1) - 0.3
+    targets = torch.randint(-1, V, (M,), device="cuda")
+    d_loss, d_logp = torch.randn(M, device="cuda"), torch.randn(M, device="cuda")
+    r = distill_forward(z, V, ids, t, scale, tail, ts, targets)
+    dz, am = distill_backward(z, V, ids, t, r, d_loss, scale, tail, ts, targets, d_logp)
+    torch.cuda.synchronize()
+    for rows in parts_of(M):
+        pr = distill_forward(z[rows], V, ids[rows], t[rows], scale, tail, ts, targets[rows])
+        pz, _ = distill_backward(z[rows], V, ids[rows], t[rows], pr, d_loss[rows], scale, tail, ts, targets[rows], d_logp[rows])
+        torch.cuda.synchronize()
+        assert torch.equal(pz, dz[rows]) and all(torch.equal(v, r[k][rows]) for k, v in pr.items())
+    assert am.item() == max(x.float().abs().max().item() for x in dz.split(1024))
+    n = 6
+    check_distill(wide(z[:n])[:, :V], ids[:n].cpu().numpy(), t[:n].cpu().numpy(), {k: v[:n] for k, v in r.items()}, dz[:n],
+                  dz[:n].float().abs().max().reshape(1), scale, tail, ts, f64(d_loss[:n]), targets[:n].cpu().numpy(), f64(d_logp[:n]))
+    distill_backward(z, V, ids, t, r, d_loss, scale, tail, ts, targets, d_logp, out=z)   # in place
+    torch.cuda.synchronize()
+    assert torch.equal(z, dz)

@@ -314,3 +314,60 @@ def test_gradients_on_any_word(M, D, gates):
         torch.cuda.synchronize()
         assert torch.equal(dgate, want["dgate"]) and torch.equal(dg_post, want["dg_post"]) and torch.equal(dg_pre, want["dg_pre"])
         assert (flat[:at] == 5.0).all() and rest[0].item() == 5.0 and (rest[1 + 2 * D + 2 * M:] == 5.0).all()
+
+
+# The backward's kernels that load past the caches, from 2^25 elements on: a wave, and blocks of up to 256, 512 and 1024 threads a row.
+@pytest.mark.parametrize("D,post,gates,pre", [(512, True, 0, True), (1024, False, 1, True), (1032, True, 2, True), (2816, True, 1, True), (4096, False, 0, True),
+                                              (4096, True, 4, False), (8192, True, 8, True), (16384, False, 2, True), (16384, True, 2, True)])
+def test_large_tensors_have_the_bits_of_their_rows(D, post, gates, pre):
+    """Every row of a tensor of more than 2^25 elements has the bits that a call on a part of the rows gives it, which loads the
+    other way; the sums over all rows are those over the parts; a part of the first agrees with the oracle."""
+    M = ((1 << 25) // D // 64 + 2) * 64
+    per_gate, a, b = M // max(gates, 1), 0.75, 1.5
+    s = make(0, D, post, gates, pre, 21)
+    torch.manual_seed(D)
+    for name, std in (("x", 1.0), ("y", 0.5), ("dh", 1e-2), ("dn", 1e-2)):
+        if s[name] is not None:
+            s[name] = (torch.randn((M, D), device="cuda") * std).bfloat16()
+    r = run_forward(s, M, D, a, b)
+    g = run_backward(s, r, M, D, a, b)
+    torch.cuda.synchronize()
+
+    def rows_of(first, n):
+        part = {k: v[first:first + n] if k in ("x", "y", "dh", "dn") and v is not None else v for k, v in s.items()}
+        if gates:
+            part["gate"] = s["gate"][first // per_gate:first // per_gate + 1]
+        pr = run_forward(part, n, D, a, b)
+        pg = run_backward(part, pr, n, D, a, b)
+        torch.cuda.synchronize()
+        rows = slice(first, first + n)
+        assert all(v is None or torch.equal(v, r[k][rows]) for k, v in pr.items() if k != "amax_n")
+        assert torch.equal(pg["dx"], g["dx"][rows]) and torch.equal(pg["dy"], g["dy"][rows])
+        return part, pr, pg
+    few = rows_of(0, 40)
+    check_forward(*few[:2], a, b)
+    check_backward(*few, a, b)
+    sums = {k: torch.zeros_like(g[k], dtype=torch.float64) for k in ("dg_post", "dgate", "dg_pre") if g[k] is not None}
+    step = per_gate // 4
+    for first in range(0, M, step):
+        pg = rows_of(first, step)[2]
+        for k, v in sums.items():
+            (v[first // per_gate] if k == "dgate" else v).add_(pg[k].view(-1).double())
+    assert g["amax_dy"].item() == g["dy"].float().abs().max().item()
+    if pre:
+        assert r["amax_n"].item() == r["n"].float().abs().max().item()
+    # The terms are the same fp32 numbers on both sides: only the additions differ, each side's off by the magnitudes' sum times
+    # one rounding for each row of a block (256 or more of them), block and group.
+    adds = 2 * 2.0 ** -24 * (M / 256 + 66)
+    spread = lambda t: t.repeat_interleave(M // len(t), dim=0)
+    for k, v in sums.items():
+        if k == "dg_pre":
+            terms = s["dn"].float() * r["h"].float() * r["rstd_pre"][:, None]
+        else:  # t as dx / a, which is off by half a step of bf16
+            terms = g["dx"].float() * ((1 + HALF) * b / a) * s["y"].float()
+            if post:
+                terms *= r["rstd_post"][:, None]
+                terms *= s["g_post"].float() if k == "dgate" else 1.0
+            terms *= spread(s["gate"].float()) if gates and k == "dg_post" else 1.0
+        size = terms.abs().view(gates if k == "dgate" else 1, -1, D).sum(dim=1, dtype=torch.float64).view(v.shape)
+        assert ((g[k].double() - v).abs() <= adds * size + 1e-38).all(), k
