@@ -429,27 +429,38 @@ __global__ __launch_bounds__(kResFinalCols* kResFinalGroups) void residual_final
 // ---- host ----------------------------------------------------------------------------------------
 
 // f(upper bound of a block's threads, chunks a thread, threads): a row of dc chunks by as few waves as hold it with U chunks each
-template <class F>
-static void with_row_shape(int64_t dc, int u, F&& f)
+template <int T>
+using Threads = std::integral_constant<int, T>;
+template <class U, class F>
+static void with_block(int64_t dc, U u, F&& f)
 {
-    using std::integral_constant;
-    const int threads = (int)((dc + u * kWave - 1) / (u * kWave)) * kWave;
-    const auto bounded = [&](auto U) {
-        if (threads <= 64) f(integral_constant<int, 64>{}, U, res_threads(64));
-        else if (threads <= 256) f(integral_constant<int, 256>{}, U, threads);
-        else if (threads <= 512) f(integral_constant<int, 512>{}, U, threads);
-        else f(integral_constant<int, 1024>{}, U, threads);
-    };
-    if (u == 1) bounded(integral_constant<int, 1>{});
-    else bounded(integral_constant<int, 2>{});
+    const int threads = (int)((dc + u() * kWave - 1) / (u() * kWave)) * kWave;
+    if (threads <= 256) f(Threads<256>{}, u, threads);
+    else if (threads <= 512) f(Threads<512>{}, u, threads);
+    else f(Threads<1024>{}, u, threads);
 }
-static int fwd_chunks(int64_t dc) { return dc <= 64 ? 1 : 2; }
+using One = std::integral_constant<int, 1>;
+using Two = std::integral_constant<int, 2>;
+template <class F>
+static void with_fwd_shape(int64_t dc, F&& f)
+{
+    if (dc <= 64) f(Threads<64>{}, One{}, res_threads(64));
+    else if (dc <= 128) f(Threads<64>{}, Two{}, res_threads(64));
+    else with_block(dc, Two{}, f);
+}
 // The backward holds four rows and up to three rows of sums.  One chunk a thread leaves registers for enough waves up to 8192
 // elements (16384 x 8192 394 -> 371 us, 8192 x 2048 59 -> 50), but a row of 520 to 1024 elements is better a wave's own, without
 // barriers (8192 x 1024 45 -> 30); with a norm of the branch the two are within 6 % between 2816 and 4096 (2001 x 2816 26.9 -> 25.8,
 // 8192 x 2816 66 -> 70).  Waves hide the loads better than loads ahead of the row, which take their registers (4096 x 4096
 // 74 -> 53).
-static int bwd_chunks(int64_t dc) { return dc <= 64 || (dc > 128 && dc <= 1024) ? 1 : 2; }
+template <class F>
+static void with_bwd_shape(int64_t dc, F&& f)
+{
+    if (dc <= 64) f(Threads<64>{}, One{}, res_threads(64));
+    else if (dc <= 128) f(Threads<64>{}, Two{}, res_threads(64));
+    else if (dc <= 1024) with_block(dc, One{}, f);
+    else f(Threads<1024>{}, Two{}, (int)((dc + 2 * kWave - 1) / (2 * kWave)) * kWave);
+}
 
 // How the backward divides its rows: `parts` blocks share a group of rows with one gate row while there are fewer groups than
 // blocks, else a block takes whole groups.
@@ -459,7 +470,7 @@ struct ResidualPlan {
 };
 static ResidualPlan plan_bwd(int64_t M, int64_t D, int64_t gate_rows)
 {
-    const int64_t groups = gate_rows > 0 ? gate_rows : 1, per_gate = M / groups, slots = D / 8 <= 64 * bwd_chunks(D / 8) ? kResWaveRows : 1;  // rows that a block takes at once
+    const int64_t groups = gate_rows > 0 ? gate_rows : 1, per_gate = M / groups, slots = D / 8 <= 128 ? kResWaveRows : 1;  // rows that a block takes at once
     const int blocks = D / 8 > 512 ? kResBwdBlocks / 2 : kResBwdBlocks;
     int64_t parts = blocks / groups, most = (per_gate + slots - 1) / slots;
     if (parts > most) parts = most;
@@ -514,7 +525,7 @@ f8_status f8_residual_norm(const void* x_bf16, int64_t ldx, const void* y_bf16, 
                                 (const uint4*)g_pre_bf16, M, gate_rows > 0 ? M / gate_rows : M, (int)(D / 8), skip_scale, branch_scale, eps,
                                 1.0f / (float)D, 1.0 / (double)D, (uint16_t*)h_bf16, (uint16_t*)n_bf16, ldh, ldn, rstd_post, rstd_pre,
                                 amax_n ? (uint32_t*)workspace : nullptr};
-        with_row_shape(D / 8, fwd_chunks(D / 8), [&](auto T, auto U, int threads) {
+        with_fwd_shape(D / 8, [&](auto T, auto U, int threads) {
             constexpr int kRows = T() == kWave ? kResWaveRows : 1;
             const int64_t b = (M + kRows - 1) / kRows;
             nb = (int)(b < kResBlocks ? b : kResBlocks);
@@ -558,7 +569,7 @@ f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf
                                     plan.units, plan.parts, (int)(D / 8), skip_scale, branch_scale, 1.0f / (float)D, (uint16_t*)dx_bf16, (uint16_t*)dy_bf16,
                                     lddx, lddy, dg_pre ? sums : nullptr, dg_post ? sums + set : nullptr,
                                     dgate ? (direct ? dgate : sums + 2 * set) : nullptr, amax_dy ? maxima : nullptr};
-        with_row_shape(D / 8, bwd_chunks(D / 8), [&](auto T, auto U, int threads) {
+        with_bwd_shape(D / 8, [&](auto T, auto U, int threads) {
             const auto pick = [&](auto ONCE) {
                 constexpr bool O = ONCE();
                 return post ? (gated ? (pre ? residual_norm_bwd_kernel<T(), U(), true, true, true, O> : residual_norm_bwd_kernel<T(), U(), true, true, false, O>)

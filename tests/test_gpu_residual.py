@@ -317,8 +317,9 @@ def test_gradients_on_any_word(M, D, gates):
 
 
 # The backward's kernels that load past the caches, from 2^25 elements on: a wave, and blocks of up to 256, 512 and 1024 threads a row.
-@pytest.mark.parametrize("D,post,gates,pre", [(512, True, 0, True), (1024, False, 1, True), (1032, True, 2, True), (2816, True, 1, True), (4096, False, 0, True),
-                                              (4096, True, 4, False), (8192, True, 8, True), (16384, False, 2, True), (16384, True, 2, True)])
+@pytest.mark.parametrize("D,post,gates,pre", [(4096, False, 0, True), (8192, True, 8, True), (16384, True, 4, True)]
+                         + [(D, post, gates, pre) for D in (512, 1024, 1032, 2816, 4104, 8200) for post in (False, True) for gates in (0, 1)
+                            for pre in (False, True)])
 def test_large_tensors_have_the_bits_of_their_rows(D, post, gates, pre):
     """Every row of a tensor of more than 2^25 elements has the bits that a call on a part of the rows gives it, which loads the
     other way; the sums over all rows are those over the parts; a part of the first agrees with the oracle."""
@@ -371,3 +372,18 @@ def test_large_tensors_have_the_bits_of_their_rows(D, post, gates, pre):
             terms *= spread(s["gate"].float()) if gates and k == "dg_post" else 1.0
         size = terms.abs().view(gates if k == "dgate" else 1, -1, D).sum(dim=1, dtype=torch.float64).view(v.shape)
         assert ((g[k].double() - v).abs() <= adds * size + 1e-38).all(), k
+
+
+# a width for each shape of the kernels: rows of a wave with one and two chunks a thread, of up to 256, 512 and 1024 threads, and of two chunks again
+@pytest.mark.parametrize("D", (256, 1024, 1032, 2816, 4104, 8200))
+@pytest.mark.parametrize("gates", (0, 3))
+@pytest.mark.parametrize("post", (False, True))
+@pytest.mark.parametrize("pre", (False, True))
+def test_every_shape_with_every_form(D, post, gates, pre):
+    M, a, b = 21, 0.75, 1.5
+    s = make(M, D, post, gates, pre, D)
+    r = run_forward(s, M, D, a, b)
+    g = run_backward(s, r, M, D, a, b)
+    torch.cuda.synchronize()
+    check_forward(s, r, a, b)
+    check_backward(s, r, g, a, b)
