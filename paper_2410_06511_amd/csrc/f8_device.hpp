@@ -31,6 +31,12 @@ __host__ __device__ inline float fmax_of(int fmt) { return fmt == F8_E4M3 ? 448.
 // A 32-bit word holds two bf16; widening to fp32 is a shift / mask.
 __device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ inline void unpack8(uint4 v, float* f)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[2 * j] = bf16_lo(w[j]), f[2 * j + 1] = bf16_hi(w[j]);
+}
 
 // fp32 -> bf16 bits, round to nearest even (finite inputs; NaN stays NaN).
 __device__ inline uint32_t f32_to_bf16_bits(float f)

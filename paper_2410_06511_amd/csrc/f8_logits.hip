@@ -81,12 +81,6 @@ __device__ inline float order_value(uint32_t o) { return __uint_as_float((o & 0x
 __device__ inline uint64_t element_key(uint32_t o, uint32_t col) { return (uint64_t)o << 32 | (uint32_t)~col; }
 __device__ inline uint32_t key_column(uint64_t k) { return ~(uint32_t)k; }
 
-__device__ inline void unpack(uint4 v, float* z)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) z[2 * j] = bf16_lo(w[j]), z[2 * j + 1] = bf16_hi(w[j]);
-}
 // chunk c of a row; columns from V on read as -inf
 template <bool ONCE>
 __device__ inline uint4 load_logits(const uint4* row, int c, int V)
@@ -515,7 +509,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
             uint32_t mask;
             if (list_chunk(list, a.t.K, c0, &mask, nullptr) >= 0) {
                 float z[8];
-                unpack(own, z);
+                unpack8(own, z);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const bool on = mask >> j & 1;
@@ -534,7 +528,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
             float z[kLgUnroll][8], m = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kLgUnroll; ++u) {
-                unpack(w[u], z[u]);
+                unpack8(w[u], z[u]);
                 if constexpr (TAIL)
                     if (c + u * kLgThreads < c1 && list.marked(c + u * kLgThreads - c0)) {
 #pragma unroll
@@ -702,7 +696,7 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
         // chunk cu of the row, with the listed ones among its elements
         auto emit = [&](int cu, uint4 w, uint32_t mask, const float* q) {
             float z[8];
-            unpack(w, z);
+            unpack8(w, z);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool on = LIST && q && (mask >> j & 1);

@@ -44,12 +44,6 @@ struct ResidualArgs {
 constexpr int kResWaveRows = 4;
 constexpr int res_threads(int THREADS) { return THREADS == kWave ? kWave * kResWaveRows : THREADS; }
 
-__device__ inline void unpack8(uint4 v, float* f)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[2 * j] = bf16_lo(w[j]), f[2 * j + 1] = bf16_hi(w[j]);
-}
 __device__ inline uint4 pack8(const float* f)
 {
     return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
