@@ -36,6 +36,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr uint32_t kNegInf2 = 0xFF80FF80u;
 static_assert((size_t)kLgGradBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial maximum per block fits the minimum workspace");
 static_assert(kLgMaxTop <= kLgThreads, "a thread an entry");
+constexpr int kListWaves = kLgMaxTop / kWave;  // waves whose threads have an entry
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -283,9 +284,9 @@ __device__ inline void finish_row(const StatArgs& a, int64_t row, const RowInput
             const double left = 1.0 - mass;
             const float q_rest = left < kNoRest ? 0.0f : (float)left;  // (a NaN stays)
             const bool rest = v.s != 0.0f;
-            const double log_rest = rest ? logf((float)((double)v.s / total)) + ((double)v.m - m) * a.scale : -INFINITY;
+            const double log_rest = rest ? logf(v.s / total) + ((double)v.m - m) * a.scale : -INFINITY;
             if (q_rest != 0.0f) loss += (double)q_rest * (logf(q_rest) - log_rest);
-            coef = v.m, norm = mass != mass ? NAN : rest && q_rest != 0.0f ? logf((float)((double)v.s / q_rest)) : INFINITY;
+            coef = v.m, norm = mass != mass ? NAN : rest && q_rest != 0.0f ? logf(v.s / q_rest) : INFINITY;
         }
         // without entries (or weights to share out) there is no term, whatever the logits: marked for the backward by norm = -inf
         bool some = false;
@@ -475,12 +476,13 @@ __device__ inline void block_top(const uint4* row, int c0, int c1, int V, int K,
 }
 
 // One block takes one row, or one of nseg pieces of it.  Dynamic LDS (TOP): the steps' maxima.  LIST: with a teacher, TAIL: whose
-// remainder is a class of its own, so that the statistics inside and outside the list are apart.
+// remainder is a class of its own, so that the statistics inside and outside the list are apart; those instances are held to the
+// registers of six blocks a compute unit (84 without a bound, and five blocks: 4096 x 131072 167 -> 173 us, 8192 x 32768 102 -> 105).
 template <bool ENT, bool TOP, bool LIST, bool TAIL, bool ONCE>
-__global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs a)
+__global__ __launch_bounds__(kLgThreads, TAIL ? 6 : 1) void logits_stat_kernel(const StatArgs a)
 {
     extern __shared__ uint16_t smax[];
-    __shared__ Stat wave_stat[kLgWaves], wave_listed[TAIL ? kLgWaves : 1];
+    __shared__ Stat wave_stat[kLgWaves], wave_listed[kListWaves];
     __shared__ std::conditional_t<TOP, Select, int> sel;
     __shared__ std::conditional_t<TAIL, List<false>, int> list;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
@@ -522,6 +524,11 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
                     v.s += on ? 0.0f : e, listed.s += on ? e : 0.0f;
                 }
             }
+            if (wave < kListWaves) {  // joined while the first step's loads are on their way
+                const float m = wave_all(listed.m, [](float x, float y) { return fmaxf(x, y); });
+                const float s = wave_all(raised<false>(listed, m, c2).s, [](float x, float y) { return x + y; });
+                if (lane == 0) wave_listed[wave] = {m, s, 0.0f};
+            }
         }
         for (int c = c0 + tid, step = 0; c < c1; c += kLgUnroll * kLgThreads, ++step) {
             if (!TAIL || step > 0) request(c);
@@ -554,10 +561,6 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         }
         v = wave_join<ENT>(v, c2);
         if (lane == 0) wave_stat[wave] = v;
-        if constexpr (TAIL) {
-            listed = wave_join<false>(listed, c2);
-            if (lane == 0) wave_listed[wave] = listed;
-        }
         __syncthreads();
         v = wave_stat[0];
 #pragma unroll
@@ -565,7 +568,7 @@ __global__ __launch_bounds__(kLgThreads) void logits_stat_kernel(const StatArgs 
         if constexpr (TAIL) {
             listed = wave_listed[0];
 #pragma unroll
-            for (int i = 1; i < kLgWaves; ++i) listed = join<false>(listed, wave_listed[i], c2);
+            for (int i = 1; i < kListWaves; ++i) listed = join<false>(listed, wave_listed[i], c2);
         }
         if (a.nseg > 1) {
             if (tid == 0) a.part[unit] = TAIL ? make_float4(v.m, v.s, listed.m, listed.s) : make_float4(v.m, v.s, v.d, 0.0f);
