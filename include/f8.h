@@ -663,11 +663,15 @@ size_t f8_residual_norm_bwd_workspace_bytes(int64_t M, int64_t D, int64_t gate_r
  *     both leave outside the list is one more class:
  *     loss = sum_k q_k (log q_k - log p[id_k]) + q_rest (log q_rest - log p_rest),
  *     q_rest = 1 - sum_k q_k (below 2^-20: 0).
+ * p_rest is 0, and the loss infinite, only where all logits outside the list are
+ * -inf, however far below the list they lie.
  * A row without entries (tail = 0: none with a weight above 0) has loss 0 and no
  * gradient, whatever its logits; else a NaN or +inf among its logits makes both
- * NaN.  An id that occurs twice counts with both weights.  logp (nullable, with targets): as above, for a term
- * on the given tokens in the same pass.  stats [M, 4] fp32, kept for the backward:
- * the two numbers above, and two of the teacher's.
+ * NaN.  An id that occurs twice counts with both weights.  logp (nullable, with
+ * targets): as above, for a term on the given tokens in the same pass, of the
+ * same p: hard labels at temperature 1 beside a divergence that scale softens
+ * need an f8_token_logprobs of their own.  stats [M, 4] fp32, kept for the
+ * backward: the two numbers above, and two for the teacher's term.
  * f8_distill_bwd: dlogits from d_loss and (nullable, with targets) d_logp, [M] fp32.
  * workspace of both forwards: f8_logits_workspace_bytes(M, V, top_k) bytes (top_k
  * 0 for f8_distill).  1 <= V <= 2^22; any M >= 0.  No atomics on results: they are reproducible.

@@ -7,8 +7,8 @@
 //   dz_j = scale * (g (p_j - q_j) + the given token's term above) [for j outside the list q_j = q_rest s_j, where s is the softmax
 //   of the logits outside the list alone].
 // Bound by memory: one read of the logits forward (2 bytes an element), one read and one write backward (4 bytes).  8192 x 131072
-// forward 315 us (6.8 TB/s), backward 785 (5.5); beside the loads stand about 9 instructions and an exponential an element, some
-// two thirds of what a compute unit can issue at that rate.
+// forward 314 us (6.8 TB/s), backward 783 (5.5); beside the loads stand about 9 instructions and an exponential an element, which keep
+// the vector units busy for 79 % of the time, 92 % with alternatives and 94 % with a teacher's list and the rest (4096 x 131072 166 us).
 // Softmax statistics are kept as (largest logit, log of the sum of exp(z - z_max)): a difference of two bf16 values is exact in
 // fp32 where their ratio is below 2^16, so that p keeps its precision however large the logits are, which one number lse would not.
 #include <float.h>
@@ -102,7 +102,7 @@ __device__ inline uint4 load_logits(const uint4* row, int c, int V)
 // The entries of one row that fall into a block's columns.  A chunk that holds some has a slot, the number of one of them; there its
 // entries leave which elements they are and their weights.  The sweep leaves these chunks out, and the thread whose entry is the
 // first element takes it: the same one whichever entry gave the slot its number, so that sums keep their order.
-// (2048 x 32768 with 128 entries: forward 38 us, backward 53; adjacent tokens 32 and 47, 45 and 162 with a search among all entries.)
+// (2048 x 32768 with 128 entries: forward 37 us, backward 53; adjacent tokens 32 and 48, 45 and 162 with a search among all entries.)
 constexpr uint8_t kNoSlot = 0xFF;
 template <bool WEIGHTS>
 struct List {
@@ -793,7 +793,8 @@ static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted, int leas
 // full step (of a chunk a thread at least: 100 x 8000 with 20 alternatives 14.8, so 9.5; 16 x 32768 16.2, so 13.3).
 constexpr int64_t kLgBlocksWanted = 512;
 // Loads past the caches.  Forward: from 1 GiB on, of which the backward would find little (8192 x 131072 357 -> 317 us, the backward
-// unchanged; 2048 x 131072 102 -> 93, but its backward 188 -> 205).  Backward, the last to read: from 256 MiB on (4096 x 32768
+// unchanged; 6144 x 131072 275 -> 241, backward 533 -> 580; at the limit, 4096 x 131072, 188 -> 168 and 343 -> 374, with a teacher
+// and the rest 193 -> 173 and 392 -> 404; below it 2048 x 131072 102 -> 93, but 188 -> 205).  Backward, the last to read: from 256 MiB on (4096 x 32768
 // 85 -> 80, 2000 x 131072 with a teacher 211 -> 180; but 512 x 50001 21.9 -> 23.0).
 constexpr int64_t kLgOnce = (int64_t)1 << 29, kLgGradOnce = (int64_t)1 << 27;
 

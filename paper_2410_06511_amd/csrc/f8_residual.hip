@@ -4,7 +4,7 @@
 //   dgate = sum over its rows of b t u,  dg_post = sum v y r1,  dg_pre = sum dn h r2.
 // Bound by memory: 8 bytes an element forward (x, y -> h, n), 12 backward (h, y, dh, dn -> dx, dy); as separate calls the sum,
 // the gate and each norm read and write their tensors again.  16384 x 8192 with both norms and gates: forward 190 us (5.6 TB/s),
-// backward 321 and 7 for its sums (4.9); 8192 x 4096 with the norm after the sum only: 44 (6.1), 57 and 5 (5.4).
+// backward 318 and 7 for its sums (5.0); 8192 x 4096 with the norm after the sum only: 44 (6.1), 58 and 5 (5.3).
 // A row is held in registers by TPR threads, U chunks of 16 bytes each, so that every tensor is read once although a norm needs
 // its row twice.  Sums over a row are taken in f8_rmsnorm's order (chunks 64 apart one after the other, then lanes by halves), so
 // that the plain residual and norm have the bits of f8_add followed by f8_rmsnorm.  Sums over rows have a fixed order too.
@@ -21,8 +21,8 @@ constexpr int kResBlocks = 2048;     // of the forward: one partial maximum each
 // 768 71); half as many above 4096 elements a row, where a block's waves fill a compute unit (16384 x 8192 371 -> 341 us, 300 x 8192
 // 26 -> 22).
 constexpr int kResBwdBlocks = 512;
-// Elements from which the backward loads past the caches (16384 x 8192 348 -> 326 us, 8192 x 5120 126 -> 118; 4096 x 4096 52 -> 53,
-// 2001 x 2816 26 -> 27).
+// Elements from which the backward loads past the caches (16384 x 8192 348 -> 326 us, 12288 x 4096 115 -> 92, 8192 x 5120 126 -> 118;
+// at the limit, 8192 x 4096, 65 -> 64; 4096 x 4096 52 -> 53, 2001 x 2816 26 -> 27).
 constexpr int64_t kResOnce = (int64_t)1 << 25;
 static_assert((size_t)kResBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial per block fits the minimum workspace");
 

@@ -16,7 +16,7 @@ from . import f8
 
 class OutputHead:
     def __init__(self, M, D, vocab, eps=1e-5, scale=1.0, grad_format=f8.E4M3, device="cuda", scaling="dynamic", history_len=16):
-        """scale: factor of the logits (an inverse temperature).  M: tokens, as D a multiple of 16."""
+        """scale: factor of the logits (an inverse temperature), of every loss.  M: tokens, as D a multiple of 16."""
         assert scaling in ("dynamic", "delayed")
         self.M, self.D, self.vocab, self.eps, self.scale = M, D, vocab, eps, scale
         N = self.width = (vocab + 15) // 16 * 16
@@ -103,7 +103,7 @@ class OutputHead:
 
     def forward_distill(self, x, w, teacher_ids, teacher_logp, tail=False, teacher_scale=1.0, targets=None, stream=None):
         """Divergence from the teacher's entries [M, K] (f8.token_logprobs of its logits gives them); with targets their log
-        probabilities too, in .logp."""
+        probabilities too, in .logp: under the head's scale, as the divergence, not at temperature 1 beside a softened one."""
         self._run(self.distill_forward_stages(x, w, teacher_ids, teacher_logp, tail, teacher_scale, targets, stream))
         return self.loss
 
