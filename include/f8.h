@@ -663,8 +663,8 @@ size_t f8_residual_norm_bwd_workspace_bytes(int64_t M, int64_t D, int64_t gate_r
  *     both leave outside the list is one more class:
  *     loss = sum_k q_k (log q_k - log p[id_k]) + q_rest (log q_rest - log p_rest),
  *     q_rest = 1 - sum_k q_k (below 2^-20: 0).
- * p_rest is 0, and the loss infinite, only where all logits outside the list are
- * -inf, however far below the list they lie.
+ * p_rest is 0 only where all logits outside the list are -inf: however far below
+ * the list they lie, loss (up to fp32's largest number) and gradient are these.
  * A row without entries (tail = 0: none with a weight above 0) has loss 0 and no
  * gradient, whatever its logits; else a NaN or +inf among its logits makes both
  * NaN.  An id that occurs twice counts with both weights.  logp (nullable, with

@@ -697,9 +697,9 @@ __global__ __launch_bounds__(THREADS) void logits_grad_kernel(const GradArgs a)
         // nothing to hand back: no weight, or no logit that a change could move
         const bool zero = (A == 0.0f && B == 0.0f && dlp == 0.0f && g == 0.0f) || st[1] == -INFINITY;
         // chunk cu of the row, with the listed ones among its elements
-        auto emit = [&](int cu, uint4 w, uint32_t mask, const float* q) {
+        auto emit = [&](int cu, uint4 v, uint32_t mask, const float* q) {
             float z[8];
-            unpack8(w, z);
+            unpack8(v, z);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool on = LIST && q && (mask >> j & 1);
@@ -794,8 +794,8 @@ static Split split_rows(int64_t M, int64_t cols, int64_t blocks_wanted, int leas
 constexpr int64_t kLgBlocksWanted = 512;
 // Loads past the caches.  Forward: from 1 GiB on, of which the backward would find little (8192 x 131072 357 -> 317 us, the backward
 // unchanged; 6144 x 131072 275 -> 241, backward 533 -> 580; at the limit, 4096 x 131072, 188 -> 168 and 343 -> 374, with a teacher
-// and the rest 193 -> 173 and 392 -> 404; below it 2048 x 131072 102 -> 93, but 188 -> 205).  Backward, the last to read: from 256 MiB on (4096 x 32768
-// 85 -> 80, 2000 x 131072 with a teacher 211 -> 180; but 512 x 50001 21.9 -> 23.0).
+// and the rest 193 -> 173 and 392 -> 404; below it 2048 x 131072 102 -> 93, but 188 -> 205).  Backward, the last to read: from
+// 256 MiB on (4096 x 32768 85 -> 80, 2000 x 131072 with a teacher 211 -> 180; but 512 x 50001 21.9 -> 23.0).
 constexpr int64_t kLgOnce = (int64_t)1 << 29, kLgGradOnce = (int64_t)1 << 27;
 
 static size_t logits_part_bytes(int64_t M, int64_t V, int64_t top)
