@@ -61,6 +61,9 @@ typedef enum {
  * 0x7B = 57344. */
 typedef enum { F8_E4M3 = 0, F8_E5M2 = 1 } f8_format;
 
+/* Types of gradients that a call takes in either. */
+typedef enum { F8_BF16 = 0, F8_F32 = 1 } f8_dtype;
+
 /* How many scales a [rows, cols] tensor has: one, one per row, one per column. */
 typedef enum { F8_TENSORWISE = 0, F8_ROWWISE = 1, F8_COLWISE = 2 } f8_granularity;
 
@@ -626,6 +629,60 @@ f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf
 size_t f8_residual_norm_bwd_workspace_bytes(int64_t M, int64_t D, int64_t gate_rows);
 
 /*
+ * Token embeddings, in front of the first block, and their table's gradient.
+ *   out[m, :] = bf16(scale * table[ids[m], :])
+ * ids [M] int64: a negative id stands for no token (zeros), one >= V gives NaN;
+ * table [V, D] (row pitch ldt), out [M, D] (pitch ldo) bf16.
+ *
+ * f8_embed_bwd: dtable[v, :] = scale * (sum of dout[m, :] over the m with
+ * ids[m] = v), all V rows (zeros where there is none); ids below 0 or from V on
+ * take no part.  dout [M, D] bf16; dtable [V, D] (pitch ldt in elements) bf16 or
+ * fp32 as dtable_type says.  fp32 sums in the order of the tokens, in pieces of a
+ * list of the tokens by id, then over the pieces: results are reproducible.
+ * workspace: f8_embed_bwd_workspace_bytes (none needed without tokens).
+ * Any M >= 0, V >= 0; D and the pitches multiples of 8, D <= 2^20; scale finite.
+ * out and table, dout and dtable must not overlap.
+ */
+f8_status f8_embed(const int64_t* ids, int64_t M, const void* table_bf16, int64_t ldt, int64_t V, int64_t D, float scale,
+                   void* out_bf16, int64_t ldo, void* stream);
+f8_status f8_embed_bwd(const int64_t* ids, int64_t M, const void* dout_bf16, int64_t lddo, int64_t V, int64_t D, float scale,
+                       f8_dtype dtable_type, void* dtable, int64_t ldt, void* workspace, size_t workspace_bytes, void* stream);
+size_t f8_embed_bwd_workspace_bytes(int64_t M, int64_t V, int64_t D);
+
+/*
+ * Layer norm, beside f8_rmsnorm, alone or behind a residual sum:
+ *   h = bf16(x + y)             (y NULL: h = x, and nothing is written to h)
+ *   n = (h - mean) * rstd * g + b
+ *   mean[m] = mean_d h[m, d],  rstd[m] = 1 / sqrt(mean_d (h[m, d] - mean[m])^2 + eps)
+ * x, y, h, n [M, D] bf16 with their row pitches; y and h both or neither; g, b
+ * [D] bf16, b nullable.  The statistics are those of the h that is kept, in bf16,
+ * the variance from the differences from the mean; mean, rstd (nullable) [M]
+ * fp32, kept for the backward.  amax_n (nullable, 1 float): exact maximum
+ * magnitude of the bf16 values of n, for f8_linear_fwd_chained (workspace, only
+ * then: at least 8 KiB).  fp32 arithmetic, h and n rounded once.
+ * h may be x or y and n may be x or y (the other), at the same pitch.
+ *
+ * f8_layernorm_bwd: with c = (h - mean) * rstd and v = g * dn,
+ *   dx = rstd * (v - mean_d v - c * mean_d(v c)) + dh
+ *   dg[d] = sum_m dn[m, d] c[m, d],   db[d] = sum_m dn[m, d]
+ * dh (nullable, with dx): the gradient of h through the residual stream, so that
+ * dx is the gradient of x and of y.  dx [M, D] bf16, dg, db [D] fp32: each may be
+ * NULL, not all.  amax_dx (nullable, with dx): exact maximum magnitude of dx.
+ * dx may be h, dn or dh at the same pitch.  Sums over rows are taken in a fixed
+ * order (results are reproducible).  workspace (with dg, db or amax_dx):
+ * f8_layernorm_bwd_workspace_bytes.
+ * Any M >= 0; D and the pitches multiples of 8, D <= 16384; eps >= 0 and finite.
+ */
+f8_status f8_layernorm(const void* x_bf16, int64_t ldx, const void* y_bf16, int64_t ldy, int64_t M, int64_t D, const void* g_bf16,
+                       const void* b_bf16, float eps, void* h_bf16, int64_t ldh, void* n_bf16, int64_t ldn, float* mean,
+                       float* rstd, float* amax_n, void* workspace, size_t workspace_bytes, void* stream);
+f8_status f8_layernorm_bwd(const void* h_bf16, int64_t ldh, const void* g_bf16, const float* mean, const float* rstd,
+                           const void* dn_bf16, int64_t lddn, const void* dh_bf16, int64_t lddh, int64_t M, int64_t D,
+                           void* dx_bf16, int64_t lddx, float* dg, float* db, float* amax_dx, void* workspace,
+                           size_t workspace_bytes, void* stream);
+size_t f8_layernorm_bwd_workspace_bytes(int64_t M, int64_t D);
+
+/*
  * From the logits of an output projection to the loss and back.  logits [M, *]
  * bf16 (row pitch ld, a multiple of 8; rows are read up to the next multiple of
  * 8 columns), of which the first V columns are the vocabulary: a Float8 linear's
@@ -692,6 +749,36 @@ f8_status f8_distill_bwd(const void* logits_bf16, int64_t ld, int64_t M, int64_t
                          const int64_t* targets, const float* stats, const float* d_loss, const float* d_logp,
                          void* dlogits_bf16, int64_t ldd, int64_t cols, float* amax_d, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/*
+ * Between a step's backward and its update: the norm of many gradients
+ * together, and their scaling to a largest norm.
+ * A list is an array in HOST memory, read during the call, of tensors in device
+ * memory: n contiguous elements each (n 0: none), on any address that is a
+ * multiple of the element's size.
+ *
+ * f8_grad_norm: kind F8_NORM_2: norm[0] = sqrt(sum over all elements of x^2),
+ *   sum[0] = the sum itself, in fp64, for a reduction over ranks; F8_NORM_MAX:
+ *   norm[0] = sum[0] = max |x|.  norm, sum: device memory, each may be NULL, not
+ *   both.  Squares and sums in fp64, in a fixed order (results are reproducible).
+ *   A NaN among the elements makes the norm NaN; an empty list has norm 0.
+ *   workspace: f8_grad_norm_workspace_bytes of the same sizes and types.
+ * f8_grad_clip: out = in * min(1, most / (norm[0] + 1e-6)), one fp32 product
+ *   rounded to the tensor's type; with a factor of 1 the same bits.  out: a list of
+ *   the same sizes and types (tensor i the same memory as in's or apart from it, and
+ *   no other overlaps), or NULL: in place.  A NaN norm makes everything NaN;
+ *   most >= 0.
+ */
+typedef struct f8_tensor {
+    void* data;
+    int64_t n;    /* elements */
+    int32_t type; /* f8_dtype */
+} f8_tensor;
+typedef enum { F8_NORM_2 = 0, F8_NORM_MAX = 1 } f8_norm;
+f8_status f8_grad_norm(const f8_tensor* list, int64_t count, f8_norm kind, float* norm, double* sum, void* workspace,
+                       size_t workspace_bytes, void* stream);
+f8_status f8_grad_clip(const f8_tensor* in, const f8_tensor* out, int64_t count, const float* norm, float most, void* stream);
+size_t f8_grad_norm_workspace_bytes(const f8_tensor* list, int64_t count);
 
 /*
  * Forward of the linear whose input is already quantised in saved->x (codes in

@@ -1,0 +1,318 @@
+// The norm of many gradients together, and their scaling to a largest norm, between a step's backward and its update:
+//   norm = sqrt(sum over all tensors of x^2) (or the largest |x|),   out = x min(1, most / (norm + 1e-6)).
+// Bound by memory: the norm reads every element once, the scaling reads and writes it.  Squares and sums are taken in fp64: the
+// square of a bf16 or fp32 value is exact there and cannot overflow or vanish (fp32 loses gradients below 1e-19 and above 1e19),
+// at a quarter of the rate that the memory leaves room for.
+// The tensors' addresses and sizes come as kernel arguments, kTensors to a launch; a block walks over steps of kStep elements of
+// all of a launch's tensors and finds each step's tensor by bisection in scalar registers.  Partial sums are added in a fixed order.
+#include "f8_device.hpp"
+#include "f8_host.hpp"
+
+namespace f8 {
+
+constexpr int kTensors = 96;          // of a launch: 3 KB of arguments at most
+constexpr int kGradThreads = 256;
+constexpr int kGradUnroll = 4;
+constexpr int kStep = kGradThreads * 8 * kGradUnroll;  // elements
+constexpr int kGradBlocks = 2048;     // of the norm: one partial sum each
+
+struct TensorList {
+    const void* in[kTensors];
+    void* out[kTensors];
+    int64_t n[kTensors];           // elements
+    uint32_t first[kTensors + 1];  // the tensors' first steps; the number of steps
+    uint32_t f32[kTensors / 32];   // bit i: tensor i holds fp32
+    int count;
+};
+
+// The tensor of a step: the last whose first step is not behind it (scalar: `step` is the same in all lanes).
+__device__ inline int tensor_of(const TensorList& l, uint32_t step)
+{
+    int lo = 0, hi = l.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (l.first[mid] <= step) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Tensors lie on any element: loads and stores of eight are those of the element's alignment (the memory takes them, two lines
+// instead of one now and then).
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+__device__ inline uint4 load_any(const void* p) { return __builtin_bit_cast(uint4, (u32x4)*static_cast<const u32x4_any*>(p)); }
+__device__ inline void store_any(void* p, uint4 v) { *static_cast<u32x4_any*>(p) = __builtin_bit_cast(u32x4, v); }
+
+struct Eight {
+    uint4 a, b;  // b: fp32 only
+};
+template <bool F32>
+__device__ inline void widen(const Eight& e, float* f)
+{
+    if constexpr (F32) {
+        f[0] = __uint_as_float(e.a.x), f[1] = __uint_as_float(e.a.y), f[2] = __uint_as_float(e.a.z), f[3] = __uint_as_float(e.a.w);
+        f[4] = __uint_as_float(e.b.x), f[5] = __uint_as_float(e.b.y), f[6] = __uint_as_float(e.b.z), f[7] = __uint_as_float(e.b.w);
+    } else {
+        unpack8(e.a, f);
+    }
+}
+template <bool F32>
+__device__ inline Eight load8(const void* in, int64_t i)  // elements i .. i + 7
+{
+    Eight e;
+    e.a = load_any(static_cast<const char*>(in) + i * (F32 ? 4 : 2));
+    e.b = F32 ? load_any(static_cast<const char*>(in) + i * 4 + 16) : make_uint4(0, 0, 0, 0);
+    return e;
+}
+template <bool F32>
+__device__ inline float load1(const void* in, int64_t i)
+{
+    return F32 ? static_cast<const float*>(in)[i] : bf16_lo(static_cast<const uint16_t*>(in)[i]);
+}
+
+// ---- norm ----------------------------------------------------------------------------------------
+
+// MAX: magnitudes by their bits, so that a NaN is larger than everything.
+template <bool MAX>
+struct Norm {
+    double s[2] = {0.0, 0.0};
+    uint32_t m = 0;
+    __device__ void add(float v, int k)
+    {
+        if constexpr (MAX) {
+            const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+            m = b > m ? b : m;
+        } else {
+            s[k & 1] = __builtin_fma((double)v, (double)v, s[k & 1]);
+        }
+    }
+    __device__ double value() const { return MAX ? (double)__uint_as_float(m) : s[0] + s[1]; }
+};
+__device__ inline double join(double a, double b, bool max) { return max ? (a != a || a > b ? a : b) : a + b; }
+
+template <bool MAX>
+__device__ inline double block_join(double v, double* red)
+{
+    for (int off = 32; off >= 1; off >>= 1) v = join(v, __shfl_xor(v, off, kWave), MAX);
+    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = red[0];
+    for (int w = 1; w < (int)blockDim.x / kWave; ++w) v = join(v, red[w], MAX);
+    return v;
+}
+
+template <bool MAX, bool F32>
+__device__ inline void norm_step(const void* in, int64_t n, int64_t at, Norm<MAX>& norm)
+{
+    if (at + kStep <= n) {
+        Eight e[kGradUnroll];
+#pragma unroll
+        for (int u = 0; u < kGradUnroll; ++u) e[u] = load8<F32>(in, at + (u * kGradThreads + (int)threadIdx.x) * 8);
+#pragma unroll
+        for (int u = 0; u < kGradUnroll; ++u) {
+            float f[8];
+            widen<F32>(e[u], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) norm.add(f[j], j);
+        }
+    } else {
+        for (int64_t i = at + (int)threadIdx.x * 8; i < n; i += kGradThreads * 8) {
+            if (i + 8 <= n) {
+                float f[8];
+                widen<F32>(load8<F32>(in, i), f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) norm.add(f[j], j);
+            } else {
+                for (int64_t k = i; k < n; ++k) norm.add(load1<F32>(in, k), 0);
+            }
+        }
+    }
+}
+
+template <bool MAX>
+__global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const TensorList l, double* __restrict__ part)
+{
+    __shared__ double red[kGradThreads / kWave];
+    Norm<MAX> norm;
+    const uint32_t steps = l.first[l.count];
+    for (uint32_t step = blockIdx.x; step < steps; step += gridDim.x) {
+        const int t = tensor_of(l, step);
+        const int64_t at = (int64_t)(step - l.first[t]) * kStep;
+        if (l.f32[t / 32] >> (t % 32) & 1) norm_step<MAX, true>(l.in[t], l.n[t], at, norm);
+        else norm_step<MAX, false>(l.in[t], l.n[t], at, norm);
+    }
+    const double v = block_join<MAX>(norm.value(), red);
+    if (threadIdx.x == 0) part[blockIdx.x] = v;
+}
+
+template <bool MAX>
+__global__ __launch_bounds__(1024) void grad_norm_final_kernel(const double* __restrict__ part, int64_t n, float* norm, double* sum)
+{
+    __shared__ double red[1024 / kWave];
+    double v = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 1024) v = join(v, part[i], MAX);
+    v = block_join<MAX>(v, red);
+    if (threadIdx.x == 0) {
+        if (norm) norm[0] = (float)(MAX ? v : __builtin_sqrt(v));
+        if (sum) sum[0] = v;
+    }
+}
+
+// ---- scaling -------------------------------------------------------------------------------------
+
+template <bool F32>
+__device__ inline void clip_step(const void* in, void* out, int64_t n, int64_t at, float factor)
+{
+    const auto put = [&](const Eight& e, int64_t i) {
+        char* o = static_cast<char*>(out) + i * (F32 ? 4 : 2);
+        if (factor == 1.0f) {  // the same bits
+            store_any(o, e.a);
+            if (F32) store_any(o + 16, e.b);
+            return;
+        }
+        float f[8];
+        widen<F32>(e, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] *= factor;
+        if constexpr (F32) {
+            store_any(o, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+            store_any(o + 16, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
+        } else {
+            store_any(o, make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])));
+        }
+    };
+    if (at + kStep <= n) {
+        Eight e[kGradUnroll];
+#pragma unroll
+        for (int u = 0; u < kGradUnroll; ++u) e[u] = load8<F32>(in, at + (u * kGradThreads + (int)threadIdx.x) * 8);
+#pragma unroll
+        for (int u = 0; u < kGradUnroll; ++u) put(e[u], at + (u * kGradThreads + (int)threadIdx.x) * 8);
+    } else {
+        for (int64_t i = at + (int)threadIdx.x * 8; i < n; i += kGradThreads * 8) {
+            if (i + 8 <= n) {
+                put(load8<F32>(in, i), i);
+            } else {
+                for (int64_t k = i; k < n; ++k) {
+                    if constexpr (F32) {
+                        const float v = static_cast<const float*>(in)[k];
+                        static_cast<float*>(out)[k] = factor == 1.0f ? v : v * factor;
+                    } else {
+                        const uint16_t v = static_cast<const uint16_t*>(in)[k];
+                        static_cast<uint16_t*>(out)[k] = factor == 1.0f ? v : (uint16_t)pack_bf16(bf16_lo(v) * factor, 0.0f);
+                    }
+                }
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(const TensorList l, const float* __restrict__ norm, float most)
+{
+    float factor = most / (norm[0] + 1e-6f);
+    factor = factor > 1.0f ? 1.0f : factor;  // (a NaN stays one)
+    const uint32_t steps = l.first[l.count];
+    for (uint32_t step = blockIdx.x; step < steps; step += gridDim.x) {
+        const int t = tensor_of(l, step);
+        if (factor == 1.0f && l.in[t] == l.out[t]) continue;
+        const int64_t at = (int64_t)(step - l.first[t]) * kStep;
+        if (l.f32[t / 32] >> (t % 32) & 1) clip_step<true>(l.in[t], l.out[t], l.n[t], at, factor);
+        else clip_step<false>(l.in[t], l.out[t], l.n[t], at, factor);
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+
+constexpr int64_t kMaxElements = (int64_t)1 << 40;  // of a tensor
+
+static f8_status check_list(const f8_tensor* list, int64_t count)
+{
+    if (count < 0) return F8_ERR_SHAPE;
+    if (count && !list) return F8_ERR_NULL;
+    for (int64_t i = 0; i < count; ++i) {
+        if (list[i].type != F8_BF16 && list[i].type != F8_F32) return F8_ERR_ENUM;
+        if (list[i].n < 0 || list[i].n > kMaxElements) return F8_ERR_SHAPE;
+        if (list[i].n && !list[i].data) return F8_ERR_NULL;
+        if ((uintptr_t)list[i].data & (list[i].type == F8_F32 ? 3 : 1)) return F8_ERR_ALIGN;
+    }
+    return F8_OK;
+}
+
+// The list in launches of at most kTensors tensors and 2^31 steps: f(TensorList, steps).
+template <class F>
+static void for_launches(const f8_tensor* in, const f8_tensor* out, int64_t count, F&& f)
+{
+    TensorList l;
+    const auto clear = [&] {
+        l.count = 0, l.first[0] = 0;
+        for (auto& w : l.f32) w = 0;
+    };
+    clear();
+    for (int64_t i = 0; i < count; ++i) {
+        if (in[i].n == 0) continue;
+        const uint32_t steps = (uint32_t)((in[i].n + kStep - 1) / kStep);
+        if (l.count == kTensors || (uint64_t)l.first[l.count] + steps > 0x7FFFFFFFu) f(l), clear();
+        l.in[l.count] = in[i].data, l.out[l.count] = out ? out[i].data : nullptr, l.n[l.count] = in[i].n;
+        if (in[i].type == F8_F32) l.f32[l.count / 32] |= 1u << (l.count % 32);
+        l.first[l.count + 1] = l.first[l.count] + steps;
+        ++l.count;
+    }
+    if (l.count) f(l);
+}
+static unsigned grad_blocks(const TensorList& l) { return l.first[l.count] < kGradBlocks ? l.first[l.count] : kGradBlocks; }
+
+}  // namespace f8
+
+using namespace f8;
+
+extern "C" {
+
+size_t f8_grad_norm_workspace_bytes(const f8_tensor* list, int64_t count)
+{
+    size_t parts = 0;
+    if (check_list(list, count) == F8_OK) for_launches(list, nullptr, count, [&](const TensorList& l) { parts += grad_blocks(l); });
+    const size_t bytes = parts * sizeof(double);
+    return bytes < kMinWorkspaceBytes ? kMinWorkspaceBytes : bytes;
+}
+
+f8_status f8_grad_norm(const f8_tensor* list, int64_t count, f8_norm kind, float* norm, double* sum, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    if ((int)kind != F8_NORM_2 && (int)kind != F8_NORM_MAX) return F8_ERR_ENUM;
+    const f8_status s = check_list(list, count);
+    if (s != F8_OK) return s;
+    if (!norm && !sum) return F8_ERR_NULL;
+    if (!aligned16(workspace) || ((uintptr_t)norm & 3) || ((uintptr_t)sum & 7)) return F8_ERR_ALIGN;
+    if (!workspace || workspace_bytes_ < f8_grad_norm_workspace_bytes(list, count)) return F8_ERR_WORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    double* const part = (double*)workspace;
+    int64_t parts = 0;
+    const bool max = kind == F8_NORM_MAX;
+    for_launches(list, nullptr, count, [&](const TensorList& l) {
+        const unsigned b = grad_blocks(l);
+        (max ? grad_norm_kernel<true> : grad_norm_kernel<false>)<<<b, kGradThreads, 0, st>>>(l, part + parts);
+        parts += b;
+    });
+    (max ? grad_norm_final_kernel<true> : grad_norm_final_kernel<false>)<<<1, 1024, 0, st>>>(part, parts, norm, sum);
+    return last_launch_status();
+}
+
+f8_status f8_grad_clip(const f8_tensor* in, const f8_tensor* out, int64_t count, const float* norm, float most, void* stream)
+{
+    if (!out) out = in;
+    f8_status s = check_list(in, count);
+    if (s != F8_OK || (s = check_list(out, count)) != F8_OK) return s;
+    if (!norm) return F8_ERR_NULL;
+    if ((uintptr_t)norm & 3) return F8_ERR_ALIGN;
+    if (!(most >= 0.0f)) return F8_ERR_SHAPE;
+    for (int64_t i = 0; i < count; ++i) {
+        if (in[i].type != out[i].type) return F8_ERR_ENUM;
+        const int64_t bytes = in[i].n * (in[i].type == F8_F32 ? 4 : 2);
+        if (in[i].n != out[i].n || (in[i].data != out[i].data && bytes && !apart({in[i].data, bytes}, {out[i].data, bytes}))) return F8_ERR_SHAPE;
+    }
+    for_launches(in, out, count, [&](const TensorList& l) {
+        const uint32_t steps = l.first[l.count], most_blocks = 8 * kGradBlocks;
+        grad_clip_kernel<<<steps < most_blocks ? steps : most_blocks, kGradThreads, 0, (hipStream_t)stream>>>(l, norm, most);
+    });
+    return last_launch_status();
+}
+
+}  // extern "C"

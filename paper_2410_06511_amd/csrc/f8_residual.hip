@@ -8,14 +8,12 @@
 // A row is held in registers by TPR threads, U chunks of 16 bytes each, so that every tensor is read once although a norm needs
 // its row twice.  Sums over a row are taken in f8_rmsnorm's order (chunks 64 apart one after the other, then lanes by halves), so
 // that the plain residual and norm have the bits of f8_add followed by f8_rmsnorm.  Sums over rows have a fixed order too.
-#include <type_traits>
-
 #include "f8_device.hpp"
 #include "f8_host.hpp"
+#include "f8_rows.hpp"
 
 namespace f8 {
 
-constexpr int64_t kResMaxD = 16384;
 constexpr int kResBlocks = 2048;     // of the forward: one partial maximum each
 // Blocks of the backward, each of which leaves a partial row of every gain's sums (4096 x 4096 with 256 / 512 blocks 58 / 53 us,
 // 768 71); half as many above 4096 elements a row, where a block's waves fill a compute unit (16384 x 8192 371 -> 341 us, 300 x 8192
@@ -39,35 +37,6 @@ struct ResidualArgs {
     float *rstd_post, *rstd_pre;
     uint32_t* partial;
 };
-
-// Kernels for THREADS == 64: a row per wave, four waves a block; above: a row per block of at most THREADS threads.
-constexpr int kResWaveRows = 4;
-constexpr int res_threads(int THREADS) { return THREADS == kWave ? kWave * kResWaveRows : THREADS; }
-
-__device__ inline uint4 pack8(const float* f)
-{
-    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-}
-__device__ inline const uint4* row_of(const uint16_t* p, int64_t m, int64_t ld) { return reinterpret_cast<const uint4*>(p + m * ld); }
-__device__ inline uint4* row_of(uint16_t* p, int64_t m, int64_t ld) { return reinterpret_cast<uint4*>(p + m * ld); }
-
-// Maximum over a block of any number of waves, for its first wave.
-__device__ inline uint32_t waves_max(uint32_t v, uint32_t* red)
-{
-    v = wave_max_u32(v);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
-    __syncthreads();
-    return threadIdx.x < kWave ? wave_max_u32(threadIdx.x < blockDim.x / kWave ? red[threadIdx.x] : 0) : 0;
-}
-
-// 1 / sqrt(v) rounded once: the fp64 instruction (some 2^-26 off) and one Newton step.  (The norm of the branch; the one after
-// the sum has f8_rmsnorm's arithmetic and bits.)
-__device__ inline float rsqrt_exact(double v)
-{
-    const double r = __builtin_amdgcn_rsq(v);
-    return (float)(r > 0.0 && r < __builtin_inf() ? r + 0.5 * r * (1.0 - v * r * r) : r);
-}
 
 // Sum over a wave in f8_rmsnorm's order; a row waits for it up to twice.
 __device__ inline float wave_sum(float v)
@@ -103,11 +72,11 @@ struct RowSum {
 };
 
 template <int THREADS, int U, bool POST, bool PRE>
-__global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_kernel(const ResidualArgs p)
+__global__ __launch_bounds__(block_threads(THREADS)) void residual_norm_kernel(const ResidualArgs p)
 {
-    constexpr int kRows = THREADS == kWave ? kResWaveRows : 1;
+    constexpr int kRows = THREADS == kWave ? kWaveRows : 1;
     __shared__ float terms[2][RowSum<THREADS, U>::kPieces][kWave];
-    __shared__ uint32_t red[res_threads(THREADS) / kWave];
+    __shared__ uint32_t red[block_threads(THREADS) / kWave];
     RowSum<THREADS, U> sum{terms};
     const int TPR = THREADS == kWave ? kWave : (int)blockDim.x, t = THREADS == kWave ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     uint32_t mag = 0;
@@ -205,12 +174,12 @@ struct ResidualGradArgs {
 // A block takes units: the rows part, part + parts, ... of one group of rows that share a gate's row, and leaves one row of
 // sums a gain.
 template <int THREADS, int U, bool POST, bool GATE, bool PRE, bool ONCE>
-__global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_bwd_kernel(const ResidualGradArgs p)
+__global__ __launch_bounds__(block_threads(THREADS)) void residual_norm_bwd_kernel(const ResidualGradArgs p)
 {
-    constexpr int kRows = THREADS == kWave ? kResWaveRows : 1;
+    constexpr int kRows = THREADS == kWave ? kWaveRows : 1;
     __shared__ float terms[2][RowSum<THREADS, U>::kPieces][kWave];
     __shared__ float share[kRows][kRows > 1 ? kWave * U * 8 : 1];
-    __shared__ uint32_t red[res_threads(THREADS) / kWave];
+    __shared__ uint32_t red[block_threads(THREADS) / kWave];
     RowSum<THREADS, U> sum{terms};
     const int TPR = THREADS == kWave ? kWave : (int)blockDim.x;
     const int t = THREADS == kWave ? (int)threadIdx.x % kWave : (int)threadIdx.x, sub = THREADS == kWave ? (int)threadIdx.x / kWave : 0;
@@ -368,36 +337,23 @@ __global__ __launch_bounds__(res_threads(THREADS)) void residual_norm_bwd_kernel
 }
 
 // The sums of the blocks' rows, in their order: blockIdx.y is a set of `strips` rows of partial sums and its output row.
-constexpr int kResFinalCols = 32, kResFinalGroups = 16;
-struct ResidualFinalArgs {
-    const float* part[2];  // the gains' sums, one row a block
-    float* out[2];
-    int sets, strips;
-    const float* part_gate;  // `parts` rows for each row of the gate
-    float* dgate;
-    int parts;
-    int64_t D;
-    const uint32_t* partial;  // nullable: the blocks' maxima
-    int npartial;
-    float* amax;
-};
-__global__ __launch_bounds__(kResFinalCols* kResFinalGroups) void residual_final_kernel(const ResidualFinalArgs p)
+__global__ __launch_bounds__(kSumCols* kSumGroups) void column_sums_kernel(const ColumnSums p)
 {
-    __shared__ float sum[kResFinalGroups][kResFinalCols];
-    __shared__ uint32_t red[kResFinalGroups * kResFinalCols / kWave];
-    const int cl = threadIdx.x % kResFinalCols, grp = threadIdx.x / kResFinalCols;
-    const int64_t c = (int64_t)blockIdx.x * kResFinalCols + cl;
+    __shared__ float sum[kSumGroups][kSumCols];
+    __shared__ uint32_t red[kSumGroups * kSumCols / kWave];
+    const int cl = threadIdx.x % kSumCols, grp = threadIdx.x / kSumCols;
+    const int64_t c = (int64_t)blockIdx.x * kSumCols + cl;
     const int set = (int)blockIdx.y, n = set < p.sets ? p.strips : p.parts;
     const float* src = set < p.sets ? p.part[set] : p.part_gate + (int64_t)(set - p.sets) * p.parts * p.D;
     float* out = set < p.sets ? p.out[set] : p.dgate + (int64_t)(set - p.sets) * p.D;
     float s = 0.0f;
     if (c < p.D) {
         constexpr int AHEAD = 8;
-        for (int i = grp; i < n; i += kResFinalGroups * AHEAD) {
+        for (int i = grp; i < n; i += kSumGroups * AHEAD) {
             float v[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int at = i + kResFinalGroups * k;
+                const int at = i + kSumGroups * k;
                 v[k] = at < n ? src[(int64_t)at * p.D + c] : 0.0f;
             }
 #pragma unroll
@@ -409,39 +365,24 @@ __global__ __launch_bounds__(kResFinalCols* kResFinalGroups) void residual_final
     if (grp == 0 && c < p.D) {
         float v = sum[0][cl];
 #pragma unroll
-        for (int k = 1; k < kResFinalGroups; ++k) v += sum[k][cl];
+        for (int k = 1; k < kSumGroups; ++k) v += sum[k][cl];
         out[c] = v;
     }
     if (p.amax && blockIdx.x == 0 && set == 0) {
         uint32_t m = 0;
-        for (int i = threadIdx.x; i < p.npartial; i += kResFinalGroups * kResFinalCols) m = p.partial[i] > m ? p.partial[i] : m;
-        m = block_max_u32<kResFinalGroups * kResFinalCols / kWave>(m, red);
+        for (int i = threadIdx.x; i < p.npartial; i += kSumGroups * kSumCols) m = p.partial[i] > m ? p.partial[i] : m;
+        m = block_max_u32<kSumGroups * kSumCols / kWave>(m, red);
         if (threadIdx.x == 0) p.amax[0] = mag_to_float(m);
     }
 }
 
+void column_sums(const ColumnSums& p, unsigned rows, hipStream_t st)
+{
+    column_sums_kernel<<<dim3((unsigned)((p.D + kSumCols - 1) / kSumCols), rows), kSumCols * kSumGroups, 0, st>>>(p);
+}
+
 // ---- host ----------------------------------------------------------------------------------------
 
-// f(upper bound of a block's threads, chunks a thread, threads): a row of dc chunks by as few waves as hold it with U chunks each
-template <int T>
-using Threads = std::integral_constant<int, T>;
-template <class U, class F>
-static void with_block(int64_t dc, U u, F&& f)
-{
-    const int threads = (int)((dc + u() * kWave - 1) / (u() * kWave)) * kWave;
-    if (threads <= 256) f(Threads<256>{}, u, threads);
-    else if (threads <= 512) f(Threads<512>{}, u, threads);
-    else f(Threads<1024>{}, u, threads);
-}
-using One = std::integral_constant<int, 1>;
-using Two = std::integral_constant<int, 2>;
-template <class F>
-static void with_fwd_shape(int64_t dc, F&& f)
-{
-    if (dc <= 64) f(Threads<64>{}, One{}, res_threads(64));
-    else if (dc <= 128) f(Threads<64>{}, Two{}, res_threads(64));
-    else with_block(dc, Two{}, f);
-}
 // The backward holds four rows and up to three rows of sums.  One chunk a thread leaves registers for enough waves up to 8192
 // elements (16384 x 8192 394 -> 371 us, 8192 x 2048 59 -> 50), but a row of 520 to 1024 elements is better a wave's own, without
 // barriers (8192 x 1024 45 -> 30); with a norm of the branch the two are within 6 % between 2816 and 4096 (2001 x 2816 26.9 -> 25.8,
@@ -450,8 +391,8 @@ static void with_fwd_shape(int64_t dc, F&& f)
 template <class F>
 static void with_bwd_shape(int64_t dc, F&& f)
 {
-    if (dc <= 64) f(Threads<64>{}, One{}, res_threads(64));
-    else if (dc <= 128) f(Threads<64>{}, Two{}, res_threads(64));
+    if (dc <= 64) f(Threads<64>{}, One{}, block_threads(64));
+    else if (dc <= 128) f(Threads<64>{}, Two{}, block_threads(64));
     else if (dc <= 1024) with_block(dc, One{}, f);
     else f(Threads<1024>{}, Two{}, (int)((dc + 2 * kWave - 1) / (2 * kWave)) * kWave);
 }
@@ -464,7 +405,7 @@ struct ResidualPlan {
 };
 static ResidualPlan plan_bwd(int64_t M, int64_t D, int64_t gate_rows)
 {
-    const int64_t groups = gate_rows > 0 ? gate_rows : 1, per_gate = M / groups, slots = D / 8 <= 128 ? kResWaveRows : 1;  // rows that a block takes at once
+    const int64_t groups = gate_rows > 0 ? gate_rows : 1, per_gate = M / groups, slots = D / 8 <= 128 ? kWaveRows : 1;  // rows that a block takes at once
     const int blocks = D / 8 > 512 ? kResBwdBlocks / 2 : kResBwdBlocks;
     int64_t parts = blocks / groups, most = (per_gate + slots - 1) / slots;
     if (parts > most) parts = most;
@@ -477,7 +418,7 @@ static bool bad_pitch(int64_t ld, int64_t D) { return ld < D || (ld % 8); }
 
 static f8_status check_residual(int64_t M, int64_t D, const void* gate, int64_t gate_rows, float a, float b)
 {
-    if (M < 0 || M > 0x7FFFFFFF || D < 0 || D > kResMaxD || (D % 8) || gate_rows < 0 || gate_rows > 0x7FFFFFFF || gate_rows * D > 0x7FFFFFFFFLL ||
+    if (M < 0 || M > 0x7FFFFFFF || D < 0 || D > kRowMaxD || (D % 8) || gate_rows < 0 || gate_rows > 0x7FFFFFFF || gate_rows * D > 0x7FFFFFFFFLL ||
         (gate != nullptr) != (gate_rows > 0) || (gate_rows > 0 && M % gate_rows) || !(a - a == 0.0f) || !(b - b == 0.0f))
         return F8_ERR_SHAPE;
     return F8_OK;
@@ -519,8 +460,8 @@ f8_status f8_residual_norm(const void* x_bf16, int64_t ldx, const void* y_bf16, 
                                 (const uint4*)g_pre_bf16, M, gate_rows > 0 ? M / gate_rows : M, (int)(D / 8), skip_scale, branch_scale, eps,
                                 1.0f / (float)D, 1.0 / (double)D, (uint16_t*)h_bf16, (uint16_t*)n_bf16, ldh, ldn, rstd_post, rstd_pre,
                                 amax_n ? (uint32_t*)workspace : nullptr};
-        with_fwd_shape(D / 8, [&](auto T, auto U, int threads) {
-            constexpr int kRows = T() == kWave ? kResWaveRows : 1;
+        with_row_shape(D / 8, [&](auto T, auto U, int threads) {
+            constexpr int kRows = T() == kWave ? kWaveRows : 1;
             const int64_t b = (M + kRows - 1) / kRows;
             nb = (int)(b < kResBlocks ? b : kResBlocks);
             const auto kernel = g_post_bf16 ? (g_pre_bf16 ? residual_norm_kernel<T(), U(), true, true> : residual_norm_kernel<T(), U(), true, false>)
@@ -575,19 +516,19 @@ f8_status f8_residual_norm_bwd(const void* h_bf16, int64_t ldh, const void* y_bf
             kernel<<<plan.blocks, threads, 0, st>>>(a);
         });
     }
-    ResidualFinalArgs f = {};
+    ColumnSums f = {};
     if (dg_pre) f.part[f.sets] = sums, f.out[f.sets++] = dg_pre;
     if (dg_post) f.part[f.sets] = sums + set, f.out[f.sets++] = dg_post;
     f.strips = plan.blocks, f.parts = plan.parts, f.part_gate = sums + 2 * set, f.dgate = dgate, f.D = D;
     const int64_t gate_sets = dgate && !direct ? gate_rows : 0;  // (fewer than blocks)
     if (M == 0 && dgate && D > 0) {  // no rows: zeros
-        ResidualFinalArgs z = {};
+        ColumnSums z = {};
         z.dgate = dgate, z.D = gate_rows * D;
-        residual_final_kernel<<<(unsigned)((z.D + kResFinalCols - 1) / kResFinalCols), kResFinalCols * kResFinalGroups, 0, st>>>(z);
+        column_sums(z, 1, st);
     }
     if (f.sets + gate_sets > 0 && D > 0) {
         if (amax_dy) f.partial = maxima, f.npartial = plan.blocks, f.amax = amax_dy;
-        residual_final_kernel<<<dim3((unsigned)((D + kResFinalCols - 1) / kResFinalCols), (unsigned)(f.sets + gate_sets)), kResFinalCols * kResFinalGroups, 0, st>>>(f);
+        column_sums(f, (unsigned)(f.sets + gate_sets), st);
     } else if (amax_dy) {
         amax_final(maxima, D > 0 ? plan.blocks : 0, amax_dy, st);
     }

@@ -15,6 +15,8 @@ TENSORWISE, ROWWISE, COLWISE = 0, 1, 2
 NT, NN, TN = 0, 1, 2
 DYNAMIC, DELAYED, STATIC = 0, 1, 2
 MAX_HISTORY = 1024
+BF16, F32 = 0, 1
+NORM_2, NORM_MAX = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libf8.so")
@@ -32,6 +34,8 @@ EXPORTS = ["f8_workspace_bytes", "f8_status_string", "f8_amax", "f8_scale", "f8_
            "f8_rmsnorm_bwd_add", "f8_linear_fwd_wq", "f8_linear_fwd_noalloc", "f8_linear_fwd_quantise",
            "f8_residual_norm", "f8_residual_norm_bwd", "f8_residual_norm_bwd_workspace_bytes", "f8_logits_workspace_bytes",
            "f8_token_logprobs", "f8_token_logprobs_bwd", "f8_distill", "f8_distill_bwd",
+           "f8_embed", "f8_embed_bwd", "f8_embed_bwd_workspace_bytes", "f8_layernorm", "f8_layernorm_bwd", "f8_layernorm_bwd_workspace_bytes",
+           "f8_grad_norm", "f8_grad_clip", "f8_grad_norm_workspace_bytes",
            "f8_probe_mfma", "f8_probe_copy", "f8_probe_read", "f8_probe_clock"]
 
 
@@ -48,6 +52,10 @@ class QTensorStruct(C.Structure):
 
 class SavedStruct(C.Structure):
     _fields_ = [("x", QTensorStruct), ("w", QTensorStruct), ("dy", QTensorStruct)]
+
+
+class TensorStruct(C.Structure):
+    _fields_ = [("data", _p), ("n", _i64), ("type", C.c_int32)]
 
 
 class LinearDesc(C.Structure):
@@ -131,9 +139,19 @@ def lib():
         l.f8_token_logprobs_bwd.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _p, _p, _p, _p, _i64, _i64, _p, _p, C.c_size_t, _p]
         l.f8_distill.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _i64, _int, f, _p, _p, _p, _p, _p, C.c_size_t, _p]
         l.f8_distill_bwd.argtypes = [_p, _i64, _i64, _i64, f, _p, _p, _i64, _int, f, _p, _p, _p, _p, _p, _i64, _i64, _p, _p, C.c_size_t, _p]
+        l.f8_embed.argtypes = [_p, _i64, _p, _i64, _i64, _i64, f, _p, _i64, _p]
+        l.f8_embed_bwd.argtypes = [_p, _i64, _p, _i64, _i64, _i64, f, _int, _p, _i64, _p, C.c_size_t, _p]
+        l.f8_embed_bwd_workspace_bytes.argtypes = [_i64] * 3
+        l.f8_layernorm.argtypes = [_p, _i64, _p, _i64, _i64, _i64, _p, _p, f, _p, _i64, _p, _i64, _p, _p, _p, _p, C.c_size_t, _p]
+        l.f8_layernorm_bwd.argtypes = [_p, _i64, _p, _p, _p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _p, _p, _p, _p, C.c_size_t, _p]
+        l.f8_layernorm_bwd_workspace_bytes.argtypes = [_i64] * 2
+        l.f8_grad_norm.argtypes = [_p, _i64, _int, _p, _p, _p, C.c_size_t, _p]
+        l.f8_grad_clip.argtypes = [_p, _p, _i64, _p, f, _p]
+        l.f8_grad_norm_workspace_bytes.argtypes = [_p, _i64]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = _int
-        for name in ("f8_sdpa_bwd_workspace_bytes", "f8_residual_norm_bwd_workspace_bytes", "f8_logits_workspace_bytes"):
+        for name in ("f8_sdpa_bwd_workspace_bytes", "f8_residual_norm_bwd_workspace_bytes", "f8_logits_workspace_bytes",
+                     "f8_embed_bwd_workspace_bytes", "f8_layernorm_bwd_workspace_bytes", "f8_grad_norm_workspace_bytes"):
             getattr(l, name).restype = C.c_size_t
         _lib = l
     return _lib
@@ -529,6 +547,15 @@ def _rows(name, t, shape, dev):
     _refuse(name, t, _BF16, shape)
 
 
+def _wide_rows(name, t, dtype, shape, dev):
+    """_rows of a matrix of another type."""
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape:
+        ld, step = t.stride()
+        if step == 1 or shape[1] <= 1:
+            return t.data_ptr(), ld if shape[0] > 1 else (max(ld, shape[1]) + 7) // 8 * 8
+    _refuse(name, t, dtype, shape)
+
+
 def _room(ws, dev):
     """Address and bytes of a workspace."""
     if ws is None:
@@ -631,6 +658,99 @@ def distill_bwd(logits, vocab, teacher_ids, teacher_logp, stats, dlogits, d_loss
                                 _packed("teacher_logp", teacher_logp, _F32, (M, K), dev), K, int(bool(tail)), teacher_scale, _packed("targets", targets, _I64, of_m, dev),
                                 _packed("stats", stats, _F32, (M, 4), dev), _packed("d_loss", d_loss, _F32, of_m, dev), _packed("d_logp", d_logp, _F32, of_m, dev),
                                 *_rows("dlogits", dlogits, (M, cols), dev), cols, _packed("amax_d", amax_d, _F32, (1,), dev), wp, wb, _stream(stream)))
+
+
+# ---- token embeddings, layer norm, the norm of all gradients --------------------------------
+
+def embed(ids, table, out, scale=1.0, stream=None):
+    """out[m] = scale table[ids[m]].  ids: [M] int64 (negative: no token); table [V, D], out [M, D]."""
+    (M,), (V, D), dev = ids.shape, table.shape, _current()
+    tp, ldt = _rows("table", table, (V, D), dev)
+    op, ldo = _rows("out", out, (M, D), dev)
+    _check(lib().f8_embed(_packed("ids", ids, _I64, (M,), dev), M, tp, ldt, V, D, scale, op, ldo, _stream(stream)))
+
+
+def embed_bwd_workspace_bytes(M, vocab, D):
+    return int(lib().f8_embed_bwd_workspace_bytes(M, vocab, D))
+
+
+def embed_bwd(ids, dout, dtable, scale=1.0, workspace=None, stream=None):
+    """dtable: [V, D], bf16 or fp32; all its rows are written."""
+    (M,), (V, D), dev = ids.shape, dtable.shape, _current()
+    dp, lddo = _rows("dout", dout, (M, D), dev)
+    wide = dtable.dtype is _F32
+    tp, ldt = _wide_rows("dtable", dtable, _F32 if wide else _BF16, (V, D), dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_embed_bwd(_packed("ids", ids, _I64, (M,), dev), M, dp, lddo, V, D, scale, F32 if wide else BF16, tp, ldt, wp, wb, _stream(stream)))
+
+
+def layernorm(x, g, n, b=None, y=None, h=None, eps=1e-5, mean=None, rstd=None, amax_n=None, workspace=None, stream=None):
+    """h = x + y (x itself without y); n = (h - mean) rstd g + b."""
+    shape = M, D = x.shape
+    of_d, of_m, dev = (D,), (M,), _current()
+    (xp, ldx), (yp, ldy), (hp, ldh), (np_, ldn) = _rows("x", x, shape, dev), _rows("y", y, shape, dev), _rows("h", h, shape, dev), _rows("n", n, shape, dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_layernorm(xp, ldx, yp, ldy, M, D, _packed("g", g, _BF16, of_d, dev), _packed("b", b, _BF16, of_d, dev), eps, hp, ldh, np_, ldn,
+                              _packed("mean", mean, _F32, of_m, dev), _packed("rstd", rstd, _F32, of_m, dev), _packed("amax_n", amax_n, _F32, (1,), dev), wp, wb,
+                              _stream(stream)))
+
+
+def layernorm_bwd_workspace_bytes(M, D):
+    return int(lib().f8_layernorm_bwd_workspace_bytes(M, D))
+
+
+def layernorm_bwd(h, g, mean, rstd, dn, dx=None, dh=None, dg=None, db=None, amax_dx=None, workspace=None, stream=None):
+    """h: what was normalised (x + y, or x); dh: its gradient through the residual stream."""
+    shape = M, D = dn.shape
+    of_d, of_m, dev = (D,), (M,), _current()
+    (hp, ldh), (np_, lddn), (ap, lddh), (xp, lddx) = _rows("h", h, shape, dev), _rows("dn", dn, shape, dev), _rows("dh", dh, shape, dev), _rows("dx", dx, shape, dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_layernorm_bwd(hp, ldh, _packed("g", g, _BF16, of_d, dev), _packed("mean", mean, _F32, of_m, dev), _packed("rstd", rstd, _F32, of_m, dev), np_, lddn,
+                                  ap, lddh, M, D, xp, lddx, _packed("dg", dg, _F32, of_d, dev), _packed("db", db, _F32, of_d, dev),
+                                  _packed("amax_dx", amax_dx, _F32, (1,), dev), wp, wb, _stream(stream)))
+
+
+class GradList:
+    """A list of tensors (f8_tensor): contiguous, bf16 or fp32, on one GPU, at any address.  It keeps them alive; a tensor whose
+    memory is replaced (resized, set to other data) needs a new list."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.device = self.tensors[0].get_device() if self.tensors else None
+        for i, t in enumerate(self.tensors):
+            if t.dtype not in (_BF16, _F32) or not t.is_cuda or t.get_device() != self.device or not t.is_contiguous():
+                raise F8Error(F8_ERR_SHAPE, f"tensor {i} of a list: a contiguous tensor of bf16 or fp32 on the list's GPU is wanted; got {t.dtype}, "
+                                            f"{tuple(t.shape)}, strides {t.stride()} on {t.device}")
+        self._struct = (TensorStruct * len(self.tensors))(*[(t.data_ptr(), t.numel(), F32 if t.dtype is _F32 else BF16) for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def struct(self, name, dev):
+        if self.tensors and self.device != dev:
+            raise F8Error(F8_ERR_SHAPE, f"{name}: tensors on device {self.device}, not on the current one, {dev}")
+        return C.addressof(self._struct)
+
+
+def grad_norm_workspace_bytes(grads):
+    return int(lib().f8_grad_norm_workspace_bytes(C.addressof(grads._struct), len(grads)))
+
+
+def grad_norm(grads, norm=None, total=None, kind=NORM_2, workspace=None, stream=None):
+    """grads: GradList; norm [1] fp32; total [1] fp64: the sum of squares (NORM_MAX: the largest magnitude), e.g. for a reduction over ranks."""
+    dev = _current()
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_grad_norm(grads.struct("grads", dev), len(grads), kind, _packed("norm", norm, _F32, (1,), dev), _packed("total", total, torch.float64, (1,), dev),
+                              wp, wb, _stream(stream)))
+
+
+def grad_clip(grads, norm, most, out=None, stream=None):
+    """grads scaled by min(1, most / (norm + 1e-6)), in place or into the tensors of `out` (a GradList of the same sizes and types)."""
+    dev = _current()
+    if out is not None and len(out) != len(grads):
+        raise F8Error(F8_ERR_SHAPE, f"{len(out)} tensors for {len(grads)}")
+    _check(lib().f8_grad_clip(grads.struct("grads", dev), None if out is None else out.struct("out", dev), len(grads), _packed("norm", norm, _F32, (1,), dev), most,
+                              _stream(stream)))
 
 
 # ---- measuring helpers ---------------------------------------------------------------

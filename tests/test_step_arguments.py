@@ -1,0 +1,114 @@
+"""Refusals of f8.embed, f8.layernorm, f8.grad_norm and their companions: on the host, before any launch (no GPU)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2410_06511_amd import f8
+
+FAKE = 0x10000  # a 16-byte aligned non-NULL address that is never dereferenced on these paths
+NULL, SHAPE, ALIGN, ENUM, WORKSPACE = 1, 2, 3, 4, 5
+INF, NAN = float("inf"), float("nan")
+
+
+def call(f, defaults, **change):
+    args = dict(defaults)
+    assert set(change) <= set(args)
+    args.update(change)
+    return getattr(f8.lib(), f)(*args.values())
+
+
+EMBED = dict(ids=FAKE, M=5, table=FAKE, ldt=64, V=100, D=64, scale=1.0, out=FAKE, ldo=64, stream=None)
+EMBED_BWD = dict(ids=FAKE, M=5, dout=FAKE, lddo=64, V=100, D=64, scale=1.0, type=0, dtable=FAKE, ldt=64, ws=None, wb=0, stream=None)
+COMMON = [(SHAPE, dict(M=-1)), (SHAPE, dict(M=1 << 31)), (SHAPE, dict(V=-1)), (SHAPE, dict(V=1 << 31)), (SHAPE, dict(D=60)), (SHAPE, dict(D=-8)),
+          (SHAPE, dict(D=(1 << 20) + 8)), (SHAPE, dict(scale=INF)), (SHAPE, dict(scale=NAN)), (SHAPE, dict(ldt=56)), (SHAPE, dict(ldt=68)), (NULL, dict(ids=None)),
+          (ALIGN, dict(ids=FAKE + 4))]
+
+
+@pytest.mark.parametrize("status,change", COMMON + [
+    (NULL, dict(table=None)), (NULL, dict(out=None)), (SHAPE, dict(ldo=32)), (SHAPE, dict(ldo=65)), (ALIGN, dict(table=FAKE + 8)), (ALIGN, dict(out=FAKE + 2)),
+    (SHAPE, dict(M=0x7FFFFFFF, D=1 << 20, ldt=1 << 20, ldo=1 << 20))])
+def test_embed(status, change):
+    assert call("f8_embed", EMBED, **change) == status
+
+
+@pytest.mark.parametrize("status,change", COMMON + [
+    (NULL, dict(dout=None)), (NULL, dict(dtable=None)), (SHAPE, dict(lddo=32)), (SHAPE, dict(lddo=65)), (ALIGN, dict(dtable=FAKE + 8)), (ALIGN, dict(dout=FAKE + 2)),
+    (ENUM, dict(type=2)), (ENUM, dict(type=-1)), (WORKSPACE, dict()), (WORKSPACE, dict(ws=FAKE, wb=8192)), (ALIGN, dict(ws=FAKE + 8, wb=1 << 30))])
+def test_embed_bwd(status, change):
+    assert call("f8_embed_bwd", EMBED_BWD, **change) == status
+
+
+def test_embed_workspace():
+    assert f8.embed_bwd_workspace_bytes(0, 100, 64) >= 8192 and f8.embed_bwd_workspace_bytes(-1, 100, 64) == 8192
+    for M in (1, 4096, 4097, 1 << 20):   # sorted lists, and no more than the tokens' own gradients for the sums
+        size = f8.embed_bwd_workspace_bytes(M, 1000, 512)
+        assert 2 * 4 * M <= size <= 8192 + 4 * (4 * M + 256) + (M // 8 + 1) * 2 * 512 * 4
+
+
+NORM = dict(x=FAKE, ldx=64, y=FAKE, ldy=64, M=5, D=64, g=FAKE, b=FAKE, eps=1e-5, h=FAKE, ldh=64, n=FAKE, ldn=64, mean=FAKE, rstd=FAKE, amax=FAKE, ws=None, wb=0,
+            stream=None)
+NORM_BWD = dict(h=FAKE, ldh=64, g=FAKE, mean=FAKE, rstd=FAKE, dn=FAKE, lddn=64, dh=FAKE, lddh=64, M=5, D=64, dx=FAKE, lddx=64, dg=FAKE, db=FAKE, amax=FAKE, ws=None,
+                wb=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (NULL, dict(x=None)), (NULL, dict(n=None)), (NULL, dict(g=None)), (NULL, dict(y=None)), (NULL, dict(h=None)), (SHAPE, dict(M=-1)), (SHAPE, dict(M=1 << 31)),
+    (SHAPE, dict(D=60)), (SHAPE, dict(D=-8)), (SHAPE, dict(D=16392, ldx=16392, ldy=16392, ldh=16392, ldn=16392)), (SHAPE, dict(eps=-1.0)), (SHAPE, dict(eps=NAN)),
+    (SHAPE, dict(eps=INF)), (SHAPE, dict(ldx=56)), (SHAPE, dict(ldy=68)), (SHAPE, dict(ldh=0)), (SHAPE, dict(ldn=63)), (ALIGN, dict(x=FAKE + 8)), (ALIGN, dict(y=FAKE + 8)),
+    (ALIGN, dict(h=FAKE + 8)), (ALIGN, dict(n=FAKE + 2)), (ALIGN, dict(g=FAKE + 4)), (ALIGN, dict(b=FAKE + 4)), (WORKSPACE, dict()), (WORKSPACE, dict(ws=FAKE, wb=4096)),
+    (ALIGN, dict(ws=FAKE + 4, wb=8192))])
+def test_layernorm(status, change):
+    assert call("f8_layernorm", NORM, **change) == status
+
+
+@pytest.mark.parametrize("status,change", [
+    (NULL, dict(h=None)), (NULL, dict(g=None)), (NULL, dict(mean=None)), (NULL, dict(rstd=None)), (NULL, dict(dn=None)), (NULL, dict(dx=None)),
+    (NULL, dict(dx=None, dh=None)), (NULL, dict(dx=None, dh=None, amax=None, dg=None, db=None)), (SHAPE, dict(M=-1)), (SHAPE, dict(D=4)), (SHAPE, dict(ldh=32)),
+    (SHAPE, dict(lddn=66)), (SHAPE, dict(lddh=8)), (SHAPE, dict(lddx=60)), (ALIGN, dict(dx=FAKE + 8)), (ALIGN, dict(dh=FAKE + 8)), (ALIGN, dict(dn=FAKE + 8)),
+    (ALIGN, dict(h=FAKE + 8)), (ALIGN, dict(ws=FAKE + 8, wb=1 << 30)), (WORKSPACE, dict()), (WORKSPACE, dict(ws=FAKE, wb=8192))])
+def test_layernorm_bwd(status, change):
+    assert call("f8_layernorm_bwd", NORM_BWD, **change) == status
+
+
+def tensors(*entries):
+    return (f8.TensorStruct * len(entries))(*entries)
+
+
+@pytest.mark.parametrize("status,entry", [(SHAPE, (FAKE, -1, 0)), (SHAPE, (FAKE, (1 << 40) + 1, 0)), (NULL, (None, 3, 0)), (ENUM, (FAKE, 3, 2)), (ENUM, (FAKE, 3, -1)),
+                                          (ALIGN, (FAKE + 1, 3, 0)), (ALIGN, (FAKE + 2, 3, 1))])
+def test_grad_lists(status, entry):
+    bad, good = tensors((FAKE, 8, 1), entry), tensors((FAKE, 8, 1), (FAKE + (1 << 20), entry[1], entry[2]))
+    l = f8.lib()
+    assert l.f8_grad_norm(bad, 2, 0, FAKE, None, FAKE, 1 << 30, None) == status
+    assert l.f8_grad_clip(bad, None, 2, FAKE, 1.0, None) == status and l.f8_grad_clip(tensors((FAKE, 8, 1), (FAKE, 3, 0)), bad, 2, FAKE, 1.0, None) == status
+    assert l.f8_grad_norm_workspace_bytes(bad, 2) == 8192 and good is not None
+
+
+def test_grad_arguments():
+    l, t = f8.lib(), tensors((FAKE, 8, 1), (FAKE + 2, 3, 0))
+    assert l.f8_grad_norm(None, 2, 0, FAKE, None, FAKE, 1 << 30, None) == NULL and l.f8_grad_norm(t, -1, 0, FAKE, None, FAKE, 1 << 30, None) == SHAPE
+    assert l.f8_grad_norm(t, 2, 2, FAKE, None, FAKE, 1 << 30, None) == ENUM and l.f8_grad_norm(t, 2, 0, None, None, FAKE, 1 << 30, None) == NULL
+    assert l.f8_grad_norm(t, 2, 0, FAKE, None, None, 0, None) == WORKSPACE and l.f8_grad_norm(t, 2, 0, FAKE, None, FAKE, 4096, None) == WORKSPACE
+    assert l.f8_grad_norm(t, 2, 0, FAKE + 2, None, FAKE, 8192, None) == ALIGN and l.f8_grad_norm(t, 2, 0, FAKE, FAKE + 4, FAKE, 8192, None) == ALIGN
+    assert l.f8_grad_clip(t, None, 2, None, 1.0, None) == NULL and l.f8_grad_clip(t, None, 2, FAKE, -1.0, None) == SHAPE and l.f8_grad_clip(t, None, 2, FAKE, NAN, None) == SHAPE
+    clip = lambda out: l.f8_grad_clip(t, out, 2, FAKE, 1.0, None)
+    assert clip(tensors((FAKE, 8, 0), (FAKE + 2, 3, 0))) == ENUM and clip(tensors((FAKE, 7, 1), (FAKE + 2, 3, 0))) == SHAPE
+    assert clip(tensors((FAKE + 4, 8, 1), (FAKE + 2, 3, 0))) == SHAPE   # half over its own input
+
+
+def test_large_lists_have_room_for_every_launch():
+    n = 1000
+    t = tensors(*[(FAKE, 1 << 34, 0)] * n)
+    assert f8.lib().f8_grad_norm_workspace_bytes(t, n) >= 8 * 2048 * (n // 96)
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    bf, f32 = torch.zeros((4, 16), dtype=torch.bfloat16), torch.zeros(4)
+    for call_ in (lambda: f8.embed(torch.zeros(4, dtype=torch.int64), bf, bf), lambda: f8.embed(torch.zeros(4, dtype=torch.int32), bf, bf),
+                  lambda: f8.embed_bwd(torch.zeros(4, dtype=torch.int64), bf, bf), lambda: f8.embed_bwd(torch.zeros(4, dtype=torch.int64), bf, bf.half()),
+                  lambda: f8.layernorm(bf, bf[0], bf), lambda: f8.layernorm_bwd(bf, bf[0], f32, f32, bf, bf), lambda: f8.GradList([f32]),
+                  lambda: f8.GradList([torch.zeros(4, dtype=torch.float16)])):
+        with pytest.raises(f8.F8Error) as e:
+            call_()
+        assert e.value.code == SHAPE
