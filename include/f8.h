@@ -791,6 +791,70 @@ f8_status f8_linear_fwd_xq(const f8_linear_desc* d, const f8_scaling_state* stat
                            void* stream);
 
 /*
+ * Microscaled 4-bit linear: the Float8 linear's narrower sibling, on the OCP
+ * microscaling format MXFP4.  An element is E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives), and 32 consecutive ones along the contraction share a scale
+ * 2^e, stored as the E8M0 byte e + 127 (255: NaN):
+ *   e = max(floor(log2(max |x|)) - 2, -127)  (a block of zeros: -127),
+ *   code = E2M1 nearest to x * 2^-e, ties to the even code, magnitudes above 6: 6.
+ * A block with an infinity or a NaN has the scale NaN.
+ *
+ * f8_mx4: the codes of T[rows, cols] bf16, along either or both of its sides:
+ *   q  [rows, 16 * ceil(cols / 32)] bytes: blocks along the columns, element 2 i of
+ *     a row in the low nibble of byte i, the last block padded with zeros;
+ *   s  f8_mx4_scale_bytes(rows, cols) bytes: with R = rows rounded up to 64, the
+ *     scale of row r's block b at byte ((b / 16) * R + r) * 16 + 4 * (b % 4) +
+ *     (b % 16) / 4 (the order in which the product takes them; bytes of no block
+ *     hold 127);
+ *   q_t [cols, 16 * ceil(rows / 32)], s_t f8_mx4_scale_bytes(cols, rows): the same
+ *     of T's transpose: blocks along the rows, with scales and codes of their own.
+ * A pair (q, s) or (q_t, s_t) may be NULL where it is not wanted.
+ *
+ * f8_mx4_quantise: T (row pitch ld) into the pairs that are given, one reading for
+ *   both.  Any rows >= 0; cols a multiple of 16, ld of 8.
+ * f8_mx4_dequantise: the values of one pair as bf16 (exact): q, s of [rows, cols],
+ *   or q_t, s_t with rows and cols exchanged.  cols and ldo multiples of 8.
+ * f8_mx4_gemm: D[m, n] = bf16(sum_k A[m, k] B[n, k]), A [M, K] and B [N, K] as q, s
+ *   (packed), D with row pitch ldd; fp32 accumulation.  Any M and K >= 0; N a
+ *   multiple of 16, ldd of 8.  workspace (nullable, any size, 16-byte aligned): as in
+ *   f8_gemm_ws, a product with few output tiles and a long contraction may be
+ *   computed in ranges whose fp32 sums go there; f8_mx4_workspace_bytes(M, K, N) is
+ *   enough for the three products of a linear.  Results are reproducible; they
+ *   depend, within accumulation rounding, on the workspace's size.
+ * f8_mx4_linear_fwd: quantises X [M, K] and W [N, K] (bf16, packed) into saved->x
+ *   and saved->w (each of the pairs that are given; q and s are needed, q_t and s_t
+ *   for a backward), then Y [M, N] = X4 W4^T.  W NULL: saved->w holds the codes of
+ *   an earlier call or of f8_mx4_quantise.
+ * f8_mx4_linear_bwd: quantises dY [M, N] into saved->dy, then dX [M, K] = dY4 W4 from
+ *   dy.q and w.q_t (blocks along N), and dW [N, K] = dY4^T X4 from dy.q_t and x.q_t
+ *   (blocks along M).  dX or dW may be NULL, and the pairs for it.
+ * M any number >= 0, K and N multiples of 16; all below 2^23.
+ */
+typedef struct f8_mx4 {
+    uint8_t* q;
+    uint8_t* s;
+    uint8_t* q_t;
+    uint8_t* s_t;
+} f8_mx4;
+typedef struct f8_mx4_saved {
+    f8_mx4 x, w, dy;
+} f8_mx4_saved;
+typedef struct f8_mx4_desc {
+    int64_t M, K, N;
+} f8_mx4_desc;
+size_t f8_mx4_scale_bytes(int64_t rows, int64_t cols);
+size_t f8_mx4_workspace_bytes(int64_t M, int64_t K, int64_t N);
+f8_status f8_mx4_quantise(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, const f8_mx4* out, void* stream);
+f8_status f8_mx4_dequantise(const uint8_t* q, const uint8_t* s, int64_t rows, int64_t cols, void* out_bf16, int64_t ldo,
+                            void* stream);
+f8_status f8_mx4_gemm(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* sa, const uint8_t* B, const uint8_t* sb,
+                      void* D_bf16, int64_t ldd, void* workspace, size_t workspace_bytes, void* stream);
+f8_status f8_mx4_linear_fwd(const f8_mx4_desc* d, const void* X, const void* W, void* Y, const f8_mx4_saved* saved,
+                            void* workspace, size_t workspace_bytes, void* stream);
+f8_status f8_mx4_linear_bwd(const f8_mx4_desc* d, const void* dY, const f8_mx4_saved* saved, void* dX, void* dW,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measuring helpers (not part of the linear layer): what the chip delivers
  * with nothing else in the way, so that a benchmark can quote the kernels
  * above against measured ceilings beside the nominal peaks.

@@ -1,0 +1,223 @@
+// Quantisation to microscaled 4-bit blocks and back, and the linear on them:
+//   a block's scale is 2^e with e = floor(log2(largest magnitude)) - 2 (at least -127), so that the largest lies in [4, 8);
+//   code = the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| 2^-e, ties to the even code, above 6: 6; a block with an infinity or
+//   a NaN has the scale NaN.
+// Forward Y = X4 W4^T with blocks along K; backward dX = dY4 W4^T with blocks along N and dW = dY4^T X4 with blocks along M: a
+// tensor's other orientation has codes of its own, and one reading of the tensor gives both.
+// The cast is bound by memory: 2 bytes an element read, 17/32 for each orientation written.
+#include "f8_device.hpp"
+#include "f8_mx4.hpp"
+#include "f8_mx4_device.hpp"
+
+namespace f8 {
+
+struct Mx4Cast {
+    const uint16_t* x;
+    int64_t ld;
+    int rows, cols;
+    uint8_t *q, *s, *q_t, *s_t;  // either orientation nullable
+    int tiles_c, blocks;
+};
+
+// Tiles of 128 x 128.  Along the rows a thread has whole blocks of 32 as they lie in memory; for the other orientation the tile
+// goes through LDS, where a thread takes 32 rows of two columns.
+constexpr int kMxTile = 128;
+
+__device__ inline void mx4_cast_tile(const Mx4Cast& p, int block, uint32_t (&tile)[kMxTile][kMxTile / 2])
+{
+    const int t = threadIdx.x, r0 = block / p.tiles_c * kMxTile, c0 = block % p.tiles_c * kMxTile;
+    const bool turn = p.q_t != nullptr;
+    const int64_t pitch = mx4_pitch(p.cols), srows = mx4_rows(p.rows);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = i * 64 + t / 4, b = t % 4, row = r0 + r, col = c0 + 32 * b;
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = make_uint4(0, 0, 0, 0);
+            if (row < p.rows && col + 8 * k < p.cols) v[k] = *reinterpret_cast<const uint4*>(p.x + (int64_t)row * p.ld + col + 8 * k);
+        }
+        if (turn) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(&tile[r][16 * b + 4 * k]) = v[k];
+        }
+        if (p.q) {
+            const uint32_t code = mx4_scale_of(v);
+            if (row < p.rows && col < p.cols) *reinterpret_cast<uint4*>(p.q + row * pitch + col / 2) = mx4_encode(v, code);
+            // (rows of padding too, and blocks up to the group's end)
+            if (row < srows && col < (p.cols + kMxGroup - 1) / kMxGroup * kMxGroup)
+                p.s[mx4_scale_at(srows, row, col / kMxBlock)] = (uint8_t)(row < p.rows && col < p.cols ? code : 127);
+        }
+    }
+    if (!turn) return;
+    __syncthreads();
+    const int wave = t / kWave, lane = t % kWave, rb = r0 / kMxBlock + wave;  // 32 rows of the columns 2 lane, 2 lane + 1
+    const int64_t pitch_t = mx4_pitch(p.rows), srows_t = mx4_rows(p.cols);
+    uint32_t w[32];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) w[k] = tile[32 * wave + k][lane];
+    uint4 v[2][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a = w[8 * k + 2 * j], b = w[8 * k + 2 * j + 1];
+            lo[j] = (a & 0xFFFFu) | (b << 16), hi[j] = (a >> 16) | (b & 0xFFFF0000u);
+        }
+        v[0][k] = make_uint4(lo[0], lo[1], lo[2], lo[3]), v[1][k] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int col = c0 + 2 * lane + h;
+        const bool real = col < p.cols && rb * kMxBlock < p.rows;
+        const uint32_t code = mx4_scale_of(v[h]);
+        if (real) *reinterpret_cast<uint4*>(p.q_t + col * pitch_t + (int64_t)rb * 16) = mx4_encode(v[h], code);
+        if (col < srows_t && rb * kMxBlock < (p.rows + kMxGroup - 1) / kMxGroup * kMxGroup) p.s_t[mx4_scale_at(srows_t, col, rb)] = (uint8_t)(real ? code : 127);
+    }
+}
+
+// One or two tensors: the first a.blocks blocks of the grid are the first one's.
+__global__ __launch_bounds__(256) void mx4_cast_kernel(const Mx4Cast a, const Mx4Cast b)
+{
+    __shared__ __attribute__((aligned(16))) uint32_t tile[kMxTile][kMxTile / 2];
+    if ((int)blockIdx.x < a.blocks) mx4_cast_tile(a, (int)blockIdx.x, tile);
+    else mx4_cast_tile(b, (int)blockIdx.x - a.blocks, tile);
+}
+
+__global__ __launch_bounds__(256) void mx4_decode_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, int rows, int cols, uint16_t* out, int64_t ldo)
+{
+    const int blocks = (cols + kMxBlock - 1) / kMxBlock;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)rows * blocks) return;
+    const int row = (int)(i / blocks), b = (int)(i % blocks);
+    const uint4 codes = *reinterpret_cast<const uint4*>(q + row * mx4_pitch(cols) + 16 * (int64_t)b);
+    const uint32_t e = s[mx4_scale_at(mx4_rows(rows), row, b)];
+    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (32 * b + 8 * k < cols) *reinterpret_cast<uint4*>(out + (int64_t)row * ldo + 32 * b + 8 * k) = mx4_decode8(w[k], e);
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+
+// Blocks: enough tiles for the codes of both orientations, their padding and the scales' (a group of 512 past the end, and 64 rows).
+static Mx4Cast cast_of(const void* x, int64_t rows, int64_t cols, int64_t ld, const f8_mx4& o)
+{
+    const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m * m; };
+    const int64_t r = o.q_t ? up(rows, kMxGroup) : up(rows, kMxTile), c = o.q ? up(cols, kMxGroup) : up(cols, kMxTile);
+    const int64_t tiles_c = c / kMxTile, tiles = rows > 0 && cols > 0 ? r / kMxTile * tiles_c : 0;
+    return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)tiles_c, (int)tiles};
+}
+static bool too_many(int64_t rows, int64_t cols) { return (rows / kMxTile + 4) * (cols / kMxTile + 4) > 0x3FFFFFFF; }
+static void launch_cast(const Mx4Cast& a, const Mx4Cast& b, hipStream_t st)
+{
+    if (a.blocks + b.blocks > 0) mx4_cast_kernel<<<(unsigned)(a.blocks + b.blocks), 256, 0, st>>>(a, b);
+}
+
+static f8_status check_codes(const f8_mx4* t, bool along_cols, bool along_rows)
+{
+    if (!t || (along_cols && (!t->q || !t->s)) || (along_rows && (!t->q_t || !t->s_t))) return F8_ERR_NULL;
+    if ((t->q != nullptr) != (t->s != nullptr) || (t->q_t != nullptr) != (t->s_t != nullptr)) return F8_ERR_NULL;
+    if (!aligned16(t->q) || !aligned16(t->s) || !aligned16(t->q_t) || !aligned16(t->s_t)) return F8_ERR_ALIGN;
+    return F8_OK;
+}
+static bool bad_desc(const f8_mx4_desc* d)
+{
+    return d->M < 0 || d->K < 0 || d->N < 0 || d->M >= kMxMax || d->K >= kMxMax || d->N >= kMxMax || (d->K % 16) || (d->N % 16) || too_many(d->M, d->K) ||
+           too_many(d->M, d->N) || too_many(d->N, d->K);
+}
+
+}  // namespace f8
+
+using namespace f8;
+
+extern "C" {
+
+size_t f8_mx4_scale_bytes(int64_t rows, int64_t cols)
+{
+    if (rows < 0 || cols < 0 || rows >= kMxMax || cols >= kMxMax) return 0;
+    return mx4_scale_bytes(rows, cols);
+}
+
+size_t f8_mx4_workspace_bytes(int64_t M, int64_t K, int64_t N)
+{
+    size_t most = kMinWorkspaceBytes;
+    if (M < 0 || K < 0 || N < 0 || M >= kMxMax || K >= kMxMax || N >= kMxMax) return most;
+    for (const size_t b : {mx4_split_bytes(M, N, K), mx4_split_bytes(M, K, N), mx4_split_bytes(N, K, M)}) most = b > most ? b : most;
+    return most;
+}
+
+f8_status f8_mx4_quantise(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, const f8_mx4* out, void* stream)
+{
+    if (rows < 0 || cols < 0 || rows >= kMxMax || cols >= kMxMax || (cols % 16) || ld < cols || (ld % 8) || too_many(rows, cols)) return F8_ERR_SHAPE;
+    const f8_status s = check_codes(out, false, false);
+    if (s != F8_OK) return s;
+    if (!out->q && !out->q_t) return F8_ERR_NULL;
+    if (rows && cols && !x_bf16) return F8_ERR_NULL;
+    if (!aligned16(x_bf16)) return F8_ERR_ALIGN;
+    launch_cast(cast_of(x_bf16, rows, cols, ld, *out), Mx4Cast{}, (hipStream_t)stream);
+    return last_launch_status();
+}
+
+f8_status f8_mx4_dequantise(const uint8_t* q, const uint8_t* s, int64_t rows, int64_t cols, void* out_bf16, int64_t ldo, void* stream)
+{
+    if (rows < 0 || cols < 0 || rows >= kMxMax || cols >= kMxMax || (cols % 8) || ldo < cols || (ldo % 8)) return F8_ERR_SHAPE;
+    const int64_t blocks = (rows * ((cols + kMxBlock - 1) / kMxBlock) + 255) / 256;
+    if (blocks > 0x7FFFFFFF) return F8_ERR_SHAPE;
+    if (rows && cols && (!q || !s || !out_bf16)) return F8_ERR_NULL;
+    if (!aligned16(q) || !aligned16(s) || !aligned16(out_bf16)) return F8_ERR_ALIGN;
+    if (blocks) mx4_decode_kernel<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(q, s, (int)rows, (int)cols, (uint16_t*)out_bf16, ldo);
+    return last_launch_status();
+}
+
+f8_status f8_mx4_gemm(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* sa, const uint8_t* B, const uint8_t* sb, void* D_bf16, int64_t ldd,
+                      void* workspace, size_t workspace_bytes_, void* stream)
+{
+    if (M < 0 || N < 0 || K < 0 || M >= kMxMax || N >= kMxMax || K >= kMxMax || (N % 16) || ldd < N || (ldd % 8) || ldd >= kMxMax) return F8_ERR_SHAPE;
+    if (((M + 63) / 64) * ((N + 63) / 64) > (int64_t)0x7FFFFFFF) return F8_ERR_SHAPE;
+    if (M && N && (!D_bf16 || (K && (!A || !sa || !B || !sb)))) return F8_ERR_NULL;
+    if (!aligned16(A) || !aligned16(sa) || !aligned16(B) || !aligned16(sb) || !aligned16(D_bf16) || !aligned16(workspace)) return F8_ERR_ALIGN;
+    return mx4_gemm({(int)M, (int)N, (int)K, A, sa, B, sb, (uint16_t*)D_bf16, ldd}, workspace, workspace ? workspace_bytes_ : 0, (hipStream_t)stream);
+}
+
+f8_status f8_mx4_linear_fwd(const f8_mx4_desc* d, const void* X, const void* W, void* Y, const f8_mx4_saved* saved, void* workspace, size_t workspace_bytes_,
+                            void* stream)
+{
+    if (!d || !saved) return F8_ERR_NULL;
+    if (bad_desc(d)) return F8_ERR_SHAPE;
+    f8_status s = check_codes(&saved->x, true, false);
+    if (s != F8_OK || (s = check_codes(&saved->w, true, false)) != F8_OK) return s;
+    if (d->M && ((d->K && !X) || (d->N && !Y))) return F8_ERR_NULL;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(workspace)) return F8_ERR_ALIGN;
+    hipStream_t st = (hipStream_t)stream;
+    const Mx4Cast x = cast_of(X, d->M, d->K, d->K, saved->x), w = W ? cast_of(W, d->N, d->K, d->K, saved->w) : Mx4Cast{};
+    launch_cast(x, w, st);
+    s = last_launch_status();
+    if (s != F8_OK) return s;
+    return mx4_gemm({(int)d->M, (int)d->N, (int)d->K, saved->x.q, saved->x.s, saved->w.q, saved->w.s, (uint16_t*)Y, d->N}, workspace,
+                    workspace ? workspace_bytes_ : 0, st);
+}
+
+f8_status f8_mx4_linear_bwd(const f8_mx4_desc* d, const void* dY, const f8_mx4_saved* saved, void* dX, void* dW, void* workspace, size_t workspace_bytes_,
+                            void* stream)
+{
+    if (!d || !saved || (!dX && !dW)) return F8_ERR_NULL;
+    if (bad_desc(d)) return F8_ERR_SHAPE;
+    f8_mx4 dy = saved->dy;
+    f8_status s = check_codes(&dy, dX != nullptr, dW != nullptr);
+    if (s != F8_OK || (dX && (s = check_codes(&saved->w, false, true)) != F8_OK) || (dW && (s = check_codes(&saved->x, false, true)) != F8_OK)) return s;
+    if (d->M && d->N && !dY) return F8_ERR_NULL;
+    if (!aligned16(dY) || !aligned16(dX) || !aligned16(dW) || !aligned16(workspace)) return F8_ERR_ALIGN;
+    if (!dX) dy.q = dy.s = nullptr;
+    if (!dW) dy.q_t = dy.s_t = nullptr;
+    hipStream_t st = (hipStream_t)stream;
+    const size_t room = workspace ? workspace_bytes_ : 0;
+    launch_cast(cast_of(dY, d->M, d->N, d->N, dy), Mx4Cast{}, st);
+    s = last_launch_status();
+    if (s == F8_OK && dX) s = mx4_gemm({(int)d->M, (int)d->K, (int)d->N, dy.q, dy.s, saved->w.q_t, saved->w.s_t, (uint16_t*)dX, d->K}, workspace, room, st);
+    if (s == F8_OK && dW) s = mx4_gemm({(int)d->N, (int)d->K, (int)d->M, dy.q_t, dy.s_t, saved->x.q_t, saved->x.s_t, (uint16_t*)dW, d->K}, workspace, room, st);
+    return s;
+}
+
+}  // extern "C"

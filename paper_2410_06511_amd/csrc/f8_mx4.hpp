@@ -1,0 +1,33 @@
+// Microscaled 4-bit operands (OCP MX, E2M1 elements in blocks of 32 with an E8M0 scale): layout and launches that the linear's
+// files share.
+//   codes  [rows, pitch4(n)] bytes: element 2 i of a row in the low nibble of byte i; a row is padded with zeros to whole blocks
+//   scales [groups of 512 elements][rows padded to 64][16] bytes: block b of the group's 16 at byte 4 (b % 4) + b / 4
+// The scales' order is that of their use: the lane of a matrix instruction that holds elements 32 g .. 32 g + 31 of each 128
+// finds those of four instructions in one word.  Bytes of no block hold 127, the scale 1.
+#pragma once
+#include "f8_host.hpp"
+
+namespace f8 {
+
+constexpr int kMxBlock = 32;    // elements with one scale
+constexpr int kMxGroup = 512;   // elements of a scale group
+constexpr int kMxRows = 64;     // rows of scales in a kilobyte
+constexpr int64_t kMxMax = (int64_t)1 << 23;  // bound of M, K, N
+
+__host__ __device__ inline int64_t mx4_pitch(int64_t n) { return (n + kMxBlock - 1) / kMxBlock * 16; }
+__host__ __device__ inline int64_t mx4_rows(int64_t rows) { return (rows + kMxRows - 1) / kMxRows * kMxRows; }
+inline size_t mx4_scale_bytes(int64_t rows, int64_t n) { return (size_t)((n + kMxGroup - 1) / kMxGroup) * (size_t)mx4_rows(rows) * 16; }
+
+// Validated product D[M, N] = A[M, K] B[N, K]^T.
+struct Mx4Args {
+    int M, N, K;
+    const uint8_t *A, *sa, *B, *sb;
+    uint16_t* D;
+    int64_t ldd;
+};
+f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st);
+size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K);  // the most that a product takes of a workspace
+// The forward of few rows straight from bf16: X is quantised in the registers of the product's waves.  false: not taken.
+bool mx4_rows_bf16(int M, int N, int K, const uint16_t* X, const uint8_t* B, const uint8_t* sb, uint16_t* D, int64_t ldd, hipStream_t st);
+
+}  // namespace f8

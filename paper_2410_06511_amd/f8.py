@@ -36,6 +36,7 @@ EXPORTS = ["f8_workspace_bytes", "f8_status_string", "f8_amax", "f8_scale", "f8_
            "f8_token_logprobs", "f8_token_logprobs_bwd", "f8_distill", "f8_distill_bwd",
            "f8_embed", "f8_embed_bwd", "f8_embed_bwd_workspace_bytes", "f8_layernorm", "f8_layernorm_bwd", "f8_layernorm_bwd_workspace_bytes",
            "f8_grad_norm", "f8_grad_clip", "f8_grad_norm_workspace_bytes",
+           "f8_mx4_scale_bytes", "f8_mx4_workspace_bytes", "f8_mx4_quantise", "f8_mx4_dequantise", "f8_mx4_gemm", "f8_mx4_linear_fwd", "f8_mx4_linear_bwd",
            "f8_probe_mfma", "f8_probe_copy", "f8_probe_read", "f8_probe_clock"]
 
 
@@ -56,6 +57,18 @@ class SavedStruct(C.Structure):
 
 class TensorStruct(C.Structure):
     _fields_ = [("data", _p), ("n", _i64), ("type", C.c_int32)]
+
+
+class MX4Struct(C.Structure):
+    _fields_ = [("q", _p), ("s", _p), ("q_t", _p), ("s_t", _p)]
+
+
+class MX4SavedStruct(C.Structure):
+    _fields_ = [("x", MX4Struct), ("w", MX4Struct), ("dy", MX4Struct)]
+
+
+class MX4Desc(C.Structure):
+    _fields_ = [("M", _i64), ("K", _i64), ("N", _i64)]
 
 
 class LinearDesc(C.Structure):
@@ -148,10 +161,18 @@ def lib():
         l.f8_grad_norm.argtypes = [_p, _i64, _int, _p, _p, _p, C.c_size_t, _p]
         l.f8_grad_clip.argtypes = [_p, _p, _i64, _p, f, _p]
         l.f8_grad_norm_workspace_bytes.argtypes = [_p, _i64]
+        l.f8_mx4_scale_bytes.argtypes = [_i64] * 2
+        l.f8_mx4_workspace_bytes.argtypes = [_i64] * 3
+        l.f8_mx4_quantise.argtypes = [_p, _i64, _i64, _i64, C.POINTER(MX4Struct), _p]
+        l.f8_mx4_dequantise.argtypes = [_p, _p, _i64, _i64, _p, _i64, _p]
+        l.f8_mx4_gemm.argtypes = [_i64, _i64, _i64, _p, _p, _p, _p, _p, _i64, _p, C.c_size_t, _p]
+        l.f8_mx4_linear_fwd.argtypes = [C.POINTER(MX4Desc), _p, _p, _p, C.POINTER(MX4SavedStruct), _p, C.c_size_t, _p]
+        l.f8_mx4_linear_bwd.argtypes = [C.POINTER(MX4Desc), _p, C.POINTER(MX4SavedStruct), _p, _p, _p, C.c_size_t, _p]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = _int
         for name in ("f8_sdpa_bwd_workspace_bytes", "f8_residual_norm_bwd_workspace_bytes", "f8_logits_workspace_bytes",
-                     "f8_embed_bwd_workspace_bytes", "f8_layernorm_bwd_workspace_bytes", "f8_grad_norm_workspace_bytes"):
+                     "f8_embed_bwd_workspace_bytes", "f8_layernorm_bwd_workspace_bytes", "f8_grad_norm_workspace_bytes", "f8_mx4_scale_bytes",
+                     "f8_mx4_workspace_bytes"):
             getattr(l, name).restype = C.c_size_t
         _lib = l
     return _lib
@@ -751,6 +772,109 @@ def grad_clip(grads, norm, most, out=None, stream=None):
         raise F8Error(F8_ERR_SHAPE, f"{len(out)} tensors for {len(grads)}")
     _check(lib().f8_grad_clip(grads.struct("grads", dev), None if out is None else out.struct("out", dev), len(grads), _packed("norm", norm, _F32, (1,), dev), most,
                               _stream(stream)))
+
+
+# ---- microscaled 4-bit linear -----------------------------------------------------------------
+
+def mx4_scale_bytes(rows, cols):
+    return int(lib().f8_mx4_scale_bytes(rows, cols))
+
+
+def mx4_workspace_bytes(M, K, N):
+    return int(lib().f8_mx4_workspace_bytes(M, K, N))
+
+
+class MX4Tensor:
+    """Device buffers of the codes of T[rows, cols] (see f8_mx4): q, s with blocks along the columns, q_t, s_t along the rows;
+    sides: "q", "t" or "qt" for either or both."""
+
+    def __init__(self, rows, cols, sides="q", device="cuda"):
+        u8 = dict(dtype=torch.uint8, device=device)
+        self.rows, self.cols = rows, cols
+        codes = lambda r, c: (torch.empty((r, 16 * ((c + 31) // 32)), **u8), torch.empty(mx4_scale_bytes(r, c), **u8))
+        self.q, self.s = codes(rows, cols) if "q" in sides else (None, None)
+        self.q_t, self.s_t = codes(cols, rows) if "t" in sides else (None, None)
+        self.device = torch.device(device)
+        self._struct = MX4Struct(_ptr(self.q), _ptr(self.s), _ptr(self.q_t), _ptr(self.s_t))
+
+    def struct(self):
+        return self._struct
+
+
+class MX4Saved:
+    """f8_mx4_saved for one linear: X [M, K], W [N, K], dY [M, N].  backward=False: what a forward needs, nothing for a backward."""
+
+    def __init__(self, M, K, N, backward=True, device="cuda", x=None):
+        """x: the MX4Tensor of another linear that reads the same input."""
+        self.M, self.K, self.N = M, K, N
+        sides = "qt" if backward else "q"
+        self.x = x if x is not None else MX4Tensor(M, K, sides, device)
+        self.w = MX4Tensor(N, K, sides, device)
+        self.dy = MX4Tensor(M, N, sides, device) if backward else None
+        if (self.x.rows, self.x.cols) != (M, K):
+            raise F8Error(F8_ERR_SHAPE, f"codes of [{self.x.rows}, {self.x.cols}] for an input of [{M}, {K}]")
+        self._struct = MX4SavedStruct(self.x.struct(), self.w.struct(), self.dy.struct() if backward else MX4Struct())
+        self._desc = MX4Desc(M, K, N)
+
+    def struct(self):
+        return self._struct
+
+
+def _on_current(name, t, dev):
+    for b in (t.q, t.q_t):
+        if b is not None and b.get_device() != dev:
+            raise F8Error(F8_ERR_SHAPE, f"{name}: codes on {b.device}, not on the current GPU, {dev}")
+
+
+def mx4_quantise(x, t, stream=None):
+    """x [rows, cols] bf16 into the sides that t (MX4Tensor) has."""
+    dev = _current()
+    xp, ld = _rows("x", x, (t.rows, t.cols), dev)
+    _on_current("t", t, dev)
+    _check(lib().f8_mx4_quantise(xp, t.rows, t.cols, ld, C.byref(t.struct()), _stream(stream)))
+
+
+def mx4_dequantise(t, out, transposed=False, stream=None):
+    """The values of t's codes along the columns into out [rows, cols] bf16; transposed: of those along the rows into [cols, rows]."""
+    dev = _current()
+    rows, cols = (t.cols, t.rows) if transposed else (t.rows, t.cols)
+    q, s = (t.q_t, t.s_t) if transposed else (t.q, t.s)
+    if q is None:
+        raise F8Error(1, "mx4_dequantise: the tensor has no codes along this side")
+    _on_current("t", t, dev)
+    op, ldo = _rows("out", out, (rows, cols), dev)
+    _check(lib().f8_mx4_dequantise(_ptr(q), _ptr(s), rows, cols, op, ldo, _stream(stream)))
+
+
+def mx4_gemm(a, b, D, workspace=None, stream=None):
+    """D [M, N] = A B^T of the codes along the columns of a [M, K] and b [N, K] (MX4Tensors)."""
+    dev = _current()
+    if a.cols != b.cols or a.q is None or b.q is None:
+        raise F8Error(F8_ERR_SHAPE, f"codes along the columns of [{a.rows}, {a.cols}] and [{b.rows}, {b.cols}]")
+    _on_current("a", a, dev), _on_current("b", b, dev)
+    dp, ldd = _rows("D", D, (a.rows, b.rows), dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_mx4_gemm(a.rows, b.rows, a.cols, _ptr(a.q), _ptr(a.s), _ptr(b.q), _ptr(b.s), dp, ldd, wp, wb, _stream(stream)))
+
+
+def mx4_linear_fwd(X, W, Y, saved, workspace=None, stream=None):
+    """Y = X4 W4^T; W None: saved.w holds the weight's codes already."""
+    dev, M, K, N = _current(), saved.M, saved.K, saved.N
+    _on_current("saved", saved.x, dev), _on_current("saved", saved.w, dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_mx4_linear_fwd(C.byref(saved._desc), _packed("X", X, _BF16, (M, K), dev), _packed("W", W, _BF16, (N, K), dev), _packed("Y", Y, _BF16, (M, N), dev),
+                                   C.byref(saved.struct()), wp, wb, _stream(stream)))
+
+
+def mx4_linear_bwd(dY, saved, dX, dW, workspace=None, stream=None):
+    """dX = dY4 W4, dW = dY4^T X4; either may be None."""
+    dev, M, K, N = _current(), saved.M, saved.K, saved.N
+    if saved.dy is None:
+        raise F8Error(1, "mx4_linear_bwd: a linear that was made without a backward")
+    _on_current("saved", saved.x, dev), _on_current("saved", saved.w, dev), _on_current("saved", saved.dy, dev)
+    wp, wb = _room(workspace, dev)
+    _check(lib().f8_mx4_linear_bwd(C.byref(saved._desc), _packed("dY", dY, _BF16, (M, N), dev), C.byref(saved.struct()), _packed("dX", dX, _BF16, (M, K), dev),
+                                   _packed("dW", dW, _BF16, (N, K), dev), wp, wb, _stream(stream)))
 
 
 # ---- measuring helpers ---------------------------------------------------------------

@@ -1,0 +1,230 @@
+"""The microscaled 4-bit linear through the C ABI against oracle/mx4_oracle.py: codes, scales and their layout bit for bit, the
+products per element against fp64 on the same codes.
+
+Tolerance of a product: half a step of bf16, 2^-8 of its value, and the fp32 additions.  A product of two codes is a multiple of
+2^-2 of at most 36, so within an instruction's block the sums are exact in the 13 bits that the chip keeps below the largest; the
+rest is one fp32 addition for each group of eight and each range of the contraction, 2^-24 of the sum of magnitudes each, taken
+twice for an addition that cuts off instead of rounding."""
+import numpy as np
+import pytest
+import torch
+
+import oracle as o
+from oracle import mx4_oracle as mo
+from paper_2410_06511_amd import f8
+from helpers import bits
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def gen(shape, seed, std=1.0):
+    """Values over several powers of two, outliers and blocks of zeros among them."""
+    g = torch.Generator("cpu")
+    g.manual_seed(seed)
+    x = torch.randn(shape, generator=g) * std * torch.exp2(torch.randint(-2, 3, (shape[0], 1), generator=g).float())
+    x[torch.rand(shape, generator=g) < 0.01] *= 40.0
+    x[:, :32][::3] = 0.0
+    return x.to(BF16)
+
+
+def wide(t):
+    return o.bf16_to_f32(bits(t)).astype(np.float64)
+
+
+def check_codes(q, s, x, what):
+    codes, scales = mo.quantise(x)
+    want = mo.place_scales(scales, x.shape[1])
+    assert np.array_equal(s.cpu().numpy(), want), what
+    got = q.cpu().numpy()
+    bad = got != mo.pack(codes)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4])
+
+
+def check_product(D, a, b, what):
+    """D against a b^T, a [M, K] and b [N, K] in fp64"""
+    got, d, mag = wide(D), a @ b.T, np.abs(a) @ np.abs(b).T
+    bound = 2.0 ** -8 * np.abs(d) * (1 + 2.0 ** -7) + 2.0 * (a.shape[1] / 8 + 16) * 2.0 ** -24 * mag + 1e-38
+    bad = ~(np.abs(got - d) <= bound)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4])
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 16), (1, 4096), (3, 48), (31, 32), (32, 64), (33, 528), (64, 512), (65, 1040), (127, 128), (130, 144), (300, 272), (513, 80), (16, 2064)])
+def test_quantise(rows, cols):
+    x = gen((rows, cols + 24), rows + cols).cuda()[:, :cols]   # (a row pitch)
+    both, along, across = f8.MX4Tensor(rows, cols, "qt"), f8.MX4Tensor(rows, cols, "q"), f8.MX4Tensor(rows, cols, "t")
+    for t in (both, along, across):
+        for b in (t.q, t.s, t.q_t, t.s_t):
+            if b is not None:
+                b.fill_(0xAB)
+        f8.mx4_quantise(x, t)
+    torch.cuda.synchronize()
+    check_codes(both.q, both.s, wide(x), "along"), check_codes(both.q_t, both.s_t, wide(x).T, "across")
+    assert torch.equal(both.q, along.q) and torch.equal(both.s, along.s) and torch.equal(both.q_t, across.q_t) and torch.equal(both.s_t, across.s_t)
+    out, out_t = torch.empty((rows, cols), dtype=BF16, device="cuda"), torch.full((cols, (rows + 15) // 8 * 8), 7.0, dtype=BF16, device="cuda")
+    f8.mx4_dequantise(both, out)
+    assert np.array_equal(wide(out), mo.rounded(wide(x)))
+    if rows % 8 == 0:
+        f8.mx4_dequantise(both, out_t[:, :rows], transposed=True)
+        assert np.array_equal(wide(out_t[:, :rows]), mo.rounded(wide(x).T)) and bool((out_t[:, rows:] == 7.0).all())
+
+
+def test_every_bf16_value():
+    """Each of the 65536 patterns as an element below each of a set of scales, and as the largest of its block."""
+    every = torch.arange(65536, dtype=torch.int32).to(torch.uint16).view(BF16)
+    for top in (0.0, 2.0 ** -133, 2.0 ** -126, 2.0 ** -125, 2.0 ** -124, 1.9921875, 4.0, 7.0, 2.0 ** 60, 3.0 * 2.0 ** 126):
+        x = torch.full((65536 // 31 + 1, 32), 0.0).to(BF16)
+        flat = torch.zeros((65536 // 31 + 1) * 31, dtype=BF16)
+        ok = every.float().abs() <= max(top, 2.0 ** -133) if top else torch.ones(65536, dtype=torch.bool)
+        flat[:65536] = torch.where(ok, every, torch.zeros_like(every))
+        x[:, 1:] = flat.view(-1, 31)
+        x[:, 0] = top
+        xg = x.cuda()
+        t = f8.MX4Tensor(x.shape[0], 32)
+        f8.mx4_quantise(xg, t)
+        codes, scales = mo.quantise(wide(xg))
+        assert np.array_equal(t.s.cpu().numpy(), mo.place_scales(scales, 32)), top
+        real = scales[:, 0] != 255    # (the codes of a block that is not a number say nothing)
+        assert np.array_equal(t.q.cpu().numpy()[real], mo.pack(codes)[real]), top
+
+
+PRODUCTS = [(1, 16, 16), (1, 4096, 256), (1, 272, 4096), (3, 48, 48), (16, 64, 512), (17, 528, 1040), (32, 2048, 768), (33, 64, 4112), (64, 272, 2048), (65, 144, 80),
+            (130, 80, 1552), (200, 512, 8192), (300, 1040, 528), (128, 256, 1024), (513, 784, 272), (1030, 1552, 1040), (2100, 528, 2064), (257, 4112, 512)]
+
+
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_product(M, N, K):
+    A, B = gen((M, K), M + K).cuda(), gen((N, K), N + K + 1, 0.05).cuda()
+    a, b = f8.MX4Tensor(M, K), f8.MX4Tensor(N, K)
+    f8.mx4_quantise(A, a), f8.mx4_quantise(B, b)
+    D = torch.full((M, N + 8), 7.0, dtype=BF16, device="cuda")
+    f8.mx4_gemm(a, b, D[:, :N])
+    torch.cuda.synchronize()
+    check_product(D[:, :N], mo.rounded(wide(A)), mo.rounded(wide(B)), (M, N, K))
+    assert bool((D[:, N:] == 7.0).all())
+    ws = torch.full((f8.mx4_workspace_bytes(M, K, N),), 255, dtype=torch.uint8, device="cuda")
+    E, F = torch.empty((M, N), dtype=BF16, device="cuda"), torch.empty((M, N), dtype=BF16, device="cuda")
+    f8.mx4_gemm(a, b, E, ws), f8.mx4_gemm(a, b, F, ws)
+    check_product(E, mo.rounded(wide(A)), mo.rounded(wide(B)), (M, N, K, "workspace"))
+    assert torch.equal(E, F)
+
+
+def test_nothing_but_the_operands_enters():
+    """Around the operands lie bytes that stand for NaN scales and large codes; rows and columns past the ends are theirs."""
+    M, N, K = 70, 80, 560
+    A, B = gen((M, K), 1).cuda(), gen((N, K), 2).cuda()
+    D = []
+    for fill in (0, 255):
+        tensors = []
+        for x in (A, B):
+            t = f8.MX4Tensor(*x.shape)
+            room = [torch.full((b.numel() + 8192,), fill, dtype=torch.uint8, device="cuda") for b in (t.q, t.s)]
+            t.q, t.s = room[0][4096:4096 + t.q.numel()].view(t.q.shape), room[1][4096:4096 + t.s.numel()]
+            t._struct = f8.MX4Struct(t.q.data_ptr(), t.s.data_ptr(), None, None)
+            f8.mx4_quantise(x, t)
+            assert all(bool((r[:4096] == fill).all()) and bool((r[-4096:] == fill).all()) for r in room)
+            tensors.append(t)
+        D.append(torch.empty((M, N), dtype=BF16, device="cuda"))
+        f8.mx4_gemm(tensors[0], tensors[1], D[-1])
+    assert torch.equal(D[0], D[1])
+
+
+def test_a_contraction_of_nothing():
+    for M, N in ((5, 32), (300, 528)):
+        a, b = f8.MX4Tensor(M, 0), f8.MX4Tensor(N, 0)
+        D = torch.full((M, N), 7.0, dtype=BF16, device="cuda")
+        f8.mx4_gemm(a, b, D)
+        assert not D.any().item()
+
+
+def test_what_is_not_a_number_stays_in_its_row():
+    M, N, K = 40, 64, 512
+    A, B = gen((M, K), 1).cuda(), gen((N, K), 2).cuda()
+    A[3, 100], A[17, 0] = float("nan"), float("inf")
+    a, b, D = f8.MX4Tensor(M, K), f8.MX4Tensor(N, K), torch.empty((M, N), dtype=BF16, device="cuda")
+    f8.mx4_quantise(A, a), f8.mx4_quantise(B, b)
+    f8.mx4_gemm(a, b, D)
+    assert bool(D[[3, 17]].isnan().all())
+    rest = [m for m in range(M) if m not in (3, 17)]
+    assert bool(D[rest].isfinite().all())
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 512, 256), (5, 48, 80), (48, 256, 64), (300, 1040, 272), (520, 784, 1552), (1000, 256, 2048), (4100, 528, 512)])
+def test_linear(M, K, N):
+    X, W, dY = gen((M, K), 1).cuda(), gen((N, K), 2, 0.02).cuda(), gen((M, N), 3, 1e-3).cuda()
+    saved = f8.MX4Saved(M, K, N)
+    Y, dX, dW = (torch.full(s, 7.0, dtype=BF16, device="cuda") for s in ((M, N), (M, K), (N, K)))
+    ws = torch.full((f8.mx4_workspace_bytes(M, K, N),), 255, dtype=torch.uint8, device="cuda")
+    f8.mx4_linear_fwd(X, W, Y, saved, ws)
+    f8.mx4_linear_bwd(dY, saved, dX, dW, ws)
+    torch.cuda.synchronize()
+    x, w, dy = wide(X), wide(W), wide(dY)
+    for t, v in ((saved.x, x), (saved.w, w), (saved.dy, dy)):
+        check_codes(t.q, t.s, v, "q"), check_codes(t.q_t, t.s_t, v.T, "q_t")
+    check_product(Y, mo.rounded(x), mo.rounded(w), "Y")
+    check_product(dX, mo.rounded(dy), mo.rounded(w.T), "dX")
+    check_product(dW, mo.rounded(dy.T), mo.rounded(x.T), "dW")
+    # the weight's codes kept, single gradients, without what a backward needs
+    Y2, dX2, dW2 = (torch.empty_like(t) for t in (Y, dX, dW))
+    f8.mx4_linear_fwd(X, None, Y2, saved, ws)
+    f8.mx4_linear_bwd(dY, saved, dX2, None, ws)
+    f8.mx4_linear_bwd(dY, saved, None, dW2, ws)
+    assert torch.equal(Y, Y2) and torch.equal(dX, dX2) and torch.equal(dW, dW2)
+    short = f8.MX4Saved(M, K, N, backward=False)
+    f8.mx4_quantise(W, short.w)
+    f8.mx4_linear_fwd(X, None, Y2, short, ws)
+    assert torch.equal(Y, Y2)
+
+
+def test_gradients_by_differences():
+    """On values that the format holds the linear is exact, and so are differences of its loss."""
+    r = np.random.default_rng(0)
+    M, K, N = 64, 96, 64
+    def exact(shape):
+        v = mo.GRID[r.integers(0, 8, shape)] * r.choice([-1.0, 1.0], shape)
+        v[::32, :], v[:, ::32] = 4.0, 4.0      # every block, either way, keeps the scale 1
+        return torch.tensor(v, dtype=torch.float32).to(BF16).cuda()
+    X, W, dY = exact((M, K)), exact((N, K)), exact((M, N))
+    saved = f8.MX4Saved(M, K, N)
+    Y, dX, dW = (torch.empty(s, dtype=BF16, device="cuda") for s in ((M, N), (M, K), (N, K)))
+    f8.mx4_linear_fwd(X, W, Y, saved)
+    f8.mx4_linear_bwd(dY, saved, dX, dW)
+    loss = lambda X, W: float((wide(X) @ wide(W).T * wide(dY)).sum())
+    for i, k in ((5, 7), (33, 40), (63, 95)):
+        up, down = X.clone(), X.clone()
+        up[i, k], down[i, k] = 3.0, 2.0
+        assert abs(loss(up, W) - loss(down, W) - dX[i, k].item()) <= 2.0 ** -8 * abs(dX[i, k].item()) + 1e-6
+        up, down = W.clone(), W.clone()
+        up[i, k], down[i, k] = 3.0, 2.0
+        assert abs(loss(X, up) - loss(X, down) - dW[i, k].item()) <= 2.0 ** -8 * abs(dW[i, k].item()) + 1e-6
+
+
+@pytest.mark.parametrize("M", [1, 300])
+def test_on_another_stream_and_in_a_graph(M):
+    K, N = 1024, 528
+    batches = [(gen((M, K), i).cuda(), gen((N, K), 10 + i, 0.02).cuda(), gen((M, N), 20 + i).cuda()) for i in range(3)]
+    ws = torch.empty(f8.mx4_workspace_bytes(M, K, N), dtype=torch.uint8, device="cuda")
+    new = lambda: [torch.empty(s, dtype=BF16, device="cuda") for s in ((M, N), (M, K), (N, K))]
+    def step(X, W, dY, saved, out, stream=None):
+        f8.mx4_linear_fwd(X, W, out[0], saved, ws, stream)
+        f8.mx4_linear_bwd(dY, saved, out[1], out[2], ws, stream)
+    eager = []
+    for b in batches:
+        eager.append(new())
+        step(*b, f8.MX4Saved(M, K, N), eager[-1])
+    side, out, saved = torch.cuda.Stream(), new(), f8.MX4Saved(M, K, N)
+    torch.cuda.synchronize()
+    step(*batches[1], saved, out, side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, eager[1]))
+    X, W, dY = (t.clone() for t in batches[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(X, W, dY, saved, out)
+    for i in (0, 1, 2, 1):
+        X.copy_(batches[i][0]), W.copy_(batches[i][1]), dY.copy_(batches[i][2])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.randn(1 << 20, device="cuda").sum().isfinite().item()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager[i]))

@@ -112,3 +112,68 @@ def test_binding_refuses_what_the_library_cannot_see():
         with pytest.raises(f8.F8Error) as e:
             call_()
         assert e.value.code == SHAPE
+
+
+# ---- microscaled 4-bit linear ------------------------------------------------------------------
+
+MX4 = lambda **change: f8.MX4Struct(*{**dict(q=FAKE, s=FAKE, q_t=FAKE, s_t=FAKE), **change}.values())
+QUANTISE = dict(x=FAKE, rows=5, cols=64, ld=64, out=None, stream=None)
+GEMM = dict(M=5, N=32, K=64, A=FAKE, sa=FAKE, B=FAKE, sb=FAKE, D=FAKE, ldd=32, ws=None, wb=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change,codes", [
+    (SHAPE, dict(rows=-1), {}), (SHAPE, dict(cols=72, ld=72), {}), (SHAPE, dict(cols=-16), {}), (SHAPE, dict(ld=48), {}), (SHAPE, dict(ld=68), {}), (SHAPE, dict(rows=1 << 23), {}),
+    (SHAPE, dict(rows=(1 << 23) - 1, cols=(1 << 23) - 16, ld=1 << 23), {}), (NULL, dict(x=None), {}), (ALIGN, dict(x=FAKE + 8), {}),
+    (NULL, {}, dict(q=None)), (NULL, {}, dict(s=None)), (NULL, {}, dict(s_t=None)), (NULL, {}, dict(q=None, s=None, q_t=None, s_t=None)), (ALIGN, {}, dict(q=FAKE + 8)),
+    (ALIGN, {}, dict(s_t=FAKE + 4))])
+def test_mx4_quantise(status, change, codes):
+    t = MX4(**codes)
+    assert call("f8_mx4_quantise", QUANTISE, **{"out": C.byref(t), **change}) == status
+    assert call("f8_mx4_quantise", QUANTISE) == NULL
+
+
+@pytest.mark.parametrize("status,change", [
+    (SHAPE, dict(M=-1)), (SHAPE, dict(N=24)), (SHAPE, dict(K=-1)), (SHAPE, dict(K=1 << 23)), (SHAPE, dict(ldd=24)), (SHAPE, dict(ldd=36)), (NULL, dict(A=None)), (NULL, dict(sa=None)),
+    (NULL, dict(B=None)), (NULL, dict(sb=None)), (NULL, dict(D=None)), (ALIGN, dict(A=FAKE + 8)), (ALIGN, dict(sb=FAKE + 8)), (ALIGN, dict(D=FAKE + 8)), (ALIGN, dict(ws=FAKE + 8, wb=99)),
+    (SHAPE, dict(M=(1 << 23) - 1, N=(1 << 23) - 16, ldd=(1 << 23) - 16))])
+def test_mx4_gemm(status, change):
+    assert call("f8_mx4_gemm", GEMM, **change) == status
+
+
+@pytest.mark.parametrize("status,change", [(SHAPE, dict(rows=-1)), (SHAPE, dict(cols=12)), (SHAPE, dict(ldo=56)), (NULL, dict(q=None)), (NULL, dict(s=None)), (NULL, dict(out=None)),
+                                           (ALIGN, dict(out=FAKE + 8)), (ALIGN, dict(q=FAKE + 8))])
+def test_mx4_dequantise(status, change):
+    assert call("f8_mx4_dequantise", dict(q=FAKE, s=FAKE, rows=5, cols=64, out=FAKE, ldo=64, stream=None), **change) == status
+
+
+def test_mx4_linear():
+    l = f8.lib()
+    def fwd(d=(5, 64, 32), X=FAKE, W=FAKE, Y=FAKE, x=MX4(), w=MX4(), ws=None):
+        sv = f8.MX4SavedStruct(x, w, MX4())
+        return l.f8_mx4_linear_fwd(C.byref(f8.MX4Desc(*d)), X, W, Y, C.byref(sv), ws, 0, None)
+    for d in ((-1, 64, 32), (5, 72, 32), (5, 64, 40), (5, -16, 32), (1 << 23, 64, 32), (5, 1 << 23, 32)):
+        assert fwd(d) == SHAPE
+    assert fwd(X=None) == NULL and fwd(Y=None) == NULL and fwd(x=MX4(q=None, s=None)) == NULL and fwd(w=MX4(s=None)) == NULL and fwd(w=MX4(q_t=None)) == NULL
+    assert fwd(X=FAKE + 2) == ALIGN and fwd(W=FAKE + 8) == ALIGN and fwd(Y=FAKE + 8) == ALIGN and fwd(ws=FAKE + 4) == ALIGN and fwd(x=MX4(q=FAKE + 4)) == ALIGN
+    def bwd(d=(5, 64, 32), dY=FAKE, dX=FAKE, dW=FAKE, x=MX4(), w=MX4(), dy=MX4()):
+        sv = f8.MX4SavedStruct(x, w, dy)
+        return l.f8_mx4_linear_bwd(C.byref(f8.MX4Desc(*d)), dY, C.byref(sv), dX, dW, None, 0, None)
+    assert bwd((5, 64, 40)) == SHAPE and bwd(dY=None) == NULL and bwd(dX=None, dW=None) == NULL and bwd(dY=FAKE + 8) == ALIGN and bwd(dW=FAKE + 8) == ALIGN
+    assert bwd(dy=MX4(q=None, s=None)) == NULL and bwd(dy=MX4(q_t=None, s_t=None)) == NULL and bwd(x=MX4(q_t=None, s_t=None)) == NULL and bwd(w=MX4(q_t=None, s_t=None)) == NULL
+    assert l.f8_mx4_linear_fwd(None, FAKE, FAKE, FAKE, None, None, 0, None) == NULL and l.f8_mx4_linear_bwd(None, FAKE, None, FAKE, FAKE, None, 0, None) == NULL
+
+
+def test_mx4_sizes():
+    assert f8.mx4_scale_bytes(1, 16) == 64 * 16 and f8.mx4_scale_bytes(65, 513) == 2 * 128 * 16 and f8.mx4_scale_bytes(0, 64) == 0 and f8.mx4_scale_bytes(-1, 64) == 0
+    assert f8.mx4_workspace_bytes(5, 64, 32) >= 8192 and f8.mx4_workspace_bytes(-1, 64, 32) == 8192
+    t = f8.MX4Tensor(5, 48, "qt", "cpu")
+    assert t.q.shape == (5, 32) and t.q_t.shape == (48, 16) and t.s.numel() == 64 * 16 and t.s_t.numel() == 64 * 16
+    bf = torch.zeros((5, 48), dtype=torch.bfloat16)
+    saved = f8.MX4Saved(5, 48, 16, device="cpu")
+    for call_ in (lambda: f8.mx4_quantise(bf, t), lambda: f8.mx4_dequantise(t, bf), lambda: f8.mx4_linear_fwd(bf, None, bf, saved), lambda: f8.mx4_gemm(t, t, bf),
+                  lambda: f8.mx4_linear_bwd(bf, saved, bf, None), lambda: f8.MX4Saved(6, 48, 16, device="cpu", x=t), lambda: f8.mx4_gemm(t, f8.MX4Tensor(5, 64, "q", "cpu"), bf)):
+        with pytest.raises(f8.F8Error) as e:
+            call_()
+        assert e.value.code == SHAPE
+    with pytest.raises(f8.F8Error):
+        f8.mx4_linear_bwd(bf, f8.MX4Saved(5, 48, 16, backward=False, device="cpu"), bf, None)
