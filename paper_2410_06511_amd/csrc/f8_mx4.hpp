@@ -18,16 +18,16 @@ __host__ __device__ inline int64_t mx4_pitch(int64_t n) { return (n + kMxBlock -
 __host__ __device__ inline int64_t mx4_rows(int64_t rows) { return (rows + kMxRows - 1) / kMxRows * kMxRows; }
 inline size_t mx4_scale_bytes(int64_t rows, int64_t n) { return (size_t)((n + kMxGroup - 1) / kMxGroup) * (size_t)mx4_rows(rows) * 16; }
 
-// Validated product D[M, N] = A[M, K] B[N, K]^T.
+// Validated product D[M, N] = A[M, K] B[N, K]^T; a launch may take a part of it: the rows m0 .. M - 1, the columns n0 .. N - 1.
 struct Mx4Args {
     int M, N, K;
     const uint8_t *A, *sa, *B, *sb;
     uint16_t* D;
     int64_t ldd;
+    int m0 = 0, n0 = 0;                   // multiples of 256
+    int64_t a_srows = mx4_rows(M), b_srows = mx4_rows(N);  // rows of the operands' scales
 };
 f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st);
 size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K);  // the most that a product takes of a workspace
-// The forward of few rows straight from bf16: X is quantised in the registers of the product's waves.  false: not taken.
-bool mx4_rows_bf16(int M, int N, int K, const uint16_t* X, const uint8_t* B, const uint8_t* sb, uint16_t* D, int64_t ldd, hipStream_t st);
 
 }  // namespace f8

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
     const int m0 = tm * ROWS, n0 = tn * COLS;
     const int64_t pitch = mx4_pitch(p.K);
     const uint8_t *a_base = p.A + m0 * pitch, *b_base = p.B + n0 * pitch;
-    const int64_t a_scales = mx4_rows(p.M) * 16, b_scales = mx4_rows(p.N) * 16;  // bytes of a group
+    const int64_t a_scales = p.a_srows * 16, b_scales = p.b_srows * 16;  // bytes of a group
     const uint8_t *sa_base = p.sa + (int64_t)m0 * 16, *sb_base = p.sb + (int64_t)n0 * 16;
 
     // load l of a step: 8 rows of 128 bytes, A's rows first; lane: row lane / 8 of them, one 16-byte chunk.  Past the end of the
@@ -114,6 +114,355 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
     }
 }
 
+// ---- tiles ---------------------------------------------------------------------------------------
+
+// As gemm_tile_kernel (f8_gemm_kernels.hpp) for two operands whose contraction is contiguous: persistent workgroups, two LDS
+// stages of 128 bytes of each row (256 elements here: two instructions of 128), loads two steps ahead of the products and spread
+// over them, the same order of fragments.  What is different:
+//   - a slot of the step, which there is one instruction of 32 cycles, is two of 16; the two of one accumulator are a slot apart.
+//   - the scales of a pair of steps, 16 bytes for each row, come to LDS in the pair before and to registers in its last half step:
+//     a word for each fragment, whose byte the instruction picks.
+//   - M is any number: rows past the end read the last one again, and are not stored.
+// SPLITK: work item w is tile w % tiles, range w / tiles of the contraction, whose fp32 sums go to partial[range][M][N].
+// RAGGED: the row's bytes are no multiple of 256: what lies past their end is loaded as zero, by the range check of buffer loads.
+template <int BM, int BN>
+struct Mx4Lds {
+    // (one row of MFMA tiles at a time: two workgroups of 128 x 128 tiles fit a compute unit)
+    static constexpr int kEpw = BN / 2 / 16 >= 8 ? 8 : 4, kEpr = 1, kEpStride = kEpw == 4 ? 128 : 16 * kEpw * 2 + 16;
+    static constexpr int kStage = (BM + BN) * kBK, kScales = (BM + BN) * 16, kEpilogue = 4 * 16 * kEpr * kEpStride;
+};
+
+template <int BM, int BN, bool SPLITK, bool RAGGED>
+__global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tiles_m, int tiles_n, int KT /* steps of a work item, even */, int splits,
+                                                       float* __restrict__ partial)
+{
+    using L = Mx4Lds<BM, BN>;
+    __shared__ __attribute__((aligned(1024))) uint8_t st0[L::kStage];
+    __shared__ __attribute__((aligned(1024))) uint8_t st1[L::kStage];
+    __shared__ __attribute__((aligned(1024))) uint8_t scb[L::kScales];
+    __shared__ __attribute__((aligned(16))) uint8_t epb[L::kEpilogue];
+    constexpr int NW = 4, WM = BM / 2, WN = BN / 2, TM = WM / 16, TN = WN / 16;  // waves, wave tile, fragments
+    constexpr int A_BYTES = BM * kBK, A_LOADS = BM / 8 / NW, B_LOADS = BN / 8 / NW, LOADS = A_LOADS + B_LOADS;
+    constexpr int EPW = L::kEpw, EPR = L::kEpr, EP_STRIDE = L::kEpStride;
+    using std::integral_constant;
+    using I0 = integral_constant<int, 0>;
+    using I1 = integral_constant<int, 1>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / 2, wn = wave % 2, fr = lane & 15, fg = lane >> 4;
+    const int tiles_mn = tiles_m * tiles_n, total = SPLITK ? tiles_mn * splits : tiles_mn;
+    const int64_t pitch = mx4_pitch(p.K);
+    const int groups = (p.K + kMxGroup - 1) / kMxGroup;
+    auto stage_ptr = [&](auto S) -> uint8_t* {
+        if constexpr (decltype(S)::value == 0) return st0;
+        else return st1;
+    };
+
+    // ---- load stream: wave w fills rows [w * R / 4, ...) of each operand's tile in pieces of 8 rows; lane i lands at row i / 8,
+    // physical chunk i % 8 of a piece, and fetches the logical chunk that belongs there
+    const int chunk = 16 * ((lane & 7) ^ swz(lane >> 3));  // (the swizzle looks at bits 1 and 2 of the row only)
+    const uint8_t *a_base, *b_base, *sa_base, *sb_base;
+    uint32_t a_off[A_LOADS], b_off[B_LOADS];
+    int64_t left = 0;    // bytes of a row from the item's first on
+    int group0 = 0;      // the item's first group
+    int ld_item = (int)blockIdx.x;
+    auto load_context = [&](int item) {
+        int tm, tn;
+        tile_coords(SPLITK ? item % tiles_mn : item, tiles_m, tiles_n, &tm, &tn);
+        const int64_t koff = SPLITK ? (int64_t)(item / tiles_mn) * KT * kBK : 0;
+        left = pitch - koff, group0 = (int)(koff / (2 * kBK));
+        const int m0 = p.m0 + tm * BM, n0 = p.n0 + tn * BN;
+        a_base = p.A + (int64_t)m0 * pitch + koff, b_base = p.B + (int64_t)n0 * pitch + koff;
+        const int a_last = p.M - 1 - m0, b_last = p.N - 1 - n0;
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) {
+            const int row = wave * (BM / NW) + 8 * i + (lane >> 3);
+            a_off[i] = (uint32_t)(row < a_last ? row : a_last) * (uint32_t)pitch + chunk;
+        }
+#pragma unroll
+        for (int i = 0; i < B_LOADS; ++i) {
+            const int row = wave * (BN / NW) + 8 * i + (lane >> 3);
+            b_off[i] = (uint32_t)(row < b_last ? row : b_last) * (uint32_t)pitch + chunk;
+        }
+        // this wave's 64 rows of each operand's scales (the last ones again past the end)
+        const int a_piece = m0 / 64 + wave % (BM / 64), b_piece = n0 / 64 + wave % (BN / 64);
+        const int a_most = (int)(p.a_srows / 64) - 1, b_most = (int)(p.b_srows / 64) - 1;
+        sa_base = p.sa + (int64_t)(a_piece < a_most ? a_piece : a_most) * 1024;
+        sb_base = p.sb + (int64_t)(b_piece < b_most ? b_piece : b_most) * 1024;
+    };
+    auto cut_loads = [&](int kt) {  // of step kt, what lies past the rows' end; so it does for all steps to come
+        if constexpr (!RAGGED) return;
+        const int64_t valid = left - (int64_t)kt * kBK;
+        if (valid >= kBK) return;  // uniform
+        if (chunk >= valid) {
+#pragma unroll
+            for (int i = 0; i < A_LOADS; ++i) a_off[i] = kPastEnd;
+#pragma unroll
+            for (int i = 0; i < B_LOADS; ++i) b_off[i] = kPastEnd;
+        }
+    };
+    auto source_at = [](const uint8_t* q) {
+        if constexpr (RAGGED) return buffer_at(q);
+        else return q;
+    };
+    auto issue_one = [&](auto ga, auto gb, auto S, auto IDX) {
+        constexpr int idx = decltype(IDX)::value;
+        constexpr bool is_a = idx < A_LOADS;
+        constexpr int j = is_a ? idx : idx - A_LOADS;
+        const uint32_t lds = lds_address(stage_ptr(S) + (is_a ? 0 : A_BYTES) + wave * ((is_a ? BM : BN) / NW) * kBK + j * 1024);
+        const auto src = is_a ? ga : gb;
+        uint32_t o;
+        if constexpr (is_a) o = a_off[j];
+        else o = b_off[j];
+        if constexpr (RAGGED)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(o), "s"(src) : "memory");
+        else
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(o), "s"(src) : "memory");
+    };
+    auto step_a = [&](int kt) { return a_base + (int64_t)kt * kBK; };
+    auto step_b = [&](int kt) { return b_base + (int64_t)kt * kBK; };
+    // the scales of the pair of steps from kt on (past the last group, where the codes are zeros, its scales again)
+    const uint32_t scale_lane = lane * 16;
+    auto issue_scales = [&](int kt, auto WHICH) {
+        int g = group0 + kt / 2;
+        g = g < groups ? g : groups - 1;
+        constexpr bool is_a = decltype(WHICH)::value == 0;
+        const uint8_t* src = is_a ? sa_base + g * (p.a_srows * 16) : sb_base + g * (p.b_srows * 16);
+        const uint32_t lds = lds_address(scb + (is_a ? wave % (BM / 64) * 1024 : BM * 16 + wave % (BN / 64) * 1024));
+        const uint32_t o = scale_lane;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(o), "s"(src) : "memory");
+    };
+    auto next_item = [&]() {  // past the last one the stream stays: the same number of loads in every step
+        ld_item += (int)gridDim.x;
+        if (ld_item < total) load_context(ld_item);
+    };
+
+    // ---- fragments: 16 rows, 256 elements; lane: row fr, blocks fg and 4 + fg
+    const int a_rd = (wm * WM + fr) * kBK, b_rd = A_BYTES + (wn * WN + fr) * kBK;
+    const int c0 = 16 * (fg ^ swz(fr)), c1 = 16 * ((4 + fg) ^ swz(fr));
+    struct Frag {
+        v4i k[2];
+    };
+    Frag fa[TM], fb[TN], fb_early;
+    int sa[TM], sb[TN], sb_early;
+    auto read = [&](const uint8_t* row) { return Frag{{*reinterpret_cast<const v4i*>(row + c0), *reinterpret_cast<const v4i*>(row + c1)}}; };
+    auto read_a = [&](auto S, auto I) { fa[decltype(I)::value] = read(stage_ptr(S) + a_rd + decltype(I)::value * 16 * kBK); };
+    auto read_b = [&](auto S, auto I) { fb[decltype(I)::value] = read(stage_ptr(S) + b_rd + decltype(I)::value * 16 * kBK); };
+    const int sa_rd = (wm * WM + fr) * 16 + fg * 4, sb_rd = BM * 16 + (wn * WN + fr) * 16 + fg * 4;
+    auto read_sa = [&](auto I) { sa[decltype(I)::value] = *reinterpret_cast<const int*>(scb + sa_rd + decltype(I)::value * 256); };
+    auto read_sb = [&](auto I) { sb[decltype(I)::value] = *reinterpret_cast<const int*>(scb + sb_rd + decltype(I)::value * 256); };
+
+    v4f acc[TM][TN];
+    auto zero_acc = [&]() {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    };
+
+    // ---- order of the step's slots, as in gemm_tile_kernel; slots 2 q and 2 q + 1 do the first halves of both their products,
+    // then the second halves
+    constexpr int SLOTS = TM * TN, HALF = SLOTS / 2, HM = TM / 2;
+    constexpr auto slot_i = [](int s) { return s < HALF ? s / TN : HM + (s - HALF) % HM; };
+    constexpr auto slot_j = [](int s) { return s < HALF ? s % TN : (s - HALF) / HM; };
+    auto mfma = [&](auto S, auto SLOT, auto K) {
+        constexpr int s = decltype(SLOT)::value, i = slot_i(s), j = slot_j(s), k = decltype(K)::value, byte = 2 * decltype(S)::value + k;
+        v4f& c = acc[i][j];
+        const v4i& b = fb[j].k[k];
+        const v4i& a = fa[i].k[k];
+        const int& tb = sb[j];
+        const int& ta = sa[i];
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%5,0] op_sel_hi:[%6,%6,0] cbsz:4 blgp:4"
+                     : "+a"(c)
+                     : "v"(b), "v"(a), "v"(tb), "v"(ta), "n"(byte & 1), "n"(byte >> 1));
+    };
+    auto mfma_slot = [&](auto S, auto SLOT) {
+        constexpr int s = decltype(SLOT)::value, q = s / 2 * 2;
+        mfma(S, integral_constant<int, q>{}, integral_constant<int, s % 2>{});
+        mfma(S, integral_constant<int, q + 1>{}, integral_constant<int, s % 2>{});
+    };
+    auto drain = [&]() { asm volatile("s_nop 15\n\ts_nop 15"); };  // nothing interlocks an accumulator's first ordinary read
+
+    // ---- epilogue of one tile, as in gemm_tile_kernel
+    auto epilogue = [&](int item) {
+        int tm, tn;
+        tile_coords(SPLITK ? item % tiles_mn : item, tiles_m, tiles_n, &tm, &tn);
+        const int m0 = p.m0 + tm * BM + wm * WM, n0 = p.n0 + tn * BN + wn * WN;
+        if constexpr (SPLITK) {
+            float* P = partial + (int64_t)(item / tiles_mn) * p.M * p.N;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int m = m0 + 16 * i + fr;
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int n = n0 + 16 * j + 4 * fg;
+                    if (m < p.M && n < p.N) *reinterpret_cast<v4f*>(P + (int64_t)m * p.N + n) = acc[i][j];
+                }
+            }
+            return;
+        }
+        uint8_t* ep = epb + wave * (16 * EPR * EP_STRIDE);
+        uint8_t* dbase = reinterpret_cast<uint8_t*>(p.D + (int64_t)m0 * p.ldd + n0);
+        const uint32_t ldd_b = (uint32_t)p.ldd * 2;
+        constexpr int LPR = 2 * EPW;  // lanes (16-byte pieces) per staged row
+        const uint32_t voff = (uint32_t)(lane / LPR) * ldd_b + (uint32_t)(lane % LPR) * 16;
+        auto run = [&](auto INTERIOR) {
+            static_for<(TM / EPR) * (TN / EPW)>([&](auto P) {
+                constexpr int ip = decltype(P)::value / (TN / EPW), jp = decltype(P)::value % (TN / EPW);
+#pragma unroll
+                for (int ii = 0; ii < EPR; ++ii)
+#pragma unroll
+                    for (int jj = 0; jj < EPW; ++jj) {
+                        const v4f& c = acc[EPR * ip + ii][EPW * jp + jj];
+                        const uint2 o = make_uint2(pack_bf16(c[0], c[1]), pack_bf16(c[2], c[3]));
+                        if constexpr (EPW == 4) *reinterpret_cast<uint2*>(ep + (16 * ii + fr) * EP_STRIDE + 16 * ((2 * jj + (fg >> 1)) ^ (fr & 7)) + 8 * (fg & 1)) = o;
+                        else *reinterpret_cast<uint2*>(ep + (16 * ii + fr) * EP_STRIDE + (16 * jj + 4 * fg) * 2) = o;
+                    }
+                uint8_t* pbase = dbase + ((int64_t)(16 * EPR * ip) * p.ldd + 16 * EPW * jp) * 2;
+#pragma unroll
+                for (int t = 0; t < 16 * EPR * LPR / 64; ++t) {
+                    const int idx = t * 64 + lane, piece = EPW == 4 ? (idx % LPR) ^ ((idx / LPR) & 7) : idx % LPR;
+                    const uint4 v = *reinterpret_cast<const uint4*>(ep + (idx / LPR) * EP_STRIDE + piece * 16);
+                    bool ok = true;
+                    if constexpr (!decltype(INTERIOR)::value) ok = m0 + 16 * EPR * ip + idx / LPR < p.M && n0 + 16 * EPW * jp + (idx % LPR) * 8 < p.N;
+                    if (ok) store_stream(reinterpret_cast<uint4*>(pbase + (voff + (uint32_t)(64 / LPR * t) * ldd_b)), v);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        if (p.m0 + tm * BM + BM <= p.M && p.n0 + tn * BN + BN <= p.N) run(std::true_type{});
+        else run(std::false_type{});
+    };
+
+    auto read_first_set = [&](auto S) {
+        static_for<HM>([&](auto I) { read_a(S, I); });
+        static_for<TN>([&](auto J) { read_b(S, J); });
+        static_for<HM>([&](auto I) { read_sa(I); });
+        static_for<TN>([&](auto J) { read_sb(J); });
+    };
+
+    // ---- prologue
+    load_context(ld_item);
+    issue_scales(0, I0{}), issue_scales(0, I1{});
+    auto issue_all = [&](int kt, auto S) {
+        const auto ga = source_at(step_a(kt)), gb = source_at(step_b(kt));
+        static_for<LOADS>([&](auto I) { issue_one(ga, gb, S, I); });
+    };
+    cut_loads(0);
+    issue_all(0, I0{});
+    cut_loads(1);
+    issue_all(1, I1{});
+    zero_acc();
+    __builtin_amdgcn_s_waitcnt(kWaitAllVmLgkm);
+    __syncthreads();
+    read_first_set(I0{});
+
+    // ---- one step out of stage S: the schedule of gemm_tile_kernel, and
+    //   the scales' words are read where their fragments are, but only once in a pair of steps: those that an even step starts
+    //   with in the odd step before, the lower A fragments' in the even step itself;
+    //   even steps, late slots: + the loads of the next pair's scales (behind the barrier after those reads)
+    constexpr int SYNC_A = HM + (SLOTS >= 64 ? 8 : SLOTS >= 32 ? 4 : 1);
+    constexpr int SYNC_B = HALF - 2;
+    constexpr int L_END = SLOTS >= 64 ? SLOTS - SLOTS / 8 : SLOTS;
+    static_assert(SYNC_A <= SYNC_B && L_END - SYNC_A >= LOADS / 2, "schedule does not fit");
+    constexpr auto slot_of_load = [](int l) { return SYNC_A + l * (L_END - SYNC_A) / LOADS; };
+    constexpr int PRE_B = [&] {
+        int n = 0;
+        for (int l = 0; l < LOADS; ++l) n += slot_of_load(l) < SYNC_B;
+        return n;
+    }();
+    constexpr auto slot_of_next_b = [](int j) {
+        const int s = HALF + (j + 1) * HM - 1;
+        return s < SLOTS - 3 ? s : SLOTS - 3;
+    };
+    constexpr int kWaitB = (PRE_B & 15) | ((PRE_B >> 4) << 14) | 0x0070;  // vmcnt(PRE_B) lgkmcnt(0)
+
+    auto kstep = [&](auto S, int fetch_kt) {
+        constexpr int s = decltype(S)::value;
+        using OTHER = integral_constant<int, 1 - s>;
+        const auto ga = source_at(step_a(fetch_kt)), gb = source_at(step_b(fetch_kt));
+        static_for<SLOTS>([&](auto SLOT) {
+            constexpr int slot = decltype(SLOT)::value;
+            if constexpr (slot == SYNC_A) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): my reads of stage S are back
+                __syncthreads();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (slot == SYNC_B) {
+                __builtin_amdgcn_s_waitcnt(kWaitB);
+                __syncthreads();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            mfma_slot(S, SLOT);
+            if constexpr (slot < HM) {
+                read_a(S, integral_constant<int, HM + slot>{});
+                if constexpr (s == 0) read_sa(integral_constant<int, HM + slot>{});
+            }
+            if constexpr (slot >= HALF && slot < HALF + HM) {
+                read_a(OTHER{}, integral_constant<int, slot - HALF>{});
+                if constexpr (s == 1) read_sa(integral_constant<int, slot - HALF>{});
+            }
+            static_for<TN>([&](auto J) {
+                constexpr int j = decltype(J)::value;
+                if constexpr (slot_of_next_b(j) == slot) {
+                    if constexpr (slot < HALF + (j + 1) * HM - 1) {  // fb[j] is still needed: park its successor
+                        static_assert(j == TN - 1, "one spare fragment");
+                        const Frag keep = fb[j];
+                        const int keep_scale = sb[j];
+                        read_b(OTHER{}, J);
+                        if constexpr (s == 1) read_sb(J);
+                        fb_early = fb[j], sb_early = sb[j];
+                        fb[j] = keep, sb[j] = keep_scale;
+                    } else {
+                        read_b(OTHER{}, J);
+                        if constexpr (s == 1) read_sb(J);
+                    }
+                }
+            });
+            if constexpr (slot == SLOTS - 1 && slot_of_next_b(TN - 1) < SLOTS - 1) fb[TN - 1] = fb_early, sb[TN - 1] = sb_early;
+            static_for<LOADS>([&](auto I) {
+                if constexpr (slot_of_load(decltype(I)::value) == slot) issue_one(ga, gb, S, I);
+            });
+            if constexpr (s == 0 && slot == SLOTS - 4) issue_scales(fetch_kt, I0{});
+            if constexpr (s == 0 && slot == SLOTS - 2) issue_scales(fetch_kt, I1{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    // ---- main loop.  The step computed at kt fetches step kt + 2; the last two of a tile fetch the first two of the next one.
+    for (int item = (int)blockIdx.x; item < total; item += (int)gridDim.x) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), once per tile: see gemm_tile_kernel
+        for (int kt = 0; kt < KT; kt += 2) {
+            if (kt == KT - 2) next_item();
+            const int f = kt == KT - 2 ? 0 : kt + 2;
+            cut_loads(f);
+            kstep(I0{}, f);
+            cut_loads(f + 1);
+            kstep(I1{}, f + 1);
+        }
+        drain();
+        epilogue(item);
+        zero_acc();
+        read_first_set(I0{});
+        asm volatile("s_nop 7");  // accumulators just written by ordinary instructions: let them settle
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // no load may still be writing LDS when the workgroup ends
+}
+
+// partial[s][M][N] fp32 of s < splits ranges, added in their order; a thread owns eight columns.
+__global__ __launch_bounds__(256) void mx4_reduce_kernel(const float* __restrict__ partial, int splits, int M, int N, uint16_t* __restrict__ D, int64_t ldd)
+{
+    const int chunks = N / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)M * chunks) return;
+    const int m = (int)(i / chunks), n = (int)(i % chunks) * 8;
+    const float* q = partial + (int64_t)m * N + n;
+    const int64_t stride = (int64_t)M * N;
+    v4f lo = *reinterpret_cast<const v4f*>(q), hi = *reinterpret_cast<const v4f*>(q + 4);
+    for (int s = 1; s < splits; ++s) lo += *reinterpret_cast<const v4f*>(q + s * stride), hi += *reinterpret_cast<const v4f*>(q + s * stride + 4);
+    *reinterpret_cast<uint4*>(D + (int64_t)m * ldd + n) =
+        make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+}
+
 // ---- host ----------------------------------------------------------------------------------------
 
 template <int TM, int TN, int STAGES>
@@ -123,14 +472,108 @@ static void launch_rows(const Mx4Args& a, hipStream_t st)
     mx4_rows_kernel<TM, TN, STAGES><<<(unsigned)(tiles_m * tiles_n), 256, 0, st>>>(a, tiles_m, tiles_n);
 }
 
-size_t mx4_split_bytes(int64_t, int64_t, int64_t) { return 0; }
+// Steps of a work item when the contraction is cut into `ranges`: whole pairs, at least one.
+static int steps_of(int K, int ranges)
+{
+    const int groups = (K + kMxGroup - 1) / kMxGroup, per = (groups + ranges - 1) / ranges;
+    return 2 * (per > 0 ? per : 1);
+}
 
-f8_status mx4_gemm(const Mx4Args& a, void*, size_t, hipStream_t st)
+template <int BM, int BN>
+static void launch_tiles(const Mx4Args& a, int most, hipStream_t st)
+{
+    const int tiles_m = (a.M - a.m0 + BM - 1) / BM, tiles_n = (a.N - a.n0 + BN - 1) / BN, total = tiles_m * tiles_n;
+    const auto kernel = a.K % kMxGroup ? mx4_tile_kernel<BM, BN, false, true> : mx4_tile_kernel<BM, BN, false, false>;
+    kernel<<<(unsigned)(total < most ? total : most), 256, 0, st>>>(a, tiles_m, tiles_n, steps_of(a.K, 1), 1, nullptr);
+}
+
+struct Mx4Plan {
+    enum Kind { kRows, kSplit, kFull, kFullRows, kFullCols, kHalf, kQuarter } kind;
+    int ranges, whole;
+};
+
+// Ranges of the contraction for a product whose 256 x 256 tiles would occupy at most half of the compute units, or 1: chosen by
+// estimated time as in f8_gemm_kernels.hpp (a range is whole pairs of steps, at least two of them, and not empty).
+static int split_ranges(int64_t M, int64_t N, int64_t K, int cus, double best_unsplit, size_t ws_bytes)
+{
+    const int64_t T = ((M + 255) / 256) * ((N + 255) / 256);
+    if (2 * T > cus || K < 4096) return 1;
+    const double tile_us = (double)(K / kMxStep) * 1.0;
+    int best = 1;
+    double best_cost = best_unsplit;
+    for (int s = 2; s <= 8; s *= 2) {
+        if (s * T > cus || K / s < 2048) break;
+        if ((int64_t)(s - 1) * steps_of((int)K, s) * kMxStep >= K) break;
+        if ((size_t)s * (size_t)M * (size_t)N * sizeof(float) > ws_bytes) break;
+        const double reduce_us = 3.0 + (s + 0.5) * (double)M * (double)N * 4.0 / 5.0e6;
+        const double cost = 1.0 / s + 0.04 + reduce_us / tile_us;
+        if (cost < best_cost) best = s, best_cost = cost;
+    }
+    return best;
+}
+
+static Mx4Plan plan_product(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int cus)
+{
+    const auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    const auto rounds = [&](int64_t t) { return (double)((t + cus - 1) / cus); };
+    if (K == 0 || tiles(64, 64) <= 2 * cus) return {Mx4Plan::kRows, 1, 0};
+    const int64_t tm = (M + 255) / 256, tn = (N + 255) / 256, T = tm * tn, whole = T / cus * cus, rest = T - whole;
+    // A last round with at most half of the workgroups busy: the whole rounds on their own, the rest with tiles half as wide.
+    const bool by_rows = whole > 0 && rest > 0 && 2 * rest <= cus && whole % tn == 0, by_cols = !by_rows && whole > 0 && rest > 0 && 2 * rest <= cus && whole % tm == 0;
+    constexpr double kHalfTile = 0.63, kQuarterTile = 0.58;
+    const double full = by_rows || by_cols ? (double)(whole / cus) + kHalfTile : rounds(T);
+    const double half = rounds(tiles(256, 128)) * kHalfTile, quarter = rounds(tiles(128, 128)) * kQuarterTile;
+    const double best = full <= half && full <= quarter ? full : half <= quarter ? half : quarter;
+    const int ranges = split_ranges(M, N, K, cus, best, ws_bytes);
+    if (ranges > 1) return {Mx4Plan::kSplit, ranges, 0};
+    if (best == full) return {by_rows ? Mx4Plan::kFullRows : by_cols ? Mx4Plan::kFullCols : Mx4Plan::kFull, 1, (int)whole};
+    return {best == half ? Mx4Plan::kHalf : Mx4Plan::kQuarter, 1, 0};
+}
+
+size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (M == 0 || N == 0) return 0;
+    const Mx4Plan plan = plan_product(M, N, K, ~(size_t)0, cu_count());
+    return plan.kind == Mx4Plan::kSplit ? (size_t)plan.ranges * (size_t)M * (size_t)N * sizeof(float) : 0;
+}
+
+f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st)
 {
     if (a.M == 0 || a.N == 0) return last_launch_status();
-    if (a.M <= 16) launch_rows<1, 2, 5>(a, st);
-    else if (a.M <= 32) launch_rows<2, 2, 4>(a, st);
-    else launch_rows<4, 4, 2>(a, st);
+    const int cus = cu_count();
+    const Mx4Plan plan = plan_product(a.M, a.N, a.K, ws ? ws_bytes : 0, cus);
+    const int tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
+    switch (plan.kind) {
+        case Mx4Plan::kRows:
+            if (a.M <= 16) launch_rows<1, 2, 5>(a, st);
+            else if (a.M <= 32) launch_rows<2, 2, 4>(a, st);
+            else launch_rows<4, 4, 2>(a, st);
+            break;
+        case Mx4Plan::kSplit: {
+            const auto kernel = a.K % kMxGroup || a.K / kMxGroup % plan.ranges ? mx4_tile_kernel<256, 256, true, true> : mx4_tile_kernel<256, 256, true, false>;
+            kernel<<<(unsigned)(tm * tn * plan.ranges), 256, 0, st>>>(a, tm, tn, steps_of(a.K, plan.ranges), plan.ranges, (float*)ws);
+            const int64_t threads = (int64_t)a.M * (a.N / 8);
+            mx4_reduce_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>((const float*)ws, plan.ranges, a.M, a.N, a.D, a.ldd);
+            break;
+        }
+        case Mx4Plan::kFullRows:
+        case Mx4Plan::kFullCols: {
+            Mx4Args one = a, two = a;
+            if (plan.kind == Mx4Plan::kFullRows) {
+                one.M = plan.whole / tn * 256;
+                two.m0 = one.M;
+            } else {
+                one.N = plan.whole / tm * 256;
+                two.n0 = one.N;
+            }
+            launch_tiles<256, 256>(one, cus, st);
+            launch_tiles<256, 128>(two, cus, st);
+            break;
+        }
+        case Mx4Plan::kFull: launch_tiles<256, 256>(a, cus, st); break;
+        case Mx4Plan::kHalf: launch_tiles<256, 128>(a, cus, st); break;
+        case Mx4Plan::kQuarter: launch_tiles<128, 128>(a, 2 * cus, st); break;
+    }
     return last_launch_status();
 }
 
