@@ -173,14 +173,16 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
         const int m0 = p.m0 + tm * BM, n0 = p.n0 + tn * BN;
         a_base = p.A + (int64_t)m0 * pitch + koff, b_base = p.B + (int64_t)n0 * pitch + koff;
         const int a_last = p.M - 1 - m0, b_last = p.N - 1 - n0;
+        int row8 = lane >> 3;
+        asm volatile("" : "+v"(row8));  // (the rows are not to be kept in registers)
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) {
-            const int row = wave * (BM / NW) + 8 * i + (lane >> 3);
+            const int row = wave * (BM / NW) + 8 * i + row8;
             a_off[i] = (uint32_t)(row < a_last ? row : a_last) * (uint32_t)pitch + chunk;
         }
 #pragma unroll
         for (int i = 0; i < B_LOADS; ++i) {
-            const int row = wave * (BN / NW) + 8 * i + (lane >> 3);
+            const int row = wave * (BN / NW) + 8 * i + row8;
             b_off[i] = (uint32_t)(row < b_last ? row : b_last) * (uint32_t)pitch + chunk;
         }
         // this wave's 64 rows of each operand's scales (the last ones again past the end)
@@ -276,14 +278,18 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
                      : "v"(b), "v"(a), "v"(tb), "v"(ta), "n"(byte & 1), "n"(byte >> 1));
     };
     auto mfma_slot = [&](auto S, auto SLOT) {
-        constexpr int s = decltype(SLOT)::value, q = s / 2 * 2;
-        mfma(S, integral_constant<int, q>{}, integral_constant<int, s % 2>{});
-        mfma(S, integral_constant<int, q + 1>{}, integral_constant<int, s % 2>{});
+        mfma(S, SLOT, I0{});
+        mfma(S, SLOT, I1{});
     };
     auto drain = [&]() { asm volatile("s_nop 15\n\ts_nop 15"); };  // nothing interlocks an accumulator's first ordinary read
 
-    // ---- epilogue of one tile, as in gemm_tile_kernel
+    // ---- epilogue of one tile, as in gemm_tile_kernel, but its stores are still under way when the next tile begins: the loads
+    // that one starts with are waited for before them, so its first step waits for no load
     auto epilogue = [&](int item) {
+        int lane = (int)threadIdx.x & 63;  // (not to be kept in registers over the products, nor what follows from it)
+        asm volatile("" : "+v"(lane));
+        const int fr = lane & 15, fg = lane >> 4;
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
         int tm, tn;
         tile_coords(SPLITK ? item % tiles_mn : item, tiles_m, tiles_n, &tm, &tn);
         const int m0 = p.m0 + tm * BM + wm * WM, n0 = p.n0 + tn * BN + wn * WN;
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
     };
     constexpr int kWaitB = (PRE_B & 15) | ((PRE_B >> 4) << 14) | 0x0070;  // vmcnt(PRE_B) lgkmcnt(0)
 
-    auto kstep = [&](auto S, int fetch_kt) {
+    auto kstep = [&](auto S, int fetch_kt, bool first) {
         constexpr int s = decltype(S)::value;
         using OTHER = integral_constant<int, 1 - s>;
         const auto ga = source_at(step_a(fetch_kt)), gb = source_at(step_b(fetch_kt));
@@ -388,7 +394,8 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (slot == SYNC_B) {
-                __builtin_amdgcn_s_waitcnt(kWaitB);
+                if (s == 0 && first) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+                else __builtin_amdgcn_s_waitcnt(kWaitB);
                 __syncthreads();
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -430,14 +437,13 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
 
     // ---- main loop.  The step computed at kt fetches step kt + 2; the last two of a tile fetch the first two of the next one.
     for (int item = (int)blockIdx.x; item < total; item += (int)gridDim.x) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), once per tile: see gemm_tile_kernel
         for (int kt = 0; kt < KT; kt += 2) {
             if (kt == KT - 2) next_item();
             const int f = kt == KT - 2 ? 0 : kt + 2;
             cut_loads(f);
-            kstep(I0{}, f);
+            kstep(I0{}, f, kt == 0);
             cut_loads(f + 1);
-            kstep(I1{}, f + 1);
+            kstep(I1{}, f + 1, false);
         }
         drain();
         epilogue(item);
