@@ -258,7 +258,24 @@ static void for_launches(const f8_tensor* in, const f8_tensor* out, int64_t coun
     }
     if (l.count) f(l);
 }
-static unsigned grad_blocks(const TensorList& l) { return l.first[l.count] < kGradBlocks ? l.first[l.count] : kGradBlocks; }
+static unsigned grad_blocks(uint32_t steps) { return steps < kGradBlocks ? steps : kGradBlocks; }
+// Blocks of all launches: as for_launches deals the tensors out.
+static int64_t all_blocks(const f8_tensor* list, int64_t count)
+{
+    int64_t blocks = 0, steps = 0, tensors = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (list[i].n == 0) continue;
+        const int64_t more = (list[i].n + kStep - 1) / kStep;
+        if (tensors == kTensors || steps + more > 0x7FFFFFFF) blocks += grad_blocks((uint32_t)steps), steps = tensors = 0;
+        steps += more, ++tensors;
+    }
+    return blocks + grad_blocks((uint32_t)steps);
+}
+static size_t norm_bytes(const f8_tensor* list, int64_t count)
+{
+    const size_t bytes = (size_t)all_blocks(list, count) * sizeof(double);
+    return bytes < kMinWorkspaceBytes ? kMinWorkspaceBytes : bytes;
+}
 
 }  // namespace f8
 
@@ -268,10 +285,7 @@ extern "C" {
 
 size_t f8_grad_norm_workspace_bytes(const f8_tensor* list, int64_t count)
 {
-    size_t parts = 0;
-    if (check_list(list, count) == F8_OK) for_launches(list, nullptr, count, [&](const TensorList& l) { parts += grad_blocks(l); });
-    const size_t bytes = parts * sizeof(double);
-    return bytes < kMinWorkspaceBytes ? kMinWorkspaceBytes : bytes;
+    return check_list(list, count) == F8_OK ? norm_bytes(list, count) : kMinWorkspaceBytes;
 }
 
 f8_status f8_grad_norm(const f8_tensor* list, int64_t count, f8_norm kind, float* norm, double* sum, void* workspace, size_t workspace_bytes_, void* stream)
@@ -281,13 +295,13 @@ f8_status f8_grad_norm(const f8_tensor* list, int64_t count, f8_norm kind, float
     if (s != F8_OK) return s;
     if (!norm && !sum) return F8_ERR_NULL;
     if (!aligned16(workspace) || ((uintptr_t)norm & 3) || ((uintptr_t)sum & 7)) return F8_ERR_ALIGN;
-    if (!workspace || workspace_bytes_ < f8_grad_norm_workspace_bytes(list, count)) return F8_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes_ < norm_bytes(list, count)) return F8_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     double* const part = (double*)workspace;
     int64_t parts = 0;
     const bool max = kind == F8_NORM_MAX;
     for_launches(list, nullptr, count, [&](const TensorList& l) {
-        const unsigned b = grad_blocks(l);
+        const unsigned b = grad_blocks(l.first[l.count]);
         (max ? grad_norm_kernel<true> : grad_norm_kernel<false>)<<<b, kGradThreads, 0, st>>>(l, part + parts);
         parts += b;
     });

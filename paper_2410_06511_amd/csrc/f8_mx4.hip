@@ -16,37 +16,44 @@ struct Mx4Cast {
     int64_t ld;
     int rows, cols;
     uint8_t *q, *s, *q_t, *s_t;  // either orientation nullable
-    int tiles_c, blocks;
+    int squares, squares_c, blocks;  // squares of 4 x 4 tiles, those side by side
 };
 
-// Tiles of 128 x 128.  Along the rows a thread has whole blocks of 32 as they lie in memory; for the other orientation the tile
-// goes through LDS, where a thread takes 32 rows of two columns.
+// Tiles of 128 x 128.  Along the rows four threads have a block of 32; for the other orientation the tile goes through LDS, where a
+// thread takes 32 rows of two columns.
+// A tile writes half lines of codes and a quarter of each 16 bytes of scales: the tiles of a square of 512 x 512 follow each other
+// on one XCD (workgroups go round the eight of them), whose L2 joins their pieces.
 constexpr int kMxTile = 128;
 
 __device__ inline void mx4_cast_tile(const Mx4Cast& p, int block, uint32_t (&tile)[kMxTile][kMxTile / 2])
 {
-    const int t = threadIdx.x, r0 = block / p.tiles_c * kMxTile, c0 = block % p.tiles_c * kMxTile;
+    const int square = block / 128 * 8 + block % 8, in = block / 8 % 16;
+    if (square >= p.squares) return;
+    const int t = threadIdx.x, r0 = (square / p.squares_c * 4 + in / 4) * kMxTile, c0 = (square % p.squares_c * 4 + in % 4) * kMxTile;
+    if ((r0 >= p.rows && !(p.q_t && c0 < mx4_rows(p.cols))) || (c0 >= p.cols && !(p.q && r0 < mx4_rows(p.rows)))) return;  // not even padding
     const bool turn = p.q_t != nullptr;
     const int64_t pitch = mx4_pitch(p.cols), srows = mx4_rows(p.rows);
+    // 16 threads take a row's 16-byte chunks, four of them a block
+    constexpr int PER = kMxTile * kMxTile / 8 / 256;
+    const int k = t % 16, col = c0 + 8 * k;
+    uint4 v[PER];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = i * 64 + t / 4, b = t % 4, row = r0 + r, col = c0 + 32 * b;
-        uint4 v[4];
+    for (int i = 0; i < PER; ++i) {
+        const int row = r0 + 16 * i + t / 16;
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (row < p.rows && col < p.cols) v[i] = *reinterpret_cast<const uint4*>(p.x + (int64_t)row * p.ld + col);
+    }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[k] = make_uint4(0, 0, 0, 0);
-            if (row < p.rows && col + 8 * k < p.cols) v[k] = *reinterpret_cast<const uint4*>(p.x + (int64_t)row * p.ld + col + 8 * k);
-        }
-        if (turn) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(&tile[r][16 * b + 4 * k]) = v[k];
-        }
+    for (int i = 0; i < PER; ++i) {
+        const int r = 16 * i + t / 16, row = r0 + r;
+        if (turn) *reinterpret_cast<uint4*>(&tile[r][4 * k]) = v[i];
         if (p.q) {
-            const uint32_t code = mx4_scale_of(v);
-            if (row < p.rows && col < p.cols) *reinterpret_cast<uint4*>(p.q + row * pitch + col / 2) = mx4_encode(v, code);
+            const uint32_t code = mx4_scale_of_quad(v[i]);
+            const bool real = row < p.rows && col / kMxBlock * kMxBlock < p.cols;
+            if (real) *reinterpret_cast<uint32_t*>(p.q + row * pitch + col / 2) = mx4_encode8(v[i], code);
             // (rows of padding too, and blocks up to the group's end)
-            if (row < srows && col < (p.cols + kMxGroup - 1) / kMxGroup * kMxGroup)
-                p.s[mx4_scale_at(srows, row, col / kMxBlock)] = (uint8_t)(row < p.rows && col < p.cols ? code : 127);
+            if (k % 4 == 0 && row < srows && col < (p.cols + kMxGroup - 1) / kMxGroup * kMxGroup)
+                p.s[mx4_scale_at(srows, row, col / kMxBlock)] = (uint8_t)(real ? code : 127);
         }
     }
     if (!turn) return;
@@ -56,23 +63,23 @@ __device__ inline void mx4_cast_tile(const Mx4Cast& p, int block, uint32_t (&til
     uint32_t w[32];
 #pragma unroll
     for (int k = 0; k < 32; ++k) w[k] = tile[32 * wave + k][lane];
-    uint4 v[2][4];
+    uint4 turned[2][4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         uint32_t lo[4], hi[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t a = w[8 * k + 2 * j], b = w[8 * k + 2 * j + 1];
-            lo[j] = (a & 0xFFFFu) | (b << 16), hi[j] = (a >> 16) | (b & 0xFFFF0000u);
+            lo[j] = __builtin_amdgcn_perm(b, a, 0x05040100), hi[j] = __builtin_amdgcn_perm(b, a, 0x07060302);  // the halves of both
         }
-        v[0][k] = make_uint4(lo[0], lo[1], lo[2], lo[3]), v[1][k] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        turned[0][k] = make_uint4(lo[0], lo[1], lo[2], lo[3]), turned[1][k] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int col = c0 + 2 * lane + h;
         const bool real = col < p.cols && rb * kMxBlock < p.rows;
-        const uint32_t code = mx4_scale_of(v[h]);
-        if (real) *reinterpret_cast<uint4*>(p.q_t + col * pitch_t + (int64_t)rb * 16) = mx4_encode(v[h], code);
+        const uint32_t code = mx4_scale_of(turned[h]);
+        if (real) *reinterpret_cast<uint4*>(p.q_t + col * pitch_t + (int64_t)rb * 16) = mx4_encode(turned[h], code);
         if (col < srows_t && rb * kMxBlock < (p.rows + kMxGroup - 1) / kMxGroup * kMxGroup) p.s_t[mx4_scale_at(srows_t, col, rb)] = (uint8_t)(real ? code : 127);
     }
 }
@@ -101,15 +108,13 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(const uint8_t* __restri
 
 // ---- host ----------------------------------------------------------------------------------------
 
-// Blocks: enough tiles for the codes of both orientations, their padding and the scales' (a group of 512 past the end, and 64 rows).
+// (Squares of 512 x 512 hold the codes of both orientations, their padding and the scales': whole groups of 512, and 64 rows.)
 static Mx4Cast cast_of(const void* x, int64_t rows, int64_t cols, int64_t ld, const f8_mx4& o)
 {
-    const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m * m; };
-    const int64_t r = o.q_t ? up(rows, kMxGroup) : up(rows, kMxTile), c = o.q ? up(cols, kMxGroup) : up(cols, kMxTile);
-    const int64_t tiles_c = c / kMxTile, tiles = rows > 0 && cols > 0 ? r / kMxTile * tiles_c : 0;
-    return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)tiles_c, (int)tiles};
+    const int64_t across = (cols + kMxGroup - 1) / kMxGroup, squares = rows > 0 && cols > 0 ? (rows + kMxGroup - 1) / kMxGroup * across : 0;
+    return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)squares, (int)across, (int)((squares + 7) / 8 * 128)};
 }
-static bool too_many(int64_t rows, int64_t cols) { return (rows / kMxTile + 4) * (cols / kMxTile + 4) > 0x3FFFFFFF; }
+static bool too_many(int64_t rows, int64_t cols) { return (rows / kMxGroup + 1) * (cols / kMxGroup + 1) > 0x2FFFFFF; }
 static void launch_cast(const Mx4Cast& a, const Mx4Cast& b, hipStream_t st)
 {
     if (a.blocks + b.blocks > 0) mx4_cast_kernel<<<(unsigned)(a.blocks + b.blocks), 256, 0, st>>>(a, b);

@@ -562,6 +562,8 @@ def _rows(name, t, shape, dev):
     if t is None:
         return None, 0
     if t.dtype is _BF16 and t.get_device() == dev and t.shape == shape:
+        if t.is_contiguous() and not shape[1] & 7:   # (the usual case: its strides need no look)
+            return t.data_ptr(), shape[1]
         ld, step = t.stride()
         if step == 1 or shape[1] <= 1:
             return t.data_ptr(), ld if shape[0] > 1 else (max(ld, shape[1]) + 7) // 8 * 8
@@ -583,7 +585,7 @@ def _room(ws, dev):
         return None, 0
     if ws.get_device() != dev or not ws.is_contiguous():
         _refuse("workspace", ws, ws.dtype, tuple(ws.shape))
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 def residual_norm(x, y, h, n=None, g_post=None, gate=None, g_pre=None, skip_scale=1.0, branch_scale=1.0, eps=1e-5, rstd_post=None, rstd_pre=None,
@@ -709,11 +711,14 @@ def layernorm(x, g, n, b=None, y=None, h=None, eps=1e-5, mean=None, rstd=None, a
     """h = x + y (x itself without y); n = (h - mean) rstd g + b."""
     shape = M, D = x.shape
     of_d, of_m, dev = (D,), (M,), _current()
-    (xp, ldx), (yp, ldy), (hp, ldh), (np_, ldn) = _rows("x", x, shape, dev), _rows("y", y, shape, dev), _rows("h", h, shape, dev), _rows("n", n, shape, dev)
-    wp, wb = _room(workspace, dev)
-    _check(lib().f8_layernorm(xp, ldx, yp, ldy, M, D, _packed("g", g, _BF16, of_d, dev), _packed("b", b, _BF16, of_d, dev), eps, hp, ldh, np_, ldn,
-                              _packed("mean", mean, _F32, of_m, dev), _packed("rstd", rstd, _F32, of_m, dev), _packed("amax_n", amax_n, _F32, (1,), dev), wp, wb,
-                              _stream(stream)))
+    (xp, ldx), (np_, ldn) = _rows("x", x, shape, dev), _rows("n", n, shape, dev)
+    (yp, ldy), (hp, ldh) = ((None, 0), (None, 0)) if y is None and h is None else (_rows("y", y, shape, dev), _rows("h", h, shape, dev))
+    wp, wb = (None, 0) if workspace is None else _room(workspace, dev)
+    code = lib().f8_layernorm(xp, ldx, yp, ldy, M, D, _packed("g", g, _BF16, of_d, dev), None if b is None else _packed("b", b, _BF16, of_d, dev), eps, hp, ldh, np_, ldn,
+                              None if mean is None else _packed("mean", mean, _F32, of_m, dev), None if rstd is None else _packed("rstd", rstd, _F32, of_m, dev),
+                              None if amax_n is None else _packed("amax_n", amax_n, _F32, (1,), dev), wp, wb, _stream(stream))
+    if code:
+        _check(code)
 
 
 def layernorm_bwd_workspace_bytes(M, D):
@@ -743,6 +748,7 @@ class GradList:
                 raise F8Error(F8_ERR_SHAPE, f"tensor {i} of a list: a contiguous tensor of bf16 or fp32 on the list's GPU is wanted; got {t.dtype}, "
                                             f"{tuple(t.shape)}, strides {t.stride()} on {t.device}")
         self._struct = (TensorStruct * len(self.tensors))(*[(t.data_ptr(), t.numel(), F32 if t.dtype is _F32 else BF16) for t in self.tensors])
+        self._address, self._n = C.addressof(self._struct), len(self.tensors)
 
     def __len__(self):
         return len(self.tensors)
@@ -750,27 +756,27 @@ class GradList:
     def struct(self, name, dev):
         if self.tensors and self.device != dev:
             raise F8Error(F8_ERR_SHAPE, f"{name}: tensors on device {self.device}, not on the current one, {dev}")
-        return C.addressof(self._struct)
+        return self._address
 
 
 def grad_norm_workspace_bytes(grads):
-    return int(lib().f8_grad_norm_workspace_bytes(C.addressof(grads._struct), len(grads)))
+    return int(lib().f8_grad_norm_workspace_bytes(grads._address, grads._n))
 
 
 def grad_norm(grads, norm=None, total=None, kind=NORM_2, workspace=None, stream=None):
     """grads: GradList; norm [1] fp32; total [1] fp64: the sum of squares (NORM_MAX: the largest magnitude), e.g. for a reduction over ranks."""
     dev = _current()
     wp, wb = _room(workspace, dev)
-    _check(lib().f8_grad_norm(grads.struct("grads", dev), len(grads), kind, _packed("norm", norm, _F32, (1,), dev), _packed("total", total, torch.float64, (1,), dev),
-                              wp, wb, _stream(stream)))
+    _check(lib().f8_grad_norm(grads.struct("grads", dev), grads._n, kind, _packed("norm", norm, _F32, (1,), dev),
+                              None if total is None else _packed("total", total, torch.float64, (1,), dev), wp, wb, _stream(stream)))
 
 
 def grad_clip(grads, norm, most, out=None, stream=None):
     """grads scaled by min(1, most / (norm + 1e-6)), in place or into the tensors of `out` (a GradList of the same sizes and types)."""
     dev = _current()
-    if out is not None and len(out) != len(grads):
-        raise F8Error(F8_ERR_SHAPE, f"{len(out)} tensors for {len(grads)}")
-    _check(lib().f8_grad_clip(grads.struct("grads", dev), None if out is None else out.struct("out", dev), len(grads), _packed("norm", norm, _F32, (1,), dev), most,
+    if out is not None and out._n != grads._n:
+        raise F8Error(F8_ERR_SHAPE, f"{out._n} tensors for {grads._n}")
+    _check(lib().f8_grad_clip(grads.struct("grads", dev), None if out is None else out.struct("out", dev), grads._n, _packed("norm", norm, _F32, (1,), dev), most,
                               _stream(stream)))
 
 
@@ -794,7 +800,7 @@ class MX4Tensor:
         codes = lambda r, c: (torch.empty((r, 16 * ((c + 31) // 32)), **u8), torch.empty(mx4_scale_bytes(r, c), **u8))
         self.q, self.s = codes(rows, cols) if "q" in sides else (None, None)
         self.q_t, self.s_t = codes(cols, rows) if "t" in sides else (None, None)
-        self.device = torch.device(device)
+        self.device = (self.q if self.q is not None else self.q_t).get_device()   # (-1: not on a GPU)
         self._struct = MX4Struct(_ptr(self.q), _ptr(self.s), _ptr(self.q_t), _ptr(self.s_t))
 
     def struct(self):
@@ -811,19 +817,20 @@ class MX4Saved:
         self.x = x if x is not None else MX4Tensor(M, K, sides, device)
         self.w = MX4Tensor(N, K, sides, device)
         self.dy = MX4Tensor(M, N, sides, device) if backward else None
-        if (self.x.rows, self.x.cols) != (M, K):
-            raise F8Error(F8_ERR_SHAPE, f"codes of [{self.x.rows}, {self.x.cols}] for an input of [{M}, {K}]")
+        self.device = self.w.device
+        if (self.x.rows, self.x.cols) != (M, K) or self.x.device != self.device:
+            raise F8Error(F8_ERR_SHAPE, f"codes of [{self.x.rows}, {self.x.cols}] on device {self.x.device} for an input of [{M}, {K}] on {self.device}")
         self._struct = MX4SavedStruct(self.x.struct(), self.w.struct(), self.dy.struct() if backward else MX4Struct())
         self._desc = MX4Desc(M, K, N)
+        self._ref, self._desc_ref = C.byref(self._struct), C.byref(self._desc)
 
     def struct(self):
         return self._struct
 
 
 def _on_current(name, t, dev):
-    for b in (t.q, t.q_t):
-        if b is not None and b.get_device() != dev:
-            raise F8Error(F8_ERR_SHAPE, f"{name}: codes on {b.device}, not on the current GPU, {dev}")
+    if t.device != dev:
+        raise F8Error(F8_ERR_SHAPE, f"{name}: codes on device {t.device}, not on the current GPU, {dev}")
 
 
 def mx4_quantise(x, t, stream=None):
@@ -860,10 +867,10 @@ def mx4_gemm(a, b, D, workspace=None, stream=None):
 def mx4_linear_fwd(X, W, Y, saved, workspace=None, stream=None):
     """Y = X4 W4^T; W None: saved.w holds the weight's codes already."""
     dev, M, K, N = _current(), saved.M, saved.K, saved.N
-    _on_current("saved", saved.x, dev), _on_current("saved", saved.w, dev)
+    _on_current("saved", saved, dev)
     wp, wb = _room(workspace, dev)
-    _check(lib().f8_mx4_linear_fwd(C.byref(saved._desc), _packed("X", X, _BF16, (M, K), dev), _packed("W", W, _BF16, (N, K), dev), _packed("Y", Y, _BF16, (M, N), dev),
-                                   C.byref(saved.struct()), wp, wb, _stream(stream)))
+    _check(lib().f8_mx4_linear_fwd(saved._desc_ref, _packed("X", X, _BF16, (M, K), dev), None if W is None else _packed("W", W, _BF16, (N, K), dev),
+                                   _packed("Y", Y, _BF16, (M, N), dev), saved._ref, wp, wb, _stream(stream)))
 
 
 def mx4_linear_bwd(dY, saved, dX, dW, workspace=None, stream=None):
@@ -871,9 +878,9 @@ def mx4_linear_bwd(dY, saved, dX, dW, workspace=None, stream=None):
     dev, M, K, N = _current(), saved.M, saved.K, saved.N
     if saved.dy is None:
         raise F8Error(1, "mx4_linear_bwd: a linear that was made without a backward")
-    _on_current("saved", saved.x, dev), _on_current("saved", saved.w, dev), _on_current("saved", saved.dy, dev)
+    _on_current("saved", saved, dev)
     wp, wb = _room(workspace, dev)
-    _check(lib().f8_mx4_linear_bwd(C.byref(saved._desc), _packed("dY", dY, _BF16, (M, N), dev), C.byref(saved.struct()), _packed("dX", dX, _BF16, (M, K), dev),
+    _check(lib().f8_mx4_linear_bwd(saved._desc_ref, _packed("dY", dY, _BF16, (M, N), dev), saved._ref, _packed("dX", dX, _BF16, (M, K), dev),
                                    _packed("dW", dW, _BF16, (N, K), dev), wp, wb, _stream(stream)))
 
 
