@@ -10,7 +10,8 @@ constexpr int kMxStep = 2 * kBK;  // elements of a step: rows of 128 bytes, two 
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-__device__ inline v8i fp4_operand(v4i x) { return v8i{x[0], x[1], x[2], x[3], 0, 0, 0, 0}; }
+// (an fp4 operand is four registers; what the builtin's type has above them is never read)
+__device__ inline v8i fp4_operand(v4i x) { return __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1); }
 
 __device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p; }
 __device__ inline v4u buffer_at(const uint8_t* p) { return v4u{(uint32_t)(uint64_t)p, (uint32_t)((uint64_t)p >> 32), kRecords, 0x00020000u}; }
@@ -111,6 +112,125 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
 #pragma unroll
         for (int w = 1; w < NW; ++w) t += *reinterpret_cast<const v4f*>(&sums[w][r][c]);
         *reinterpret_cast<uint2*>(p.D + (int64_t)m * p.ldd + n) = make_uint2(pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3]));
+    }
+}
+
+// ---- few rows, many columns ------------------------------------------------------------------------
+
+// Tiles of 16 TM x 64 with one ring of STAGES groups (512 elements of each row, with their scales) for eight waves: whatever the
+// height of the tile, all of the LDS but one group is under way, with one barrier a group.  Wave w has all rows and 32 of the
+// columns, and of each group the quarter w % 4; the four quarters' sums meet in LDS at the end.  (The LDS reads are what takes
+// longest: with 16 columns and half of each group a wave reads A twice as often, 300 x 4096 x 4096 10.0 us.  mx4_rows_kernel has
+// a ring for each wave, which a tile of this size leaves two steps.)
+template <int TM, int STAGES>
+__global__ __launch_bounds__(512) void mx4_strip_kernel(const Mx4Args p, int tiles_m, int tiles_n)
+{
+    constexpr int ROWS = 16 * TM, COLS = 64, HALF = (ROWS + COLS) * kBK, A_BYTES = ROWS * kBK, STAGE = 2 * HALF + (TM + 4) * 256;
+    // loads of a wave and group: eight rows of 128 bytes each of A and B, 16 rows' scales
+    constexpr int A_LOADS = TM / 2, B_LOADS = 2, S_LOADS = (TM + 4 + 7) / 8, LOADS = A_LOADS + B_LOADS + S_LOADS;
+    constexpr int PITCH = COLS + 4;  // floats
+    static_assert(TM % 2 == 0 && STAGES * STAGE <= 160 * 1024 && (STAGES - 1) * LOADS < 64 && 4 * ROWS * PITCH * 4 <= STAGES * STAGE, "LDS; wait count; the sums take the ring's place");
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[STAGES][STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int quarter = wave % 4, cols0 = wave / 4 * 32, fr = lane & 15, fg = lane >> 4;
+    int tm, tn;
+    tile_coords((int)blockIdx.x, tiles_m, tiles_n, &tm, &tn);
+    const int m0 = tm * ROWS, n0 = tn * COLS;
+    const int64_t pitch = mx4_pitch(p.K);
+    const uint8_t *a_base = p.A + m0 * pitch, *b_base = p.B + n0 * pitch;
+
+    // Piece x of A: 8 rows (see mx4_rows_kernel) of the half x / (2 TM); wave w has the pieces w, w + 8, ..., of B the piece w of both
+    // halves, of the scales (16 rows, A's first) w and w + 8, or the last one again.
+    const int row8 = lane >> 3, chunk = 16 * ((lane & 7) ^ swz(row8));
+    uint32_t a_off[A_LOADS], b_off, a_lds[A_LOADS], s_lds[S_LOADS];
+    int a_begin[A_LOADS];  // of a lane's 16 bytes in a group's 256 of a row
+    const uint8_t* s_base[S_LOADS];
+    int64_t s_step[S_LOADS];
+#pragma unroll
+    for (int j = 0; j < A_LOADS; ++j) {
+        const int x = wave + 8 * j, h = x / (2 * TM), y = x % (2 * TM), row = 8 * y + row8;
+        a_begin[j] = h * kBK + chunk;
+        a_off[j] = row < p.M - m0 ? (uint32_t)row * (uint32_t)pitch + a_begin[j] : kPastEnd;
+        a_lds[j] = h * HALF + y * 1024;
+    }
+    b_off = 8 * wave + row8 < p.N - n0 ? (uint32_t)(8 * wave + row8) * (uint32_t)pitch + chunk : kPastEnd;
+#pragma unroll
+    for (int j = 0; j < S_LOADS; ++j) {
+        const int x = wave + 8 * j < TM + 4 ? wave + 8 * j : TM + 3;
+        const bool is_a = x < TM;
+        const int64_t rows = is_a ? p.a_srows : p.b_srows, row = is_a ? m0 + 16 * x : n0 + 16 * (x - TM);
+        s_base[j] = (is_a ? p.sa : p.sb) + (row < rows ? row : rows - 16) * 16;  // (past the end: some others)
+        s_step[j] = rows * 16, s_lds[j] = 2 * HALF + x * 256;
+    }
+    const uint32_t scale_off = lane * 4;
+    const int groups = (p.K + kMxGroup - 1) / kMxGroup;
+    const uint32_t ring0 = lds_address(&ring[0][0]);
+    auto request = [&](int g, int stage) {
+        const int64_t left = pitch - (int64_t)g * 2 * kBK, at = g < groups ? g : 0;  // left: bytes of a row, may be negative
+        const v4u a = buffer_at(a_base + at * 2 * kBK), b = buffer_at(b_base + at * 2 * kBK);
+        const uint32_t to = ring0 + stage * STAGE;
+        static_for<A_LOADS + B_LOADS>([&](auto J) {
+            constexpr int j = J(), h = j - A_LOADS;
+            uint32_t o, lds;
+            if constexpr (j < A_LOADS) o = a_begin[j] < left ? a_off[j] : kPastEnd, lds = to + a_lds[j];
+            else o = h * kBK + chunk < left ? b_off + h * kBK : kPastEnd, lds = to + h * HALF + A_BYTES + wave * 1024;
+            const v4u src = j < A_LOADS ? a : b;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(o), "s"(src) : "memory");
+        });
+        static_for<S_LOADS>([&](auto J) {
+            const v4u src = buffer_at(s_base[J()] + at * s_step[J()]);
+            const uint32_t o = g < groups ? scale_off : kPastEnd, lds = to + s_lds[J()];
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds), "v"(o), "s"(src) : "memory");
+        });
+    };
+    v4f acc[TM][2];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) acc[i][0] = acc[i][1] = v4f{0.f, 0.f, 0.f, 0.f};
+    static_for<STAGES - 1>([&](auto I) { request(I(), I()); });
+    constexpr int kWait = (STAGES - 2) * LOADS;
+    const int at = quarter / 2 * HALF + fr * kBK + 16 * ((quarter % 2 * 4 + fg) ^ swz(fr));  // of a fragment's first rows in a stage
+    int stage = 0;
+    for (int g = 0; g < groups; ++g) {
+        // this wave's loads of the oldest group have landed, and behind the barrier everyone's; everyone is done with the group
+        // before, whose place the request takes
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kWait) : "memory");
+        request(g + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+        const uint8_t *st = ring[stage] + at, *sc = ring[stage] + 2 * HALF + fr * 16 + fg * 4;
+        v4i a[TM], b[2];
+        int sa[TM], sb[2];  // (a word holds the four quarters' scales)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            b[j] = *reinterpret_cast<const v4i*>(st + A_BYTES + (cols0 + 16 * j) * kBK);
+            sb[j] = *reinterpret_cast<const int*>(sc + (TM + cols0 / 16 + j) * 256) >> 8 * quarter;
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            a[i] = *reinterpret_cast<const v4i*>(st + 16 * i * kBK);
+            sa[i] = *reinterpret_cast<const int*>(sc + i * 256) >> 8 * quarter;
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(b[j]), fp4_operand(a[i]), acc[i][j], kFp4, kFp4, 0, sb[j], 0, sa[i]);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // no load may still be writing the ring
+    __syncthreads();
+    float(*sums)[ROWS][PITCH] = reinterpret_cast<float(*)[ROWS][PITCH]>(&ring[0][0]);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<v4f*>(&sums[quarter][16 * i + fr][cols0 + 16 * j + 4 * fg]) = acc[i][j];
+    __syncthreads();
+    for (int q = threadIdx.x; q < ROWS * 8; q += 512) {  // eight neighbouring results
+        const int r = q / 8, c = q % 8 * 8;
+        if (m0 + r >= p.M || n0 + c >= p.N) continue;
+        v4f lo = *reinterpret_cast<const v4f*>(&sums[0][r][c]), hi = *reinterpret_cast<const v4f*>(&sums[0][r][c + 4]);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) lo += *reinterpret_cast<const v4f*>(&sums[k][r][c]), hi += *reinterpret_cast<const v4f*>(&sums[k][r][c + 4]);
+        *reinterpret_cast<uint4*>(p.D + (int64_t)(m0 + r) * p.ldd + n0 + c) =
+            make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
     }
 }
 
@@ -478,6 +598,13 @@ static void launch_rows(const Mx4Args& a, hipStream_t st)
     mx4_rows_kernel<TM, TN, STAGES><<<(unsigned)(tiles_m * tiles_n), 256, 0, st>>>(a, tiles_m, tiles_n);
 }
 
+template <int TM, int STAGES>
+static void launch_strip(const Mx4Args& a, hipStream_t st)
+{
+    const int tiles_m = (a.M + 16 * TM - 1) / (16 * TM), tiles_n = (a.N + 63) / 64;
+    mx4_strip_kernel<TM, STAGES><<<(unsigned)(tiles_m * tiles_n), 512, 0, st>>>(a, tiles_m, tiles_n);
+}
+
 // Steps of a work item when the contraction is cut into `ranges`: whole pairs, at least one.
 static int steps_of(int K, int ranges)
 {
@@ -493,47 +620,55 @@ static void launch_tiles(const Mx4Args& a, int most, hipStream_t st)
     kernel<<<(unsigned)(total < most ? total : most), 256, 0, st>>>(a, tiles_m, tiles_n, steps_of(a.K, 1), 1, nullptr);
 }
 
+// How a product is launched: by estimated time, in us.  A kernel whose tiles take r rounds of one tile a compute unit needs
+// start + r (tile + group G) for G groups of 512 of the contraction; the constants are fits to 24 sizes of 1 to 4096 rows, good to
+// 15 %, and no kernel is taken to read its operands faster than 4.2 TB/s.  What they decide between, each in its us (rows x columns
+// x contraction; tiles of 16 x 16, 32 x 32, 64 x 64 strips, 96 x 64 strips, 128 x 128, 256 x 256):
+//   1 x 4096 x 4096      4.5   5.0   7.1   9.0  12.7  25.4        300 x 4096 x 4096    53.5  20.2  13.8  10.0  12.9  25.4
+//   1 x 14336 x 4096    14.6  10.7   8.6  10.3  16.9  27.2        1000 x 14336 x 4096   621   223  93.6  87.0  41.4  31.6
 struct Mx4Plan {
-    enum Kind { kRows, kSplit, kFull, kFullRows, kFullCols, kHalf, kQuarter } kind;
-    int ranges, whole;
+    enum Kind { kRows11, kRows12, kRows22, kRows42, kStrip4, kStrip6, kStrip8, kQuarter, kHalf, kFull, kFullRows, kFullCols, kSplit } kind;
+    int ranges, whole;  // kSplit: ranges of the contraction; kFullRows, kFullCols: tiles in whole rounds, launched on their own
 };
-
-// Ranges of the contraction for a product whose 256 x 256 tiles would occupy at most half of the compute units, or 1: chosen by
-// estimated time as in f8_gemm_kernels.hpp (a range is whole pairs of steps, at least two of them, and not empty).
-static int split_ranges(int64_t M, int64_t N, int64_t K, int cus, double best_unsplit, size_t ws_bytes)
-{
-    const int64_t T = ((M + 255) / 256) * ((N + 255) / 256);
-    if (2 * T > cus || K < 4096) return 1;
-    const double tile_us = (double)(K / kMxStep) * 1.0;
-    int best = 1;
-    double best_cost = best_unsplit;
-    for (int s = 2; s <= 8; s *= 2) {
-        if (s * T > cus || K / s < 2048) break;
-        if ((int64_t)(s - 1) * steps_of((int)K, s) * kMxStep >= K) break;
-        if ((size_t)s * (size_t)M * (size_t)N * sizeof(float) > ws_bytes) break;
-        const double reduce_us = 3.0 + (s + 0.5) * (double)M * (double)N * 4.0 / 5.0e6;
-        const double cost = 1.0 / s + 0.04 + reduce_us / tile_us;
-        if (cost < best_cost) best = s, best_cost = cost;
-    }
-    return best;
-}
 
 static Mx4Plan plan_product(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int cus)
 {
     const auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const auto rounds = [&](int64_t t) { return (double)((t + cus - 1) / cus); };
-    if (K == 0 || tiles(64, 64) <= 2 * cus) return {Mx4Plan::kRows, 1, 0};
+    const double G = (double)((K + kMxGroup - 1) / kMxGroup);
+    if (K == 0) return {Mx4Plan::kRows22, 1, 0};
+    static constexpr struct {
+        Mx4Plan::Kind kind;
+        int bm, bn;
+        double start, tile, group;
+    } kKernels[] = {{Mx4Plan::kRows11, 16, 16, 1.7, 1.05, 0.22}, {Mx4Plan::kRows12, 16, 32, 1.5, 1.0, 0.26},  {Mx4Plan::kRows22, 32, 32, 1.26, 1.2, 0.32},
+                    {Mx4Plan::kRows42, 64, 32, 1.8, 1.2, 0.46},  {Mx4Plan::kStrip4, 64, 64, 1.2, 2.1, 0.52},  {Mx4Plan::kStrip6, 96, 64, 1.3, 2.9, 0.725},
+                    {Mx4Plan::kStrip8, 128, 64, 1.1, 3.5, 0.89}, {Mx4Plan::kHalf, 256, 128, 0.0, 3.5, 1.9}};
+    const double memory = 2.0 + (double)(M + N) * (double)K * 17.0 / 32.0 / 4.2e6;
+    Mx4Plan plan = {Mx4Plan::kFull, 1, 0};
+    double best;
+    const auto take = [&](Mx4Plan::Kind kind, double us) {
+        us = (us > memory ? us : memory) + 0.1 * us;  // (of those that the memory bounds, the one with the least work)
+        if (us < best) best = us, plan = {kind, 1, 0};
+    };
+    // 256 x 256: a last round with at most half of the workgroups busy goes to tiles half as wide, the whole rounds on their own
     const int64_t tm = (M + 255) / 256, tn = (N + 255) / 256, T = tm * tn, whole = T / cus * cus, rest = T - whole;
-    // A last round with at most half of the workgroups busy: the whole rounds on their own, the rest with tiles half as wide.
     const bool by_rows = whole > 0 && rest > 0 && 2 * rest <= cus && whole % tn == 0, by_cols = !by_rows && whole > 0 && rest > 0 && 2 * rest <= cus && whole % tm == 0;
-    constexpr double kHalfTile = 0.63, kQuarterTile = 0.58;
-    const double full = by_rows || by_cols ? (double)(whole / cus) + kHalfTile : rounds(T);
-    const double half = rounds(tiles(256, 128)) * kHalfTile, quarter = rounds(tiles(128, 128)) * kQuarterTile;
-    const double best = full <= half && full <= quarter ? full : half <= quarter ? half : quarter;
-    const int ranges = split_ranges(M, N, K, cus, best, ws_bytes);
-    if (ranges > 1) return {Mx4Plan::kSplit, ranges, 0};
-    if (best == full) return {by_rows ? Mx4Plan::kFullRows : by_cols ? Mx4Plan::kFullCols : Mx4Plan::kFull, 1, (int)whole};
-    return {best == half ? Mx4Plan::kHalf : Mx4Plan::kQuarter, 1, 0};
+    const double full = 8.0 + 3.1 * G, half = 3.5 + 1.9 * G;
+    best = 1e30;
+    take(by_rows ? Mx4Plan::kFullRows : by_cols ? Mx4Plan::kFullCols : Mx4Plan::kFull, by_rows || by_cols ? (double)(whole / cus) * full + half : rounds(T) * full);
+    plan.whole = (int)whole;
+    for (const auto& k : kKernels) take(k.kind, k.start + rounds(tiles(k.bm, k.bn)) * (k.tile + k.group * G));
+    const int64_t Q = tiles(128, 128);  // (two of these share a compute unit)
+    take(Mx4Plan::kQuarter, Q <= cus ? 2.6 + 1.45 * G : 3.6 + rounds(Q) * (1.65 + 0.93 * G));
+    // Ranges of the contraction, with their fp32 sums in the workspace: a range is whole groups, four at least, and not empty.
+    for (int s = 2; s <= 8 && s * T <= cus && K / s >= 4 * kMxGroup; s *= 2) {
+        const int groups = steps_of((int)K, s) / 2;
+        if ((int64_t)(s - 1) * groups * kMxGroup >= K || (size_t)s * (size_t)M * (size_t)N * sizeof(float) > ws_bytes) break;
+        take(Mx4Plan::kSplit, full - 3.1 * (G - groups) + 3.0 + (s + 0.5) * (double)M * (double)N * 4.0 / 5.0e6);
+        if (plan.kind == Mx4Plan::kSplit && plan.ranges == 1) plan.ranges = s;
+    }
+    return plan;
 }
 
 size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K)
@@ -550,11 +685,13 @@ f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st)
     const Mx4Plan plan = plan_product(a.M, a.N, a.K, ws ? ws_bytes : 0, cus);
     const int tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
     switch (plan.kind) {
-        case Mx4Plan::kRows:
-            if (a.M <= 16) launch_rows<1, 2, 5>(a, st);
-            else if (a.M <= 32) launch_rows<2, 2, 4>(a, st);
-            else launch_rows<4, 4, 2>(a, st);
-            break;
+        case Mx4Plan::kRows11: launch_rows<1, 1, 8>(a, st); break;
+        case Mx4Plan::kRows12: launch_rows<1, 2, 5>(a, st); break;
+        case Mx4Plan::kRows22: launch_rows<2, 2, 4>(a, st); break;
+        case Mx4Plan::kRows42: launch_rows<4, 2, 2>(a, st); break;
+        case Mx4Plan::kStrip4: launch_strip<4, 4>(a, st); break;
+        case Mx4Plan::kStrip6: launch_strip<6, 3>(a, st); break;
+        case Mx4Plan::kStrip8: launch_strip<8, 3>(a, st); break;
         case Mx4Plan::kSplit: {
             const auto kernel = a.K % kMxGroup || a.K / kMxGroup % plan.ranges ? mx4_tile_kernel<256, 256, true, true> : mx4_tile_kernel<256, 256, true, false>;
             kernel<<<(unsigned)(tm * tn * plan.ranges), 256, 0, st>>>(a, tm, tn, steps_of(a.K, plan.ranges), plan.ranges, (float*)ws);
