@@ -824,12 +824,16 @@ f8_status f8_linear_fwd_xq(const f8_linear_desc* d, const f8_scaling_state* stat
  * f8_mx4_linear_fwd: quantises X [M, K] and W [N, K] (bf16, packed) into saved->x
  *   and saved->w (each of the pairs that are given; q and s are needed, q_t and s_t
  *   for a backward), then Y [M, N] = X4 W4^T.  W NULL: saved->w holds the codes of
- *   an earlier call or of f8_mx4_quantise.
+ *   an earlier call or of f8_mx4_quantise.  Up to F8_MX4_TOKENS rows with K up to
+ *   F8_MX4_TOKEN_K need no codes of X: where saved->x is all NULL they are quantised
+ *   inside the product, in one launch, with the same result.
  * f8_mx4_linear_bwd: quantises dY [M, N] into saved->dy, then dX [M, K] = dY4 W4 from
  *   dy.q and w.q_t (blocks along N), and dW [N, K] = dY4^T X4 from dy.q_t and x.q_t
  *   (blocks along M).  dX or dW may be NULL, and the pairs for it.
  * M any number >= 0, K and N multiples of 16; all below 2^23.
  */
+#define F8_MX4_TOKENS 4
+#define F8_MX4_TOKEN_K 16384
 typedef struct f8_mx4 {
     uint8_t* q;
     uint8_t* s;

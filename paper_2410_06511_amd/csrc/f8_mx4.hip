@@ -191,17 +191,18 @@ f8_status f8_mx4_linear_fwd(const f8_mx4_desc* d, const void* X, const void* W, 
 {
     if (!d || !saved) return F8_ERR_NULL;
     if (bad_desc(d)) return F8_ERR_SHAPE;
-    f8_status s = check_codes(&saved->x, true, false);
+    const bool tokens = d->M <= kMxTokens && d->K <= kMxTokenK && !saved->x.q && !saved->x.q_t;  // X's codes are not wanted
+    f8_status s = check_codes(&saved->x, !tokens, false);
     if (s != F8_OK || (s = check_codes(&saved->w, true, false)) != F8_OK) return s;
     if (d->M && ((d->K && !X) || (d->N && !Y))) return F8_ERR_NULL;
     if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(workspace)) return F8_ERR_ALIGN;
     hipStream_t st = (hipStream_t)stream;
-    const Mx4Cast x = cast_of(X, d->M, d->K, d->K, saved->x), w = W ? cast_of(W, d->N, d->K, d->K, saved->w) : Mx4Cast{};
+    const Mx4Cast x = tokens ? Mx4Cast{} : cast_of(X, d->M, d->K, d->K, saved->x), w = W ? cast_of(W, d->N, d->K, d->K, saved->w) : Mx4Cast{};
     launch_cast(x, w, st);
     s = last_launch_status();
     if (s != F8_OK) return s;
-    return mx4_gemm({(int)d->M, (int)d->N, (int)d->K, saved->x.q, saved->x.s, saved->w.q, saved->w.s, (uint16_t*)Y, d->N}, workspace,
-                    workspace ? workspace_bytes_ : 0, st);
+    const Mx4Args a = {(int)d->M, (int)d->N, (int)d->K, saved->x.q, saved->x.s, saved->w.q, saved->w.s, (uint16_t*)Y, d->N};
+    return tokens ? mx4_gemm_tokens(a, (const uint16_t*)X, st) : mx4_gemm(a, workspace, workspace ? workspace_bytes_ : 0, st);
 }
 
 f8_status f8_mx4_linear_bwd(const f8_mx4_desc* d, const void* dY, const f8_mx4_saved* saved, void* dX, void* dW, void* workspace, size_t workspace_bytes_,

@@ -28,6 +28,9 @@ struct Mx4Args {
     int64_t a_srows = mx4_rows(M), b_srows = mx4_rows(N);  // rows of the operands' scales
 };
 f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st);
+// The same of up to kMxTokens rows from their bf16 values [M, K] (a.A and a.sa unused), quantised inside: the same bits.
+constexpr int kMxTokens = F8_MX4_TOKENS, kMxTokenK = F8_MX4_TOKEN_K;  // (their codes fit beside the ring in LDS)
+f8_status mx4_gemm_tokens(const Mx4Args& a, const uint16_t* X, hipStream_t st);
 size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K);  // the most that a product takes of a workspace
 
 }  // namespace f8

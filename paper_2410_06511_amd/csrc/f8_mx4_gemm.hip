@@ -18,10 +18,14 @@ __device__ inline v4u buffer_at(const uint8_t* p) { return v4u{(uint32_t)(uint64
 
 // Few rows: tiles of 16 TM x 16 TN whose four waves take every fourth step each, through a ring of STAGES steps in LDS that is
 // the wave's own, as in f8_gemm_rows.hip: no barrier until the sums meet, and the whole LDS is in flight.
-template <int TM, int TN, int STAGES>
-__global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tiles_m, int tiles_n)
+// TOKENS (TM = 1): A comes as up to kMxTokens rows of bf16, which every workgroup quantises for itself while its first steps of B
+// are under way: the codes that mx4_cast_kernel would have written, in LDS and without its launch.  (A lane that quantises its own
+// block in every step, on its way to the instruction, takes 0.8 us a step for it.)
+template <int TM, int TN, int STAGES, bool TOKENS = false>
+__global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tiles_m, int tiles_n, const uint16_t* __restrict__ X)
 {
-    constexpr int NW = 4, ROWS = 16 * TM, COLS = 16 * TN, PITCH = COLS + 4, T = TM + TN;
+    static_assert(TM == 1 || !TOKENS, "");
+    constexpr int NW = 4, ROWS = 16 * TM, COLS = 16 * TN, PITCH = COLS + 4, TA = TOKENS ? 0 : TM, T = TA + TN;  // fragments that come as codes
     constexpr int DATA = T * 16 * kBK, STAGE = DATA + T * 256, LOADS = 3 * T;
     static_assert(NW * ROWS * PITCH * 4 <= NW * STAGES * STAGE && NW * STAGES * STAGE <= 160 * 1024 && (STAGES - 1) * LOADS < 64, "LDS; wait count");
     __shared__ __attribute__((aligned(1024))) uint8_t ring[NW][STAGES][STAGE];
@@ -40,8 +44,8 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
     uint32_t off[2 * T];
     const int row8 = lane >> 3, chunk = 16 * ((lane & 7) ^ swz(row8));  // (the swizzle looks at bits 1 and 2 of the row only)
     static_for<2 * T>([&](auto L) {
-        constexpr int l = L(), r = l < 2 * TM ? 8 * l : 8 * (l - 2 * TM);
-        const int row = r + row8, left = l < 2 * TM ? p.M - m0 : p.N - n0;
+        constexpr int l = L(), r = l < 2 * TA ? 8 * l : 8 * (l - 2 * TA);
+        const int row = r + row8, left = l < 2 * TA ? p.M - m0 : p.N - n0;
         off[l] = row < left ? (uint32_t)row * (uint32_t)pitch + chunk : kPastEnd;
     });
     const uint32_t scale_off = fr * 16 + fg * 4;
@@ -55,13 +59,13 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
         static_for<2 * T>([&](auto L) {
             constexpr int l = L();
             const uint32_t o = chunk < left ? off[l] : kPastEnd, lds = to + l * 1024;
-            const v4u src = l < 2 * TM ? a : b;
+            const v4u src = l < 2 * TA ? a : b;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(o), "s"(src) : "memory");
         });
         static_for<T>([&](auto L) {
             constexpr int l = L();
-            const uint32_t o = kt < steps ? scale_off + (l < TM ? l : l - TM) * 256 : kPastEnd, lds = to + DATA + l * 256;
-            const v4u src = l < TM ? sa : sb;
+            const uint32_t o = kt < steps ? scale_off + (l < TA ? l : l - TA) * 256 : kPastEnd, lds = to + DATA + l * 256;
+            const v4u src = l < TA ? sa : sb;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds), "v"(o), "s"(src) : "memory");
         });
     };
@@ -72,7 +76,39 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
         for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
     const int mine = (steps - wave + NW - 1) / NW;
+    extern __shared__ __attribute__((aligned(16))) uint8_t tokens[];  // TOKENS: codes [M][pitch], then scales [group][M][16]
+    uint8_t* const token_scales = tokens + p.M * (int)pitch;
+    const int words = (int)pitch / 4, all_words = p.M * words;  // of eight codes
+    constexpr int FIRST = 2;
+    uint4 x[FIRST];
+    const auto eight = [&](int i) {  // the values of word i
+        const int row = i / words, k = i % words * 8;
+        return i < all_words && k < p.K ? *reinterpret_cast<const uint4*>(X + (int64_t)row * p.K + k) : make_uint4(0, 0, 0, 0);
+    };
+    const auto quantise = [&](int i, const uint4& v) {  // (four neighbouring lanes have a block)
+        const uint32_t code = mx4_scale_of_quad(v);
+        if (i >= all_words) return;
+        const int row = i / words, k = i % words, b = k / 4;
+        *reinterpret_cast<uint32_t*>(tokens + 4 * i) = mx4_encode8(v, code);
+        if (k % 4 == 0) token_scales[(b / 16 * p.M + row) * 16 + 4 * (b % 4) + b % 16 / 4] = (uint8_t)code;
+    };
+    if constexpr (TOKENS) {
+#pragma unroll
+        for (int u = 0; u < FIRST; ++u) x[u] = eight(u * 256 + (int)threadIdx.x);
+    }
     static_for<STAGES - 1>([&](auto I) { request(I(), I()); });
+    if constexpr (TOKENS) {
+#pragma unroll
+        for (int u = 0; u < FIRST; ++u) quantise(u * 256 + (int)threadIdx.x, x[u]);
+        for (int i0 = FIRST * 256; i0 < all_words; i0 += 4 * 256) {
+            uint4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = eight(i0 + u * 256 + (int)threadIdx.x);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) quantise(i0 + u * 256 + (int)threadIdx.x, v[u]);
+        }
+        __syncthreads();
+    }
     constexpr int kWait = (STAGES - 2) * LOADS;
     int stage = 0;
     for (int i = 0; i < mine; ++i) {
@@ -86,14 +122,31 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
         for (int x = 0; x < T; ++x) scale[x] = *reinterpret_cast<const int*>(st + DATA + x * 256 + lane * 4) >> 16 * (wave & 1);
         static_for<2>([&](auto J) {
             constexpr int j = J();
-            v8i f[T];
+            v8i f[TM + TN];
+            int sa[TM];
 #pragma unroll
-            for (int x = 0; x < T; ++x) f[x] = fp4_operand(*reinterpret_cast<const v4i*>(st + (16 * x + fr) * kBK + 16 * ((4 * j + fg) ^ swz(fr))));
+            for (int x = 0; x < T; ++x)
+                f[TM - TA + x] = fp4_operand(*reinterpret_cast<const v4i*>(st + (16 * x + fr) * kBK + 16 * ((4 * j + fg) ^ swz(fr))));
+            if constexpr (TOKENS) {
+                const int kt = wave + NW * i;
+                const bool some = fr < p.M && kt * kBK + 64 * j + 16 * fg < pitch;
+                v4i codes = {0, 0, 0, 0};
+                int word = 0;
+                if (some) {
+                    codes = *reinterpret_cast<const v4i*>(tokens + fr * (int)pitch + kt * kBK + 64 * j + 16 * fg);
+                    word = *reinterpret_cast<const int*>(token_scales + (kt / 2 * p.M + fr) * 16 + 4 * fg);
+                }
+                f[0] = fp4_operand(codes);
+                sa[0] = word >> 16 * (wave & 1);
+            } else {
+#pragma unroll
+                for (int x = 0; x < TM; ++x) sa[x] = scale[x];
+            }
 #pragma unroll
             for (int x = 0; x < TM; ++x)
 #pragma unroll
                 for (int y = 0; y < TN; ++y)
-                    acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f[TM + y], f[x], acc[x][y], kFp4, kFp4, j, scale[TM + y], j, scale[x]);
+                    acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f[TM + y], f[x], acc[x][y], kFp4, kFp4, j, scale[TA + y], j, sa[x]);
         });
         stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
@@ -591,11 +644,12 @@ __global__ __launch_bounds__(256) void mx4_reduce_kernel(const float* __restrict
 
 // ---- host ----------------------------------------------------------------------------------------
 
-template <int TM, int TN, int STAGES>
-static void launch_rows(const Mx4Args& a, hipStream_t st)
+template <int TM, int TN, int STAGES, bool TOKENS = false>
+static void launch_rows(const Mx4Args& a, hipStream_t st, const uint16_t* X = nullptr)
 {
     const int tiles_m = (a.M + 16 * TM - 1) / (16 * TM), tiles_n = (a.N + 16 * TN - 1) / (16 * TN);
-    mx4_rows_kernel<TM, TN, STAGES><<<(unsigned)(tiles_m * tiles_n), 256, 0, st>>>(a, tiles_m, tiles_n);
+    const size_t tokens = TOKENS ? (size_t)a.M * (mx4_pitch(a.K) + (a.K + kMxGroup - 1) / kMxGroup * 16) : 0;
+    mx4_rows_kernel<TM, TN, STAGES, TOKENS><<<(unsigned)(tiles_m * tiles_n), 256, tokens, st>>>(a, tiles_m, tiles_n, X);
 }
 
 template <int TM, int STAGES>
@@ -627,12 +681,14 @@ static void launch_tiles(const Mx4Args& a, int most, hipStream_t st)
 //   1 x 4096 x 4096      4.5   5.0   7.1   9.0  12.7  25.4        300 x 4096 x 4096    53.5  20.2  13.8  10.0  12.9  25.4
 //   1 x 14336 x 4096    14.6  10.7   8.6  10.3  16.9  27.2        1000 x 14336 x 4096   621   223  93.6  87.0  41.4  31.6
 struct Mx4Plan {
-    enum Kind { kRows11, kRows12, kRows22, kRows42, kStrip4, kStrip6, kStrip8, kQuarter, kHalf, kFull, kFullRows, kFullCols, kSplit } kind;
+    enum Kind { kRows11, kRows12, kRows14, kRows22, kRows42, kStrip4, kStrip6, kStrip8, kQuarter, kHalf, kFull, kFullRows, kFullCols, kSplit } kind;
     int ranges, whole;  // kSplit: ranges of the contraction; kFullRows, kFullCols: tiles in whole rounds, launched on their own
 };
 
+// Up to kMxTokens rows have their kernel by the columns alone, so that a product from bf16 has the bits of that from codes.
 static Mx4Plan plan_product(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int cus)
 {
+    if (M <= kMxTokens && K > 0) return {N <= 16 * cus ? Mx4Plan::kRows11 : N <= 32 * cus ? Mx4Plan::kRows12 : Mx4Plan::kRows14, 1, 0};
     const auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const auto rounds = [&](int64_t t) { return (double)((t + cus - 1) / cus); };
     const double G = (double)((K + kMxGroup - 1) / kMxGroup);
@@ -678,6 +734,17 @@ size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K)
     return plan.kind == Mx4Plan::kSplit ? (size_t)plan.ranges * (size_t)M * (size_t)N * sizeof(float) : 0;
 }
 
+f8_status mx4_gemm_tokens(const Mx4Args& a, const uint16_t* X, hipStream_t st)
+{
+    if (a.M == 0 || a.N == 0) return last_launch_status();
+    switch (plan_product(a.M, a.N, a.K, 0, cu_count()).kind) {
+        case Mx4Plan::kRows11: launch_rows<1, 1, 12, true>(a, st, X); break;
+        case Mx4Plan::kRows14: launch_rows<1, 4, 3, true>(a, st, X); break;
+        default: launch_rows<1, 2, 6, true>(a, st, X); break;
+    }
+    return last_launch_status();
+}
+
 f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st)
 {
     if (a.M == 0 || a.N == 0) return last_launch_status();
@@ -687,6 +754,7 @@ f8_status mx4_gemm(const Mx4Args& a, void* ws, size_t ws_bytes, hipStream_t st)
     switch (plan.kind) {
         case Mx4Plan::kRows11: launch_rows<1, 1, 8>(a, st); break;
         case Mx4Plan::kRows12: launch_rows<1, 2, 5>(a, st); break;
+        case Mx4Plan::kRows14: launch_rows<1, 4, 3>(a, st); break;
         case Mx4Plan::kRows22: launch_rows<2, 2, 4>(a, st); break;
         case Mx4Plan::kRows42: launch_rows<4, 2, 2>(a, st); break;
         case Mx4Plan::kStrip4: launch_strip<4, 4>(a, st); break;

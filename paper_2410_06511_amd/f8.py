@@ -17,6 +17,7 @@ DYNAMIC, DELAYED, STATIC = 0, 1, 2
 MAX_HISTORY = 1024
 BF16, F32 = 0, 1
 NORM_2, NORM_MAX = 0, 1
+MX4_TOKENS, MX4_TOKEN_K = 4, 16384
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libf8.so")
@@ -792,7 +793,7 @@ def mx4_workspace_bytes(M, K, N):
 
 class MX4Tensor:
     """Device buffers of the codes of T[rows, cols] (see f8_mx4): q, s with blocks along the columns, q_t, s_t along the rows;
-    sides: "q", "t" or "qt" for either or both."""
+    sides: "q", "t" or "qt" for either or both, "" for none."""
 
     def __init__(self, rows, cols, sides="q", device="cuda"):
         u8 = dict(dtype=torch.uint8, device=device)
@@ -800,7 +801,7 @@ class MX4Tensor:
         codes = lambda r, c: (torch.empty((r, 16 * ((c + 31) // 32)), **u8), torch.empty(mx4_scale_bytes(r, c), **u8))
         self.q, self.s = codes(rows, cols) if "q" in sides else (None, None)
         self.q_t, self.s_t = codes(cols, rows) if "t" in sides else (None, None)
-        self.device = (self.q if self.q is not None else self.q_t).get_device()   # (-1: not on a GPU)
+        self.device = torch.empty(0, **u8).get_device()   # (-1: not on a GPU)
         self._struct = MX4Struct(_ptr(self.q), _ptr(self.s), _ptr(self.q_t), _ptr(self.s_t))
 
     def struct(self):
@@ -808,13 +809,14 @@ class MX4Tensor:
 
 
 class MX4Saved:
-    """f8_mx4_saved for one linear: X [M, K], W [N, K], dY [M, N].  backward=False: what a forward needs, nothing for a backward."""
+    """f8_mx4_saved for one linear: X [M, K], W [N, K], dY [M, N].  backward=False: what a forward needs, nothing for a backward
+    (of up to MX4_TOKENS rows of up to MX4_TOKEN_K not even the codes of X)."""
 
     def __init__(self, M, K, N, backward=True, device="cuda", x=None):
         """x: the MX4Tensor of another linear that reads the same input."""
         self.M, self.K, self.N = M, K, N
         sides = "qt" if backward else "q"
-        self.x = x if x is not None else MX4Tensor(M, K, sides, device)
+        self.x = x if x is not None else MX4Tensor(M, K, sides if backward or M > MX4_TOKENS or K > MX4_TOKEN_K else "", device)
         self.w = MX4Tensor(N, K, sides, device)
         self.dy = MX4Tensor(M, N, sides, device) if backward else None
         self.device = self.w.device

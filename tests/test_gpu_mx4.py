@@ -180,6 +180,27 @@ def test_linear(M, K, N):
     assert torch.equal(Y, Y2)
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 16, 16), (1, 4096, 4096), (2, 528, 8192), (3, 4112, 272), (4, 14336, 528), (4, 1040, 8208), (1, 16384, 80), (2, 48, 16), (4, 16400, 48), (1, 768, 28672)])
+def test_tokens_without_codes_of_their_own(M, K, N):
+    """Up to four rows are quantised inside the product: the bits of the separate quantisation and product."""
+    X, W = gen((M, K), 5).cuda(), gen((N, K), 6, 0.02).cuda()
+    if M > 1:
+        X[1] = 0.0
+    codes, none = f8.MX4Saved(M, K, N, backward=False, x=f8.MX4Tensor(M, K)), f8.MX4Saved(M, K, N, backward=False)
+    assert (none.x.q is None) == (K <= f8.MX4_TOKEN_K)
+    Y, Z = (torch.full((M, N), 7.0, dtype=BF16, device="cuda") for _ in range(2))
+    f8.mx4_linear_fwd(X, W, Y, codes)
+    f8.mx4_linear_fwd(X, W, Z, none)
+    assert torch.equal(Y, Z)
+    Z.fill_(7.0)
+    f8.mx4_linear_fwd(X, None, Z, none)
+    assert torch.equal(Y, Z)
+    check_product(Y, mo.rounded(wide(X)), mo.rounded(wide(W)), "tokens")
+    X[0, K // 2] = float("inf")
+    f8.mx4_linear_fwd(X, None, Z, none)
+    assert bool(Z[0].isnan().all()) and torch.equal(Y[1:], Z[1:])
+
+
 def test_gradients_by_differences():
     """On values that the format holds the linear is exact, and so are differences of its loss."""
     r = np.random.default_rng(0)

@@ -155,6 +155,9 @@ def test_mx4_linear():
         assert fwd(d) == SHAPE
     assert fwd(X=None) == NULL and fwd(Y=None) == NULL and fwd(x=MX4(q=None, s=None)) == NULL and fwd(w=MX4(s=None)) == NULL and fwd(w=MX4(q_t=None)) == NULL
     assert fwd(X=FAKE + 2) == ALIGN and fwd(W=FAKE + 8) == ALIGN and fwd(Y=FAKE + 8) == ALIGN and fwd(ws=FAKE + 4) == ALIGN and fwd(x=MX4(q=FAKE + 4)) == ALIGN
+    none = dict(q=None, s=None, q_t=None, s_t=None)   # codes of X that are not wanted: of few and short rows only
+    assert fwd(x=MX4(**none)) == NULL and fwd((4, 16400, 32), x=MX4(**none)) == NULL and fwd((4, 64, 32), x=MX4(**{**none, "q_t": FAKE, "s_t": FAKE})) == NULL
+    assert fwd((4, 64, 32), X=None, x=MX4(**none)) == NULL and fwd((4, 64, 32), X=FAKE + 2, x=MX4(**none)) == ALIGN
     def bwd(d=(5, 64, 32), dY=FAKE, dX=FAKE, dW=FAKE, x=MX4(), w=MX4(), dy=MX4()):
         sv = f8.MX4SavedStruct(x, w, dy)
         return l.f8_mx4_linear_bwd(C.byref(f8.MX4Desc(*d)), dY, C.byref(sv), dX, dW, None, 0, None)
