@@ -3,38 +3,47 @@
 // Bound by memory: the norm reads every element once, the scaling reads and writes it.  Squares and sums are taken in fp64: the
 // square of a bf16 or fp32 value is exact there and cannot overflow or vanish (fp32 loses gradients below 1e-19 and above 1e19),
 // at a quarter of the rate that the memory leaves room for.
-// The tensors' addresses and sizes come as kernel arguments, kTensors to a launch; a block walks over steps of kStep elements of
-// all of a launch's tensors and finds each step's tensor by bisection in scalar registers.  Partial sums are added in a fixed order.
+// The tensors' addresses and sizes come as kernel arguments, kTensors to a launch; a block has a range of the steps of kStep
+// elements of all of a launch's tensors.  Partial sums are added in a fixed order.
 #include "f8_device.hpp"
 #include "f8_host.hpp"
 
 namespace f8 {
 
-constexpr int kTensors = 96;          // of a launch: 3 KB of arguments at most
+constexpr int kTensors = 128, kFewTensors = 16;  // of a launch: 3.6 KB of arguments, or half a KB
 constexpr int kGradThreads = 256;
 constexpr int kGradUnroll = 4;
 constexpr int kStep = kGradThreads * 8 * kGradUnroll;  // elements
-constexpr int kGradBlocks = 2048;     // of the norm: one partial sum each
+constexpr int kGradBlocks = 2048;  // of the norm: one partial sum each
+constexpr uint32_t kClipBlocks = 16384;
 
+template <int CAP>
 struct TensorList {
-    const void* in[kTensors];
-    void* out[kTensors];
-    int64_t n[kTensors];           // elements
-    uint32_t first[kTensors + 1];  // the tensors' first steps; the number of steps
-    uint32_t f32[kTensors / 32];   // bit i: tensor i holds fp32
+    const void* in[CAP];
+    void* out[CAP];
+    int64_t n[CAP];                     // elements
+    uint32_t first[CAP + 1];            // the tensors' first steps; the number of steps
+    uint32_t f32[(CAP + 31) / 32];      // bit i: tensor i holds fp32
     int count;
 };
 
-// The tensor of a step: the last whose first step is not behind it (scalar: `step` is the same in all lanes).
-__device__ inline int tensor_of(const TensorList& l, uint32_t step)
+// f(tensor, first element) for every gridDim-th of the steps: the first one's tensor by bisection (the last whose first step is not
+// behind it), then the next ones; all of it in scalar registers.  (Neighbouring steps for a block read slower: the scaling of one
+// 8B block's gradients 151 -> 172 us.  From the last step on, which the norm has read latest, nothing is gained: 153.)
+template <int CAP, class F>
+__device__ inline void each_step(const TensorList<CAP>& l, F&& f)
 {
-    int lo = 0, hi = l.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (l.first[mid] <= step) lo = mid;
+    const uint32_t steps = l.first[l.count];
+    int t = 0, hi = l.count;
+    while (hi - t > 1) {
+        const int mid = (t + hi) / 2;
+        if (l.first[mid] <= blockIdx.x) t = mid;
         else hi = mid;
     }
-    return lo;
+    for (uint32_t step = blockIdx.x; step < steps; step += gridDim.x) {
+        while (step >= l.first[t + 1]) ++t;
+        f(t, (int64_t)(step - l.first[t]) * kStep);
+    }
 }
 
 // Tensors lie on any element: loads and stores of eight are those of the element's alignment (the memory takes them, two lines
@@ -129,18 +138,15 @@ __device__ inline void norm_step(const void* in, int64_t n, int64_t at, Norm<MAX
     }
 }
 
-template <bool MAX>
-__global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const TensorList l, double* __restrict__ part)
+template <bool MAX, int CAP>
+__global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const TensorList<CAP> l, double* __restrict__ part)
 {
     __shared__ double red[kGradThreads / kWave];
     Norm<MAX> norm;
-    const uint32_t steps = l.first[l.count];
-    for (uint32_t step = blockIdx.x; step < steps; step += gridDim.x) {
-        const int t = tensor_of(l, step);
-        const int64_t at = (int64_t)(step - l.first[t]) * kStep;
+    each_step(l, [&](int t, int64_t at) {
         if (l.f32[t / 32] >> (t % 32) & 1) norm_step<MAX, true>(l.in[t], l.n[t], at, norm);
         else norm_step<MAX, false>(l.in[t], l.n[t], at, norm);
-    }
+    });
     const double v = block_join<MAX>(norm.value(), red);
     if (threadIdx.x == 0) part[blockIdx.x] = v;
 }
@@ -206,18 +212,16 @@ __device__ inline void clip_step(const void* in, void* out, int64_t n, int64_t a
     }
 }
 
-__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(const TensorList l, const float* __restrict__ norm, float most)
+template <int CAP>
+__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(const TensorList<CAP> l, const float* __restrict__ norm, float most)
 {
     float factor = most / (norm[0] + 1e-6f);
     factor = factor > 1.0f ? 1.0f : factor;  // (a NaN stays one)
-    const uint32_t steps = l.first[l.count];
-    for (uint32_t step = blockIdx.x; step < steps; step += gridDim.x) {
-        const int t = tensor_of(l, step);
-        if (factor == 1.0f && l.in[t] == l.out[t]) continue;
-        const int64_t at = (int64_t)(step - l.first[t]) * kStep;
+    each_step(l, [&](int t, int64_t at) {
+        if (factor == 1.0f && l.in[t] == l.out[t]) return;
         if (l.f32[t / 32] >> (t % 32) & 1) clip_step<true>(l.in[t], l.out[t], l.n[t], at, factor);
         else clip_step<false>(l.in[t], l.out[t], l.n[t], at, factor);
-    }
+    });
 }
 
 // ---- host ----------------------------------------------------------------------------------------
@@ -237,11 +241,11 @@ static f8_status check_list(const f8_tensor* list, int64_t count)
     return F8_OK;
 }
 
-// The list in launches of at most kTensors tensors and 2^31 steps: f(TensorList, steps).
-template <class F>
+// The list in launches of at most CAP tensors and 2^31 steps: f(TensorList, steps).
+template <int CAP, class F>
 static void for_launches(const f8_tensor* in, const f8_tensor* out, int64_t count, F&& f)
 {
-    TensorList l;
+    TensorList<CAP> l;
     const auto clear = [&] {
         l.count = 0, l.first[0] = 0;
         for (auto& w : l.f32) w = 0;
@@ -250,7 +254,7 @@ static void for_launches(const f8_tensor* in, const f8_tensor* out, int64_t coun
     for (int64_t i = 0; i < count; ++i) {
         if (in[i].n == 0) continue;
         const uint32_t steps = (uint32_t)((in[i].n + kStep - 1) / kStep);
-        if (l.count == kTensors || (uint64_t)l.first[l.count] + steps > 0x7FFFFFFFu) f(l), clear();
+        if (l.count == CAP || (uint64_t)l.first[l.count] + steps > 0x7FFFFFFFu) f(l), clear();
         l.in[l.count] = in[i].data, l.out[l.count] = out ? out[i].data : nullptr, l.n[l.count] = in[i].n;
         if (in[i].type == F8_F32) l.f32[l.count / 32] |= 1u << (l.count % 32);
         l.first[l.count + 1] = l.first[l.count] + steps;
@@ -300,11 +304,13 @@ f8_status f8_grad_norm(const f8_tensor* list, int64_t count, f8_norm kind, float
     double* const part = (double*)workspace;
     int64_t parts = 0;
     const bool max = kind == F8_NORM_MAX;
-    for_launches(list, nullptr, count, [&](const TensorList& l) {
+    const auto launch = [&]<int CAP>(const TensorList<CAP>& l) {
         const unsigned b = grad_blocks(l.first[l.count]);
-        (max ? grad_norm_kernel<true> : grad_norm_kernel<false>)<<<b, kGradThreads, 0, st>>>(l, part + parts);
+        (max ? grad_norm_kernel<true, CAP> : grad_norm_kernel<false, CAP>)<<<b, kGradThreads, 0, st>>>(l, part + parts);
         parts += b;
-    });
+    };
+    if (count <= kFewTensors) for_launches<kFewTensors>(list, nullptr, count, launch);  // (less for the host to copy)
+    else for_launches<kTensors>(list, nullptr, count, launch);
     (max ? grad_norm_final_kernel<true> : grad_norm_final_kernel<false>)<<<1, 1024, 0, st>>>(part, parts, norm, sum);
     return last_launch_status();
 }
@@ -322,10 +328,12 @@ f8_status f8_grad_clip(const f8_tensor* in, const f8_tensor* out, int64_t count,
         const int64_t bytes = in[i].n * (in[i].type == F8_F32 ? 4 : 2);
         if (in[i].n != out[i].n || (in[i].data != out[i].data && bytes && !apart({in[i].data, bytes}, {out[i].data, bytes}))) return F8_ERR_SHAPE;
     }
-    for_launches(in, out, count, [&](const TensorList& l) {
-        const uint32_t steps = l.first[l.count], most_blocks = 8 * kGradBlocks;
-        grad_clip_kernel<<<steps < most_blocks ? steps : most_blocks, kGradThreads, 0, (hipStream_t)stream>>>(l, norm, most);
-    });
+    const auto launch = [&]<int CAP>(const TensorList<CAP>& l) {
+        const uint32_t steps = l.first[l.count], blocks = kClipBlocks;
+        grad_clip_kernel<CAP><<<steps < blocks ? steps : blocks, kGradThreads, 0, (hipStream_t)stream>>>(l, norm, most);
+    };
+    if (count <= kFewTensors) for_launches<kFewTensors>(in, out, count, launch);
+    else for_launches<kTensors>(in, out, count, launch);
     return last_launch_status();
 }
 
