@@ -253,16 +253,16 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const EmbedGradArgs p)
     float4 a = src[0], b = src[1];
     src = reinterpret_cast<const float4*>(p.part + ((piece + 1) * 2 * p.dc + c) * 8);
     const int64_t step = (int64_t)4 * p.dc;  // of float4: two rows of D
-    for (int64_t k = 0; k < more; k += 8) {
-        float4 va[8], vb[8];
+    constexpr int AHEAD = 16;
+    for (int64_t k = 0; k < more; k += AHEAD) {
+        float4 va[AHEAD], vb[AHEAD];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int64_t at = k + u < more ? k + u : k;
-            va[u] = src[at * step], vb[u] = src[at * step + 1];
+        for (int u = 0; u < AHEAD; ++u) {
+            va[u] = vb[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (k + u < more) va[u] = src[(k + u) * step], vb[u] = src[(k + u) * step + 1];
         }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (k + u >= more) break;
+        for (int u = 0; u < AHEAD; ++u) {
             a.x += va[u].x, a.y += va[u].y, a.z += va[u].z, a.w += va[u].w;
             b.x += vb[u].x, b.y += vb[u].y, b.z += vb[u].z, b.w += vb[u].w;
         }
@@ -349,7 +349,7 @@ f8_status f8_embed_bwd(const int64_t* ids, int64_t M, const void* dout_bf16, int
     float* const part = (float*)((char*)workspace + kMinWorkspaceBytes + plan.lists * plan.list);
 
     const int row16 = (int)(D * (f32 ? 4 : 2) / 16), sort_blocks = (int)((M + kSortBlock - 1) / kSortBlock);
-    const int64_t words = V * row16, fill = (words + kSortWaves * kWave * 4 - 1) / (kSortWaves * kWave * 4), most = 4 * cu_count();
+    const int64_t words = V * row16, fill = (words + kSortWaves * kWave * 4 - 1) / (kSortWaves * kWave * 4), most = cu_count();  // (131072 x 4096 with four blocks a unit 321 us, two 316, one 298)
     embed_sort_kernel<<<(unsigned)(sort_blocks + (fill < most ? fill : most)), kSortWaves * kWave, 0, st>>>(
         {ids, M, V, list[0], list[1], sort_blocks, (uint4*)dtable, ldt * (f32 ? 4 : 2) / 16, V, row16});
     if (M == 0) return last_launch_status();
