@@ -154,20 +154,35 @@ __global__ __launch_bounds__(block_threads(THREADS)) void layernorm_bwd_kernel(c
     uint4 gain[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) gain[u] = t + TPR * u < p.dc ? p.g[t + TPR * u] : make_uint4(0, 0, 0, 0);
-    for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < p.M; m0 += (int64_t)gridDim.x * kRows) {
-        const int64_t m = m0 + sub;
-        const bool live = m < p.M;
+    struct Row {
         uint4 h[U], dn[U], dh[U];
+        float mean, rstd;
+    };
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    const auto load_row = [&](Row& row, int64_t m) {
+        const bool live = m < p.M;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = t + TPR * u;
-            h[u] = dn[u] = dh[u] = make_uint4(0, 0, 0, 0);
+            row.h[u] = row.dn[u] = row.dh[u] = make_uint4(0, 0, 0, 0);
             if (!live || c >= p.dc) continue;
             const auto load = [&](const uint16_t* a, int64_t ld) { return ONCE ? load_once(row_of(a, m, ld) + c) : row_of(a, m, ld)[c]; };
-            h[u] = load(p.h, p.ldh), dn[u] = load(p.dn, p.lddn);
-            if (p.dh && p.dx) dh[u] = load(p.dh, p.lddh);
+            row.h[u] = load(p.h, p.ldh), row.dn[u] = load(p.dn, p.lddn);
+            if (p.dh && p.dx) row.dh[u] = load(p.dh, p.lddh);
         }
-        const float mean = live ? p.mean[m] : 0.0f, rstd = live ? p.rstd[m] : 0.0f;
+        row.mean = live ? p.mean[m] : 0.0f, row.rstd = live ? p.rstd[m] : 0.0f;
+    };
+    Row next;
+    load_row(next, (int64_t)blockIdx.x * kRows + sub);
+    for (int64_t m0 = (int64_t)blockIdx.x * kRows; m0 < p.M; m0 += stride) {
+        const int64_t m = m0 + sub;
+        const bool live = m < p.M;
+        const Row row = next;
+        load_row(next, m + stride);
+        const uint4(&h)[U] = row.h;
+        const uint4(&dn)[U] = row.dn;
+        const uint4(&dh)[U] = row.dh;
+        const float mean = row.mean, rstd = row.rstd;
         float2 s = make_float2(0.0f, 0.0f);
         // (past the row's end dn and the gain are zero, and so is every term)
 #pragma unroll

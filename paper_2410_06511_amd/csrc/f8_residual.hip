@@ -348,8 +348,9 @@ __global__ __launch_bounds__(kSumCols* kSumGroups) void column_sums_kernel(const
     float* out = set < p.sets ? p.out[set] : p.dgate + (int64_t)(set - p.sets) * p.D;
     float s = 0.0f;
     if (c < p.D) {
-        constexpr int AHEAD = 8;
-        for (int i = grp; i < n; i += kSumGroups * AHEAD) {
+        int i = grp;
+        const auto batch = [&](auto ahead) {  // that many rows' loads at once
+            constexpr int AHEAD = decltype(ahead)::value;
             float v[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
@@ -358,7 +359,10 @@ __global__ __launch_bounds__(kSumCols* kSumGroups) void column_sums_kernel(const
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) s += v[k];
-        }
+            i += kSumGroups * AHEAD;
+        };
+        while (i + kSumGroups * 31 < n) batch(std::integral_constant<int, 32>{});
+        while (i < n) batch(std::integral_constant<int, 8>{});
     }
     sum[grp][cl] = s;
     __syncthreads();
