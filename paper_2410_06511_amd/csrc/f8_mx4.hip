@@ -92,6 +92,30 @@ __global__ __launch_bounds__(256) void mx4_cast_kernel(const Mx4Cast a, const Mx
     else mx4_cast_tile(b, (int)blockIdx.x - a.blocks, tile);
 }
 
+// One orientation alone, along the rows: a wave has a group of 512 elements of ROWS rows, and writes whole pieces of codes and scales.
+template <int ROWS>
+__global__ __launch_bounds__(256) void mx4_cast_rows_kernel(const Mx4Cast p, int groups)
+{
+    const int64_t w = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave, srows = mx4_rows(p.rows);
+    const int64_t row0 = w / groups * ROWS;
+    if (row0 >= srows) return;
+    const int g = (int)(w % groups), lane = threadIdx.x % kWave, col = g * kMxGroup + 8 * lane, b = lane / 4;
+    const int64_t pitch = mx4_pitch(p.cols);
+    uint4 v[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (row0 + i < p.rows && col < p.cols) v[i] = *reinterpret_cast<const uint4*>(p.x + (row0 + i) * p.ld + col);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const uint32_t code = mx4_scale_of_quad(v[i]);
+        const bool real = row0 + i < p.rows && col / kMxBlock * kMxBlock < p.cols;
+        if (real) *reinterpret_cast<uint32_t*>(p.q + (row0 + i) * pitch + col / 2) = mx4_encode8(v[i], code);
+        if (lane % 4 == 0) p.s[((int64_t)g * srows + row0 + i) * 16 + 4 * (b % 4) + b / 4] = (uint8_t)(real ? code : 127);
+    }
+}
+
 __global__ __launch_bounds__(256) void mx4_decode_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, int rows, int cols, uint16_t* out, int64_t ldo)
 {
     const int blocks = (cols + kMxBlock - 1) / kMxBlock;
@@ -115,8 +139,17 @@ static Mx4Cast cast_of(const void* x, int64_t rows, int64_t cols, int64_t ld, co
     return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)squares, (int)across, (int)((squares + 7) / 8 * 128)};
 }
 static bool too_many(int64_t rows, int64_t cols) { return (rows / kMxGroup + 1) * (cols / kMxGroup + 1) > 0x2FFFFFF; }
+constexpr int64_t kFewWaves = 16384;
 static void launch_cast(const Mx4Cast& a, const Mx4Cast& b, hipStream_t st)
 {
+    if (a.blocks > 0 && b.blocks == 0 && !a.q_t) {
+        // (a row for each wave while there are few)
+        const int groups = (a.cols + kMxGroup - 1) / kMxGroup;
+        const int64_t all = mx4_rows(a.rows) * groups;
+        if (all <= kFewWaves) mx4_cast_rows_kernel<1><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a, groups);
+        else mx4_cast_rows_kernel<4><<<(unsigned)((all / 4 + 3) / 4), 256, 0, st>>>(a, groups);
+        return;
+    }
     if (a.blocks + b.blocks > 0) mx4_cast_kernel<<<(unsigned)(a.blocks + b.blocks), 256, 0, st>>>(a, b);
 }
 
