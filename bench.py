@@ -52,6 +52,9 @@ def parse():
     ap.add_argument("--vocab", type=int, default=0,
                     help="llama8b_layer: an output head (final norm, Float8 projection to so many tokens, their log probabilities) follows the block, "
                          "forward and backward, and the block's gradient comes from it")
+    ap.add_argument("--norm", default="rms", choices=["rms", "layer"], help="llama8b_layer: the norms in front of the linears (and of the output head)")
+    ap.add_argument("--embed", action="store_true", help="llama8b_layer with --vocab: token embeddings in front of the block, forward and backward")
+    ap.add_argument("--clip", type=float, default=0.0, help="llama8b_layer: the norm of all gradients after the backward, and their scaling to at most this one")
     ap.add_argument("--post-norm", action="store_true", help="llama8b_layer: both branches are normalised before they join the residual stream")
     ap.add_argument("--keep-weights", action="store_true",
                     help="dynamic scaling: quantise the weights once before the timed steps and keep their codes "
@@ -844,6 +847,9 @@ def layer_main(args, w):
     if args.scaling == "static":
         print("bench.py: the transformer block runs with dynamic or delayed scaling", file=sys.stderr)
         sys.exit(2)
+    if (args.embed and not args.vocab) or (args.norm == "layer" and args.post_norm) or not 0 <= args.clip < float("inf"):
+        print("bench.py: token embeddings need --vocab, layer norms plain branches, and clipping a norm that is not negative", file=sys.stderr)
+        sys.exit(2)
     sh = wl.LAYER_SHAPE[w.key]
     B, S, Hq, Hkv, hd, D, H = (sh[k] for k in ("B", "S", "Hq", "Hkv", "hd", "D", "H"))
     M = B * S
@@ -860,23 +866,38 @@ def layer_main(args, w):
                "W2": wl.randn_bf16((D, H), 0.02, 0, generator=g).cuda()}
     if args.post_norm:
         weights.update(p1=torch.ones(D, dtype=torch.bfloat16, device="cuda"), p2=torch.ones(D, dtype=torch.bfloat16, device="cuda"))
-    blk = TransformerBlock(B, S, D, H, Hq, Hkv, hd, scaling=args.scaling, post_norm=args.post_norm)
+    blk = TransformerBlock(B, S, D, H, Hq, Hkv, hd, scaling=args.scaling, post_norm=args.post_norm, norm=args.norm)
     stream = torch.cuda.current_stream()
     head = None
     if args.vocab:
         from paper_2410_06511_amd.head import OutputHead
-        head = OutputHead(M, D, args.vocab, scaling=args.scaling)
+        head = OutputHead(M, D, args.vocab, scaling=args.scaling, norm=args.norm)
         dout = head.dx
         weights_head = {"g": torch.ones(D, dtype=torch.bfloat16, device="cuda"), "Wout": wl.randn_bf16((head.width, D), 0.02, 0, generator=g).cuda()}
         tokens = torch.randint(0, args.vocab, (M,), generator=g).cuda()
         d_logp = torch.full((M,), -1.0 / M, device="cuda")
+    embedding = clipper = None
+    if args.embed:
+        from paper_2410_06511_amd.embedding import TokenEmbedding
+        embedding = TokenEmbedding(M, D, args.vocab)
+        ids, weights_embedding = tokens.roll(1), {"Wemb": wl.randn_bf16((args.vocab, D), 1.0, 0, generator=g).cuda()}
+        x = embedding.out
+    if args.clip:
+        from paper_2410_06511_amd.embedding import GradientClipper
+        clipper = GradientClipper([p for p in (embedding, blk, head) if p], args.clip)
 
     def step():
+        if embedding:
+            embedding.forward(ids, weights_embedding, stream)
         blk.forward(x, weights, stream)
         if head:
             head.forward(blk.out, weights_head, tokens, stream=stream)
             head.backward(blk.out, weights_head, tokens, d_logp, stream=stream)
         blk.backward(x, weights, dout, stream, recompute={"full": True, "selective": "selective", None: False}[args.recompute])
+        if embedding:
+            embedding.backward(ids, blk.dx, stream)
+        if clipper:
+            clipper.clip(stream)
 
     for _ in range(args.warmup):
         step()
@@ -889,10 +910,12 @@ def layer_main(args, w):
     flops_step = sum(l.flops for l in w.linears) + (6 * M * D * head.width if head else 0)
     tflops = flops_step / (ms_per_step * 1e-3) / 1e12
 
-    calls = blk.forward_stages(x, weights, stream, joined=True)  # those of step()
+    calls = embedding.forward_stages(ids, weights_embedding, stream) if embedding else []  # those of step()
+    calls += blk.forward_stages(x, weights, stream, joined=True)
     if head:
         calls += head.forward_stages(blk.out, weights_head, tokens, stream=stream) + head.backward_stages(blk.out, weights_head, tokens, d_logp, stream=stream)
     calls += blk.backward_stages(x, weights, dout, stream, joined=True)
+    calls += (embedding.backward_stages(ids, blk.dx, stream) if embedding else []) + (clipper.stages(stream) if clipper else [])
     reps = max(3, min(args.steps, 10))
     evs = [[(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in calls] for _ in range(reps)]
     for r in range(reps):
@@ -951,7 +974,10 @@ def layer_main(args, w):
                                f"{Hq} query / {Hkv} key-value heads of {hd}: rmsnorm -> wq|wk|wv -> rope -> causal attention -> wo -> "
                                "+x -> rmsnorm -> w1|w3 -> silu(a)*b -> w2 -> +h, and the backward of every stage"
                                + (", both branches normalised" if args.post_norm else "")
-                               + (f"; then final norm, Float8 projection to {args.vocab} tokens and their log probabilities, and back" if head else ""),
+                               + (", layer norms in the place of the rmsnorms" if args.norm == "layer" else "")
+                               + (f"; token embeddings of {args.vocab} in front" if embedding else "")
+                               + (f"; then final norm, Float8 projection to {args.vocab} tokens and their log probabilities, and back" if head else "")
+                               + (f"; the norm of all gradients, scaled to at most {args.clip}" if clipper else ""),
                    "scaling_granularity": "tensorwise", "scaling_strategy": args.scaling, "grad_format": "e4m3",
                    "chained": True, "recompute_in_backward": args.recompute or "none", "flops_per_step": flops_step,
                    "attention_flops_per_step_not_counted": att_flops},

@@ -766,7 +766,7 @@ f8_status f8_distill_bwd(const void* logits_bf16, int64_t ld, int64_t M, int64_t
  * f8_grad_clip: out = in * min(1, most / (norm[0] + 1e-6)), one fp32 product
  *   rounded to the tensor's type; with a factor of 1 the same bits.  out: a list of
  *   the same sizes and types (tensor i the same memory as in's or apart from it, and
- *   no other overlaps), or NULL: in place.  A NaN norm makes everything NaN;
+ *   no other overlaps, within a list neither), or NULL: in place.  A NaN norm makes everything NaN;
  *   most >= 0.
  */
 typedef struct f8_tensor {

@@ -16,6 +16,9 @@ dAB are never written).
 post_norm, gate_rows and branch_scale give blocks whose branches are normalised, gated and scaled before they join the residual
 stream:
     h1 = x + branch_scale * a1 * rmsnorm(wo ..., p1),   out = h1 + branch_scale * a2 * rmsnorm(w2 ..., p2)
+
+norm="layer" puts layer norms in the place of the two rmsnorms in front of the linears, the second with the first residual sum in
+one call; norm_bias gives them biases.
 """
 import math
 from functools import cached_property
@@ -32,10 +35,11 @@ def _bf16(t):
 
 class TransformerBlock:
     def __init__(self, B, S, D, H, Hq, Hkv, hd=128, eps=1e-5, theta=500000.0, grad_format=f8.E4M3, device="cuda",
-                 scaling="dynamic", history_len=16, post_norm=False, gate_rows=0, branch_scale=1.0):
+                 scaling="dynamic", history_len=16, post_norm=False, gate_rows=0, branch_scale=1.0, norm="rms", norm_bias=False):
         """post_norm: the weights have p1, p2 [D], the gains of the norms after the two branches.  gate_rows: they have a1, a2
         [gate_rows, D] (1: a gate per channel, B: one per sequence; a divisor of B * S).  Gradients: dp1, dp2, da1, da2.  With any
-        of the three D is at most 16384."""
+        of the three D is at most 16384.  norm: "rms" or "layer" (D at most 16384, and none of the three); norm_bias: the weights have
+        b1, b2 [D], the layer norms' biases, with gradients db1, db2."""
         assert D == Hq * hd and scaling in ("dynamic", "delayed")
         self.post_norm, self.gate_rows, self.branch_scale = post_norm, gate_rows, branch_scale
         self.shaped = bool(post_norm or gate_rows or branch_scale != 1.0)  # a branch that is more than its last product
@@ -43,6 +47,10 @@ class TransformerBlock:
             assert D <= 16384, f"a branch with a norm, a gate or a scale holds rows of up to 16384 elements, not {D}"
             assert gate_rows >= 0 and (not gate_rows or B * S % gate_rows == 0), f"{gate_rows} rows of a gate do not divide {B * S} tokens"
             assert math.isfinite(branch_scale), f"a branch's scale of {branch_scale}"
+        assert norm in ("rms", "layer"), f"a norm {norm!r}"
+        assert norm == "layer" or not norm_bias, "a bias belongs to a layer norm"
+        assert norm == "rms" or (D <= 16384 and not self.shaped), "a block of layer norms has rows of up to 16384 elements and plain branches"
+        self.layer, self.norm_bias = norm == "layer", norm_bias
         self.delayed, self.gfmt = scaling == "delayed", grad_format
         if self.delayed:
             self.st_qkv, self.st_o, self.st_13, self.st_2 = (f8.ScalingState(f8.DELAYED, history_len, device) for _ in range(4))
@@ -82,6 +90,10 @@ class TransformerBlock:
         self.a_bwd = torch.zeros(2, **f32)   # amax of dh1 and of dqkv, raised by the calls that write them
         self.dxn, self.dx = E(M, D), E(M, D)
         self.dg1, self.dg2 = torch.empty(D, **f32), torch.empty(D, **f32)
+        if self.layer:
+            self.mean1, self.mean2 = torch.empty(M, **f32), torch.empty(M, **f32)
+            self.db1, self.db2 = (torch.empty(D, **f32) if norm_bias else None for _ in range(2))
+            self.ln_ws = torch.empty(f8.layernorm_bwd_workspace_bytes(M, D), dtype=torch.uint8, device=device)
         if self.shaped:
             vec = lambda n: torch.empty(n, **f32) if post_norm else None
             self.rstd_p1, self.rstd_p2, self.dp1, self.dp2 = vec(M), vec(M), vec(D), vec(D)
@@ -104,6 +116,12 @@ class TransformerBlock:
     @cached_property
     def datt_t(self):
         return self.datt.new_empty((self.D, self.M))
+
+    def gradients(self):
+        """Of the weights, as a backward leaves them: what a norm over all gradients takes."""
+        names = ["dWqkv", "dWo", "dW13", "dW2", "dg1", "dg2"] + ["db1", "db2"] * (self.layer and self.norm_bias)
+        names += ["dp1", "dp2"] * self.post_norm + ["da1", "da2"] * bool(self.gate_rows)
+        return [getattr(self, n) for n in names]
 
     def _slices(self, t):
         Hq, Hkv, hd = self.Hq, self.Hkv, self.hd
@@ -134,7 +152,18 @@ class TransformerBlock:
         # (f8.residual_norm holds a row in registers)
         fused = self.shaped or (joined and D <= 16384)
 
+        b1, b2 = (_bf16(w["b1"]), _bf16(w["b2"])) if s.norm_bias else (None, None)
+
+        def norm_1(a_xn, ws):
+            if self.layer:
+                return ("layernorm 1", lambda: f8.layernorm(_bf16(x), _bf16(w["g1"]).reshape(D), s.xn, b1, eps=s.eps, mean=s.mean1,
+                                                            rstd=s.rstd1, amax_n=a_xn, workspace=ws, stream=stream), 0, 4 * M * D)
+            return ("rmsnorm 1", lambda: f8.rmsnorm(x, w["g1"], s.eps, s.xn, s.rstd1, a_xn, ws, stream), 0, 4 * M * D)
+
         def norm_2(a_hn, ws):
+            if self.layer:
+                return [("layernorm 2", lambda: f8.layernorm(_bf16(x), _bf16(w["g2"]).reshape(D), s.hn, b2, s.yo, s.h1, s.eps, s.mean2,
+                                                             s.rstd2, a_hn, ws, stream), 0, 8 * M * D)]
             if not fused:
                 return [("residual 1", lambda: f8.add(x, s.yo, s.h1, stream), 0, 6 * M * D),
                         ("rmsnorm 2", lambda: f8.rmsnorm(s.h1, w["g2"], s.eps, s.hn, s.rstd2, a_hn, ws, stream), 0, 4 * M * D)]
@@ -152,7 +181,7 @@ class TransformerBlock:
                 self._replay = tuple(f8.ReplayState(sv) for sv in (s.s_qkv, s.s_o, s.s_13, s.s_2))
             r_qkv, r_o, r_13, r_2 = self._replay
             return [
-                ("rmsnorm 1", lambda: f8.rmsnorm(x, w["g1"], s.eps, s.xn, s.rstd1, None, None, stream), 0, 4 * M * D),
+                norm_1(None, None),
                 ("linear wq|wk|wv fwd", lambda: f8.linear_fwd_scaled(s.d_qkv, r_qkv, s.xn, w["Wqkv"], s.qkv, s.s_qkv, s.ws, stream),
                  2 * M * D * s.Nqkv, 0),
                 *rope,
@@ -167,7 +196,7 @@ class TransformerBlock:
             ]
         if self.delayed:
             return [
-                ("rmsnorm 1", lambda: f8.rmsnorm(x, w["g1"], s.eps, s.xn, s.rstd1, None, None, stream), 0, 4 * M * D),
+                norm_1(None, None),
                 ("linear wq|wk|wv fwd", lambda: f8.linear_fwd_scaled(s.d_qkv, s.st_qkv, s.xn, w["Wqkv"], s.qkv, s.s_qkv, s.ws, stream),
                  2 * M * D * s.Nqkv, 0),
                 *rope,
@@ -183,7 +212,7 @@ class TransformerBlock:
                 residual_2,
             ]
         return [
-            ("rmsnorm 1", lambda: f8.rmsnorm(x, w["g1"], s.eps, s.xn, s.rstd1, s.a_xn, s.ws, stream), 0, 4 * M * D),
+            norm_1(s.a_xn, s.ws),
             ("linear wq|wk|wv fwd", lambda: f8.linear_fwd_chained(s.d_qkv, s.xn, s.a_xn, w["Wqkv"], s.qkv, None, s.s_qkv, s.ws, stream),
              2 * M * D * s.Nqkv, 0),
             *rope,
@@ -272,16 +301,23 @@ class TransformerBlock:
                       lambda: f8.residual_norm_bwd(s.yo, s.dh1, s.dyo, h=s.h1, dh=dout, dn=s.dhn, g_post=p1, gate=a1, g_pre=_bf16(w["g2"]).reshape(D),
                                                    branch_scale=s.branch_scale, rstd_post=r1, rstd_pre=s.rstd2, dg_post=s.dp1, dgate=s.da1, dg_pre=s.dg2,
                                                    amax_dy=a_y[0], workspace=s.res_ws, stream=stream), 0, 12 * M * D)
+        elif self.layer:
+            norm_2 = ("layernorm 2 bwd + residual", lambda: f8.layernorm_bwd(s.h1, _bf16(w["g2"]).reshape(D), s.mean2, s.rstd2, s.dhn, s.dh1, _bf16(dout), s.dg2, s.db2,
+                                                                             a_dh1, s.ln_ws, stream), 0, 8 * M * D)
         else:
             norm_2 = ("rmsnorm 2 bwd + residual", lambda: f8.rmsnorm_bwd_add(s.h1, w["g2"], s.rstd2, s.dhn, dout, s.dh1, s.dg2, s.ws, stream, a_dh1),
                       0, 12 * M * D)
+        if self.layer:
+            norm_1 = ("layernorm 1 bwd + residual", lambda: f8.layernorm_bwd(_bf16(x), _bf16(w["g1"]).reshape(D), s.mean1, s.rstd1, s.dxn, s.dx, s.dh1, s.dg1, s.db1,
+                                                                             None, s.ln_ws, stream), 0, 8 * M * D)
+        else:
+            norm_1 = ("rmsnorm 1 bwd + residual", lambda: f8.rmsnorm_bwd_add(x, w["g1"], s.rstd1, s.dxn, s.dh1, s.dx, s.dg1, s.ws, stream), 0, 12 * M * D)
         return [("zero the amax cells", zero_amax, 0, 0)] + ffn + [
             norm_2,
             ("linear wo bwd", lin_o, 4 * M * D * D, 0),
             *attention,
             ("linear wq|wk|wv bwd", lin_qkv, 4 * M * D * s.Nqkv, 0),
-            ("rmsnorm 1 bwd + residual", lambda: f8.rmsnorm_bwd_add(x, w["g1"], s.rstd1, s.dxn, s.dh1, s.dx, s.dg1, s.ws, stream),
-             0, 12 * M * D),
+            norm_1,
         ]
 
     def forward(self, x, w, stream=None):
@@ -291,7 +327,7 @@ class TransformerBlock:
 
     # what selective recomputation runs again: everything the backward reads that is not the output
     # of a matrix product or of the attention (those are kept, as are the fp8 codes of the linears)
-    SELECTIVE = ("rmsnorm 1", "rope q, k; transpose v", "residual 1", "rmsnorm 2")
+    SELECTIVE = ("rmsnorm 1", "layernorm 1", "rope q, k; transpose v", "residual 1", "rmsnorm 2", "layernorm 2")
 
     def backward(self, x, w, dout, stream=None, recompute=False):
         """recompute (Section 2.2.1, activation checkpointing):

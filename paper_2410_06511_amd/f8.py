@@ -739,7 +739,8 @@ def layernorm_bwd(h, g, mean, rstd, dn, dx=None, dh=None, dg=None, db=None, amax
 
 class GradList:
     """A list of tensors (f8_tensor): contiguous, bf16 or fp32, on one GPU, at any address.  It keeps them alive; a tensor whose
-    memory is replaced (resized, set to other data) needs a new list."""
+    memory is replaced (resized, set to other data) needs a new list.  No two of them share memory: of a parameter that is tied,
+    its one gradient is listed once."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -748,6 +749,11 @@ class GradList:
             if t.dtype not in (_BF16, _F32) or not t.is_cuda or t.get_device() != self.device or not t.is_contiguous():
                 raise F8Error(F8_ERR_SHAPE, f"tensor {i} of a list: a contiguous tensor of bf16 or fp32 on the list's GPU is wanted; got {t.dtype}, "
                                             f"{tuple(t.shape)}, strides {t.stride()} on {t.device}")
+        end = 0
+        for at, size, i in sorted((t.data_ptr(), t.nbytes, i) for i, t in enumerate(self.tensors) if t.numel()):
+            if at < end:
+                raise F8Error(F8_ERR_SHAPE, f"tensor {i} of a list shares memory with another one")
+            end = at + size
         self._struct = (TensorStruct * len(self.tensors))(*[(t.data_ptr(), t.numel(), F32 if t.dtype is _F32 else BF16) for t in self.tensors])
         self._address, self._n = C.addressof(self._struct), len(self.tensors)
 

@@ -12,12 +12,18 @@ takes no part and whose gradients are zero.
 import torch
 
 from . import f8
+from .block import _bf16
 
 
 class OutputHead:
-    def __init__(self, M, D, vocab, eps=1e-5, scale=1.0, grad_format=f8.E4M3, device="cuda", scaling="dynamic", history_len=16):
-        """scale: factor of the logits (an inverse temperature), of every loss.  M: tokens, as D a multiple of 16."""
+    def __init__(self, M, D, vocab, eps=1e-5, scale=1.0, grad_format=f8.E4M3, device="cuda", scaling="dynamic", history_len=16, norm="rms", norm_bias=False):
+        """scale: factor of the logits (an inverse temperature), of every loss.  M: tokens, as D a multiple of 16.  norm: "rms" or
+        "layer" (D at most 16384); norm_bias: the weights have b [D], the layer norm's bias, with the gradient db."""
         assert scaling in ("dynamic", "delayed")
+        assert norm in ("rms", "layer"), f"a norm {norm!r}"
+        assert norm == "layer" or not norm_bias, "a bias belongs to a layer norm"
+        assert norm == "rms" or D <= 16384, f"a layer norm of rows of up to 16384 elements, not {D}"
+        self.layer, self.norm_bias = norm == "layer", norm_bias
         self.M, self.D, self.vocab, self.eps, self.scale = M, D, vocab, eps, scale
         N = self.width = (vocab + 15) // 16 * 16
         bf = dict(dtype=torch.bfloat16, device=device)
@@ -34,17 +40,28 @@ class OutputHead:
         self.a_dl = torch.empty(1, **f32)
         self.dxn, self.dx = torch.empty((M, D), **bf), torch.empty((M, D), **bf)
         self.dg, self.dW = torch.empty(D, **f32), torch.empty((N, D), **bf)
+        if self.layer:
+            self.mean, self.db = torch.empty(M, **f32), torch.empty(D, **f32) if norm_bias else None
+            self.ln_ws = torch.empty(f8.layernorm_bwd_workspace_bytes(M, D), dtype=torch.uint8, device=device)
+
+    def gradients(self):
+        """Of the weights, as a backward leaves them: what a norm over all gradients takes."""
+        return [self.dW, self.dg] + [self.db] * (self.layer and self.norm_bias)
 
     def projection_stages(self, x, w, stream=None):
         """w: dict with g [D] and Wout [width, D] (bf16).  [(name, call, flops, algorithmic bytes)] in execution order, as the block's."""
         s, M, D = self, self.M, self.D
-        if s.state is None:
-            norm = lambda: f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, s.a_xn, s.ws, stream)
+        dynamic = s.state is None
+        if s.layer:
+            norm = lambda: f8.layernorm(_bf16(x), _bf16(w["g"]), s.xn, _bf16(w["b"]) if s.norm_bias else None, eps=s.eps, mean=s.mean, rstd=s.rstd, amax_n=s.a_xn if dynamic else None,
+                                        workspace=s.ws, stream=stream)
+        else:
+            norm = lambda: f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, s.a_xn if dynamic else None, s.ws if dynamic else None, stream)
+        if dynamic:
             linear = lambda: f8.linear_fwd_chained(s.desc, s.xn, s.a_xn, w["Wout"], s.logits, None, s.saved, s.ws, stream)
         else:
-            norm = lambda: f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, None, None, stream)
             linear = lambda: f8.linear_fwd_scaled(s.desc, s.state, s.xn, w["Wout"], s.logits, s.saved, s.ws, stream)
-        return [("final rmsnorm", norm, 0, 4 * M * D), ("linear Wout fwd", linear, 2 * M * D * s.width, 0)]
+        return [("final layernorm" if s.layer else "final rmsnorm", norm, 0, 4 * M * D), ("linear Wout fwd", linear, 2 * M * D * s.width, 0)]
 
     def _backward_stages(self, x, w, loss, stream):
         s, M, D = self, self.M, self.D
@@ -52,8 +69,11 @@ class OutputHead:
             linear = lambda: f8.linear_bwd_chained(s.desc, s.logits, s.a_dl, s.saved, s.dxn, None, s.dW, s.ws, stream)
         else:
             linear = lambda: f8.linear_bwd_scaled(s.desc, s.state, s.logits, s.saved, s.dxn, s.dW, s.ws, stream)
-        return [loss, ("linear Wout bwd", linear, 4 * M * D * s.width, 0),
-                ("final rmsnorm bwd", lambda: f8.rmsnorm_bwd(x, w["g"], s.rstd, s.dxn, s.dx, s.dg, s.ws, stream), 0, 6 * M * D)]
+        if s.layer:
+            norm = ("final layernorm bwd", lambda: f8.layernorm_bwd(_bf16(x), _bf16(w["g"]), s.mean, s.rstd, s.dxn, s.dx, None, s.dg, s.db, None, s.ln_ws, stream), 0, 6 * M * D)
+        else:
+            norm = ("final rmsnorm bwd", lambda: f8.rmsnorm_bwd(x, w["g"], s.rstd, s.dxn, s.dx, s.dg, s.ws, stream), 0, 6 * M * D)
+        return [loss, ("linear Wout bwd", linear, 4 * M * D * s.width, 0), norm]
 
     def forward_stages(self, x, w, targets, entropy=False, stream=None):
         s = self
