@@ -8,7 +8,7 @@
 
 namespace f8 {
 
-constexpr int kLnBlocks = 2048;  // of the forward: one partial maximum each
+constexpr int kLnBlocks = 2048;  // of the forward with a maximum over n: one partial maximum each
 static_assert((size_t)kLnBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial per block fits the minimum workspace");
 constexpr int kLnBwdBlocks = 512;  // of the backward, each of which leaves a partial row of both sums
 constexpr int64_t kLnOnce = (int64_t)1 << 25;  // elements from which the backward loads past the caches
@@ -303,7 +303,10 @@ f8_status f8_layernorm(const void* x_bf16, int64_t ldx, const void* y_bf16, int6
         with_row_shape(D / 8, [&](auto T, auto U, int threads) {
             constexpr int kRows = T() == kWave ? kWaveRows : 1;
             const int64_t b = (M + kRows - 1) / kRows;
-            nb = (int)(b < kLnBlocks ? b : kLnBlocks);
+            // rows in the order of the blocks' start read and write faster than rows at a stride of the grid (16384 x 8192 with a
+            // residual 184 us for 198, 8192 x 4096 40.7 for 43); where each block leaves a maximum, there is room for so many
+            const int64_t most = amax_n ? kLnBlocks : 0x7FFFFFFF / threads;
+            nb = (int)(b < most ? b : most);
             const auto kernel = y_bf16 ? layernorm_kernel<T(), U(), true> : layernorm_kernel<T(), U(), false>;
             kernel<<<nb, threads, 0, st>>>(a);
         });
