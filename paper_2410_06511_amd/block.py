@@ -152,7 +152,7 @@ class TransformerBlock:
         # (f8.residual_norm holds a row in registers)
         fused = self.shaped or (joined and D <= 16384)
 
-        b1, b2 = (_bf16(w["b1"]), _bf16(w["b2"])) if s.norm_bias else (None, None)
+        b1, b2 = (_bf16(w["b1"]).reshape(D), _bf16(w["b2"]).reshape(D)) if s.norm_bias else (None, None)
 
         def norm_1(a_xn, ws):
             if self.layer:

@@ -133,9 +133,10 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(const uint8_t* __restri
 // ---- host ----------------------------------------------------------------------------------------
 
 // (Squares of 512 x 512 hold the codes of both orientations, their padding and the scales': whole groups of 512, and 64 rows.)
+// No squares, and no launch, if there is nothing to read or nowhere to write to.
 static Mx4Cast cast_of(const void* x, int64_t rows, int64_t cols, int64_t ld, const f8_mx4& o)
 {
-    const int64_t across = (cols + kMxGroup - 1) / kMxGroup, squares = rows > 0 && cols > 0 ? (rows + kMxGroup - 1) / kMxGroup * across : 0;
+    const int64_t across = (cols + kMxGroup - 1) / kMxGroup, squares = rows > 0 && cols > 0 && (o.q || o.q_t) ? (rows + kMxGroup - 1) / kMxGroup * across : 0;
     return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)squares, (int)across, (int)((squares + 7) / 8 * 128)};
 }
 static bool too_many(int64_t rows, int64_t cols) { return (rows / kMxGroup + 1) * (cols / kMxGroup + 1) > 0x2FFFFFF; }
@@ -153,8 +154,10 @@ static void launch_cast(const Mx4Cast& a, const Mx4Cast& b, hipStream_t st)
     if (a.blocks + b.blocks > 0) mx4_cast_kernel<<<(unsigned)(a.blocks + b.blocks), 256, 0, st>>>(a, b);
 }
 
-static f8_status check_codes(const f8_mx4* t, bool along_cols, bool along_rows)
+// The pairs that are needed are there (of an empty tensor none is: it has no bytes).
+static f8_status check_codes(const f8_mx4* t, int64_t rows, int64_t cols, bool along_cols, bool along_rows)
 {
+    if (rows == 0 || cols == 0) along_cols = along_rows = false;
     if (!t || (along_cols && (!t->q || !t->s)) || (along_rows && (!t->q_t || !t->s_t))) return F8_ERR_NULL;
     if ((t->q != nullptr) != (t->s != nullptr) || (t->q_t != nullptr) != (t->s_t != nullptr)) return F8_ERR_NULL;
     if (!aligned16(t->q) || !aligned16(t->s) || !aligned16(t->q_t) || !aligned16(t->s_t)) return F8_ERR_ALIGN;
@@ -189,9 +192,9 @@ size_t f8_mx4_workspace_bytes(int64_t M, int64_t K, int64_t N)
 f8_status f8_mx4_quantise(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, const f8_mx4* out, void* stream)
 {
     if (rows < 0 || cols < 0 || rows >= kMxMax || cols >= kMxMax || (cols % 16) || ld < cols || (ld % 8) || too_many(rows, cols)) return F8_ERR_SHAPE;
-    const f8_status s = check_codes(out, false, false);
+    const f8_status s = check_codes(out, rows, cols, false, false);
     if (s != F8_OK) return s;
-    if (!out->q && !out->q_t) return F8_ERR_NULL;
+    if (rows && cols && !out->q && !out->q_t) return F8_ERR_NULL;
     if (rows && cols && !x_bf16) return F8_ERR_NULL;
     if (!aligned16(x_bf16)) return F8_ERR_ALIGN;
     launch_cast(cast_of(x_bf16, rows, cols, ld, *out), Mx4Cast{}, (hipStream_t)stream);
@@ -225,8 +228,8 @@ f8_status f8_mx4_linear_fwd(const f8_mx4_desc* d, const void* X, const void* W, 
     if (!d || !saved) return F8_ERR_NULL;
     if (bad_desc(d)) return F8_ERR_SHAPE;
     const bool tokens = d->M <= kMxTokens && d->K <= kMxTokenK && !saved->x.q && !saved->x.q_t;  // X's codes are not wanted
-    f8_status s = check_codes(&saved->x, !tokens, false);
-    if (s != F8_OK || (s = check_codes(&saved->w, true, false)) != F8_OK) return s;
+    f8_status s = check_codes(&saved->x, d->M, d->K, !tokens, false);
+    if (s != F8_OK || (s = check_codes(&saved->w, d->N, d->K, true, false)) != F8_OK) return s;
     if (d->M && ((d->K && !X) || (d->N && !Y))) return F8_ERR_NULL;
     if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(workspace)) return F8_ERR_ALIGN;
     hipStream_t st = (hipStream_t)stream;
@@ -241,11 +244,12 @@ f8_status f8_mx4_linear_fwd(const f8_mx4_desc* d, const void* X, const void* W, 
 f8_status f8_mx4_linear_bwd(const f8_mx4_desc* d, const void* dY, const f8_mx4_saved* saved, void* dX, void* dW, void* workspace, size_t workspace_bytes_,
                             void* stream)
 {
-    if (!d || !saved || (!dX && !dW)) return F8_ERR_NULL;
+    if (!d || !saved) return F8_ERR_NULL;
     if (bad_desc(d)) return F8_ERR_SHAPE;
+    if (!dX && !dW && d->K && (d->M || d->N)) return F8_ERR_NULL;  // (gradients without elements may have no address)
     f8_mx4 dy = saved->dy;
-    f8_status s = check_codes(&dy, dX != nullptr, dW != nullptr);
-    if (s != F8_OK || (dX && (s = check_codes(&saved->w, false, true)) != F8_OK) || (dW && (s = check_codes(&saved->x, false, true)) != F8_OK)) return s;
+    f8_status s = check_codes(&dy, d->M, d->N, dX != nullptr, dW != nullptr);
+    if (s != F8_OK || (dX && (s = check_codes(&saved->w, d->N, d->K, false, true)) != F8_OK) || (dW && (s = check_codes(&saved->x, d->M, d->K, false, true)) != F8_OK)) return s;
     if (d->M && d->N && !dY) return F8_ERR_NULL;
     if (!aligned16(dY) || !aligned16(dX) || !aligned16(dW) || !aligned16(workspace)) return F8_ERR_ALIGN;
     if (!dX) dy.q = dy.s = nullptr;

@@ -736,7 +736,7 @@ size_t mx4_split_bytes(int64_t M, int64_t N, int64_t K)
 
 f8_status mx4_gemm_tokens(const Mx4Args& a, const uint16_t* X, hipStream_t st)
 {
-    if (a.M == 0 || a.N == 0) return last_launch_status();
+    if (a.M == 0 || a.N == 0 || a.K == 0) return mx4_gemm(a, nullptr, 0, st);
     switch (plan_product(a.M, a.N, a.K, 0, cu_count()).kind) {
         case Mx4Plan::kRows11: launch_rows<1, 1, 12, true>(a, st, X); break;
         case Mx4Plan::kRows14: launch_rows<1, 4, 3, true>(a, st, X); break;

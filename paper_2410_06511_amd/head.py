@@ -53,7 +53,7 @@ class OutputHead:
         s, M, D = self, self.M, self.D
         dynamic = s.state is None
         if s.layer:
-            norm = lambda: f8.layernorm(_bf16(x), _bf16(w["g"]), s.xn, _bf16(w["b"]) if s.norm_bias else None, eps=s.eps, mean=s.mean, rstd=s.rstd, amax_n=s.a_xn if dynamic else None,
+            norm = lambda: f8.layernorm(_bf16(x), _bf16(w["g"]).reshape(D), s.xn, _bf16(w["b"]).reshape(D) if s.norm_bias else None, eps=s.eps, mean=s.mean, rstd=s.rstd, amax_n=s.a_xn if dynamic else None,
                                         workspace=s.ws, stream=stream)
         else:
             norm = lambda: f8.rmsnorm(x, w["g"], s.eps, s.xn, s.rstd, s.a_xn if dynamic else None, s.ws if dynamic else None, stream)
@@ -70,7 +70,7 @@ class OutputHead:
         else:
             linear = lambda: f8.linear_bwd_scaled(s.desc, s.state, s.logits, s.saved, s.dxn, s.dW, s.ws, stream)
         if s.layer:
-            norm = ("final layernorm bwd", lambda: f8.layernorm_bwd(_bf16(x), _bf16(w["g"]), s.mean, s.rstd, s.dxn, s.dx, None, s.dg, s.db, None, s.ln_ws, stream), 0, 6 * M * D)
+            norm = ("final layernorm bwd", lambda: f8.layernorm_bwd(_bf16(x), _bf16(w["g"]).reshape(D), s.mean, s.rstd, s.dxn, s.dx, None, s.dg, s.db, None, s.ln_ws, stream), 0, 6 * M * D)
         else:
             norm = ("final rmsnorm bwd", lambda: f8.rmsnorm_bwd(x, w["g"], s.rstd, s.dxn, s.dx, s.dg, s.ws, stream), 0, 6 * M * D)
         return [loss, ("linear Wout bwd", linear, 4 * M * D * s.width, 0), norm]

@@ -141,6 +141,23 @@ def test_a_contraction_of_nothing():
         assert not D.any().item()
 
 
+@pytest.mark.parametrize("M,K,N", [(0, 64, 32), (3, 0, 48), (70, 0, 48), (3, 64, 0), (70, 64, 0), (0, 0, 16)])
+def test_linears_without_tokens_inputs_or_outputs(M, K, N):
+    """Empty tensors have no codes and no address; sums of nothing are zeros."""
+    X, W, dY = (torch.zeros(s, dtype=BF16, device="cuda") for s in ((M, K), (N, K), (M, N)))
+    for backward in (True, False):
+        saved = f8.MX4Saved(M, K, N, backward)
+        Y, dX, dW = (torch.full(s, 7.0, dtype=BF16, device="cuda") for s in ((M, N), (M, K), (N, K)))
+        f8.mx4_linear_fwd(X, W, Y, saved)
+        assert not Y.any().item()
+        if backward:
+            f8.mx4_linear_bwd(dY, saved, dX, dW)
+            assert not dX.any().item() and not dW.any().item()
+    t = f8.MX4Tensor(M, K, "qt")
+    f8.mx4_quantise(X, t)
+    f8.mx4_dequantise(t, X.clone())
+
+
 def test_what_is_not_a_number_stays_in_its_row():
     M, N, K = 40, 64, 512
     A, B = gen((M, K), 1).cuda(), gen((N, K), 2).cuda()
