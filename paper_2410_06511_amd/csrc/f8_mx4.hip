@@ -17,7 +17,16 @@ struct Mx4Cast {
     int rows, cols;
     uint8_t *q, *s, *q_t, *s_t;  // either orientation nullable
     int squares, squares_c, blocks;  // squares of 4 x 4 tiles, those side by side
+    bool once;                       // loads past the caches
 };
+// More elements than these are loaded past the caches: 8192 x 14336 along the rows 55 -> 46.5 us, both ways 86.8 -> 84.8, 14336 x
+// 4096 both ways 45.3 -> 42.1; but 8192 x 4096 along the rows 15.1 -> 16.1, across them 18.6 -> 22.3.
+constexpr int64_t kMxOnce = (int64_t)1 << 25;
+template <bool ONCE>
+__device__ inline uint4 load_eight(const uint16_t* x)
+{
+    return ONCE ? load_once(reinterpret_cast<const uint4*>(x)) : *reinterpret_cast<const uint4*>(x);
+}
 
 // Tiles of 128 x 128.  Along the rows four threads have a block of 32; for the other orientation the tile goes through LDS, where a
 // thread takes 32 rows of two columns.
@@ -37,12 +46,16 @@ __device__ inline void mx4_cast_tile(const Mx4Cast& p, int block, uint32_t (&til
     constexpr int PER = kMxTile * kMxTile / 8 / 256;
     const int k = t % 16, col = c0 + 8 * k;
     uint4 v[PER];
+    const auto load = [&](auto ONCE) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int row = r0 + 16 * i + t / 16;
-        v[i] = make_uint4(0, 0, 0, 0);
-        if (row < p.rows && col < p.cols) v[i] = *reinterpret_cast<const uint4*>(p.x + (int64_t)row * p.ld + col);
-    }
+        for (int i = 0; i < PER; ++i) {
+            const int row = r0 + 16 * i + t / 16;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (row < p.rows && col < p.cols) v[i] = load_eight<ONCE()>(p.x + (int64_t)row * p.ld + col);
+        }
+    };
+    if (p.once) load(std::true_type{});
+    else load(std::false_type{});
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int r = 16 * i + t / 16, row = r0 + r;
@@ -102,11 +115,15 @@ __global__ __launch_bounds__(256) void mx4_cast_rows_kernel(const Mx4Cast p, int
     const int g = (int)(w % groups), lane = threadIdx.x % kWave, col = g * kMxGroup + 8 * lane, b = lane / 4;
     const int64_t pitch = mx4_pitch(p.cols);
     uint4 v[ROWS];
+    const auto load = [&](auto ONCE) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        v[i] = make_uint4(0, 0, 0, 0);
-        if (row0 + i < p.rows && col < p.cols) v[i] = *reinterpret_cast<const uint4*>(p.x + (row0 + i) * p.ld + col);
-    }
+        for (int i = 0; i < ROWS; ++i) {
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (row0 + i < p.rows && col < p.cols) v[i] = load_eight<ONCE()>(p.x + (row0 + i) * p.ld + col);
+        }
+    };
+    if (ROWS > 1 && p.once) load(std::true_type{});
+    else load(std::false_type{});
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const uint32_t code = mx4_scale_of_quad(v[i]);
@@ -137,7 +154,8 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(const uint8_t* __restri
 static Mx4Cast cast_of(const void* x, int64_t rows, int64_t cols, int64_t ld, const f8_mx4& o)
 {
     const int64_t across = (cols + kMxGroup - 1) / kMxGroup, squares = rows > 0 && cols > 0 && (o.q || o.q_t) ? (rows + kMxGroup - 1) / kMxGroup * across : 0;
-    return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)squares, (int)across, (int)((squares + 7) / 8 * 128)};
+    return {(const uint16_t*)x, ld, (int)rows, (int)cols, o.q, o.s, o.q_t, o.s_t, (int)squares, (int)across, (int)((squares + 7) / 8 * 128),
+            rows * cols > kMxOnce};
 }
 static bool too_many(int64_t rows, int64_t cols) { return (rows / kMxGroup + 1) * (cols / kMxGroup + 1) > 0x2FFFFFF; }
 constexpr int64_t kFewWaves = 16384;

@@ -69,6 +69,27 @@ def test_quantise(rows, cols):
         assert np.array_equal(wide(out_t[:, :rows]), mo.rounded(wide(x).T)) and bool((out_t[:, rows:] == 7.0).all())
 
 
+def test_large_tensors_have_the_codes_of_their_parts():
+    """Tensors large enough to be loaded past the caches: the bits of small casts of parts of them, of which the test above is."""
+    rows, cols = 8256, 4112
+    x = (torch.randn((rows, cols), generator=torch.Generator("cuda").manual_seed(1), device="cuda") * 3).to(BF16)
+    both, along = f8.MX4Tensor(rows, cols, "qt"), f8.MX4Tensor(rows, cols, "q")
+    f8.mx4_quantise(x, both), f8.mx4_quantise(x, along)
+    assert torch.equal(both.q, along.q) and torch.equal(both.s, along.s)
+    at = lambda s, n: s.view(-1, (n + 63) // 64 * 64, 16)    # [group][row][16]
+    for r in range(0, rows, 1024):     # (a multiple of 64, as is what is left at the end)
+        part = x[r:r + 1024]
+        t = f8.MX4Tensor(part.shape[0], cols, "q")
+        f8.mx4_quantise(part, t)
+        assert torch.equal(t.q, both.q[r:r + 1024]) and torch.equal(at(t.s, part.shape[0]), at(both.s, rows)[:, r:r + part.shape[0]])
+    for c in range(0, cols, 1024):
+        part = x[:, c:c + 1024]
+        t = f8.MX4Tensor(rows, part.shape[1], "t")
+        f8.mx4_quantise(part, t)
+        n = (part.shape[1] + 63) // 64 * 64
+        assert torch.equal(t.q_t, both.q_t[c:c + 1024]) and torch.equal(at(t.s_t, part.shape[1]), at(both.s_t, cols)[:, c:c + n])
+
+
 def test_every_bf16_value():
     """Each of the 65536 patterns as an element below each of a set of scales, and as the largest of its block."""
     every = torch.arange(65536, dtype=torch.int32).to(torch.uint16).view(BF16)
