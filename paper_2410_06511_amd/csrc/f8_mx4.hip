@@ -19,8 +19,8 @@ struct Mx4Cast {
     int squares, squares_c, blocks;  // squares of 4 x 4 tiles, those side by side
     bool once;                       // loads past the caches
 };
-// More elements than these are loaded past the caches: 8192 x 14336 along the rows 55 -> 46.5 us, both ways 86.8 -> 84.8, 14336 x
-// 4096 both ways 45.3 -> 42.1; but 8192 x 4096 along the rows 15.1 -> 16.1, across them 18.6 -> 22.3.
+// More elements than these are loaded past the caches: 8192 x 14336 along the rows 46.5 us for 55, both ways 84.8 for 86.8, 14336 x
+// 4096 both ways 42.1 for 45.3; but 8192 x 4096 along the rows 16.1 for 15.1, across them 22.3 for 18.6.
 constexpr int64_t kMxOnce = (int64_t)1 << 25;
 template <bool ONCE>
 __device__ inline uint4 load_eight(const uint16_t* x)
@@ -87,13 +87,26 @@ __device__ inline void mx4_cast_tile(const Mx4Cast& p, int block, uint32_t (&til
         }
         turned[0][k] = make_uint4(lo[0], lo[1], lo[2], lo[3]), turned[1][k] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     }
+    // The four waves' codes of a column lie side by side: they meet in LDS, each wave's in the place of the rows that it alone has
+    // read, and four lanes write 64 bytes (16 bytes a lane, each to another line: 8192 x 14336 both ways 87.6 us for 82.2, across
+    // alone 72.8 for 65.1).
+    // Column c's piece at 16-byte word (c + 2 wave) % 128, so that a quad's four pieces and the next one's are in different banks.
+    uint4* const codes = reinterpret_cast<uint4*>(&tile[32 * wave][0]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int col = c0 + 2 * lane + h;
         const bool real = col < p.cols && rb * kMxBlock < p.rows;
         const uint32_t code = mx4_scale_of(turned[h]);
-        if (real) *reinterpret_cast<uint4*>(p.q_t + col * pitch_t + (int64_t)rb * 16) = mx4_encode(turned[h], code);
+        codes[(2 * lane + h + 2 * wave) % kMxTile] = mx4_encode(turned[h], code);
         if (col < srows_t && rb * kMxBlock < (p.rows + kMxGroup - 1) / kMxGroup * kMxGroup) p.s_t[mx4_scale_at(srows_t, col, rb)] = (uint8_t)(real ? code : 127);
+    }
+    __syncthreads();
+    const int piece = t % 4;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = t / 4 + 64 * i;
+        const uint4 o = reinterpret_cast<const uint4*>(&tile[32 * piece][0])[(c + 2 * piece) % kMxTile];
+        if (c0 + c < p.cols && r0 + 32 * piece < p.rows) *reinterpret_cast<uint4*>(p.q_t + (c0 + c) * pitch_t + (int64_t)(r0 / kMxBlock + piece) * 16) = o;
     }
 }
 
