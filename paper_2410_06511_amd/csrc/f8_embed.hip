@@ -8,12 +8,14 @@
 // The sort counts, for each token of a chunk of kChunk, how many of the chunk come before it: two instructions for each pair,
 // with the other token's id in a scalar register, in blocks that run beside those that fill the table with zeros.  Longer lists
 // are merged by pairs of sorted runs.
+// 16384 tokens of 4096 columns, 131072 rows of bf16, us: forward 52 (5.1 TB/s), sort and zeros 151 (7.1 TB/s), two merges 12, pieces 44
+// (their rows read once and written once: 5 TB/s), join 9.5.
 #include "f8_rows.hpp"
 
 namespace f8 {
 
 constexpr uint32_t kNoToken = 0xFFFFFFFFu;  // sorts behind every id
-constexpr int kChunk = 4096;                // tokens that are sorted by counting
+constexpr int kChunk = 4096;                // tokens that are sorted by counting (longer chunks cost more than a merge)
 constexpr int kSortBlock = 64;              // tokens that a block of the sort places: one a lane, its waves share the others
 constexpr int kSortWaves = 4;
 constexpr int64_t kEmbedMaxTokens = 1 << 28, kMaxFillBlocks = 1 << 23;

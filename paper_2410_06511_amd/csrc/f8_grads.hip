@@ -3,6 +3,7 @@
 // Bound by memory: the norm reads every element once, the scaling reads and writes it.  Squares and sums are taken in fp64: the
 // square of a bf16 or fp32 value is exact there and cannot overflow or vanish (fp32 loses gradients below 1e-19 and above 1e19),
 // at a quarter of the rate that the memory leaves room for.
+// One 8B block's gradients, 436 MB, us: norm 69 (6.3 TB/s), scaling 150 (5.8 TB/s); 216 tensors of 24 smaller blocks, 300 MB: 61 and 110.
 // The tensors' addresses and sizes come as kernel arguments, kTensors to a launch; a block has a range of the steps of kStep
 // elements of all of a launch's tensors.  Partial sums are added in a fixed order.
 #include "f8_device.hpp"

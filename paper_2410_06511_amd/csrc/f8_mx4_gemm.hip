@@ -8,6 +8,11 @@ namespace f8 {
 constexpr int kFp4 = 4;         // the instruction's format number
 constexpr int kMxStep = 2 * kBK;  // elements of a step: rows of 128 bytes, two instructions
 
+// Order of a row's eight 16-byte chunks in LDS: chunk c at c ^ mx4_swz(row).  A lane of an operand reads chunk fg or 4 + fg of row fr,
+// where the 8-bit products read 2 fg and 2 fg + 1, and their order costs conflicts here: 8192 x 4096 x 14336 183 us for 179, 300 x 4096
+// x 4096 10.3 for 9.9 (row & 6 as good to 0.5 %, row >> 1 & 3 as theirs).
+__device__ inline int mx4_swz(int row) { return row & 7; }
+
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 // (an fp4 operand is four registers; what the builtin's type has above them is never read)
@@ -42,7 +47,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
     // load l of a step: 8 rows of 128 bytes, A's rows first; lane: row lane / 8 of them, one 16-byte chunk.  Past the end of the
     // matrix or of the contraction it reads zeros.
     uint32_t off[2 * T];
-    const int row8 = lane >> 3, chunk = 16 * ((lane & 7) ^ swz(row8));  // (the swizzle looks at bits 1 and 2 of the row only)
+    const int row8 = lane >> 3, chunk = 16 * ((lane & 7) ^ mx4_swz(row8));
     static_for<2 * T>([&](auto L) {
         constexpr int l = L(), r = l < 2 * TA ? 8 * l : 8 * (l - 2 * TA);
         const int row = r + row8, left = l < 2 * TA ? p.M - m0 : p.N - n0;
@@ -126,7 +131,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
             int sa[TM];
 #pragma unroll
             for (int x = 0; x < T; ++x)
-                f[TM - TA + x] = fp4_operand(*reinterpret_cast<const v4i*>(st + (16 * x + fr) * kBK + 16 * ((4 * j + fg) ^ swz(fr))));
+                f[TM - TA + x] = fp4_operand(*reinterpret_cast<const v4i*>(st + (16 * x + fr) * kBK + 16 * ((4 * j + fg) ^ mx4_swz(fr))));
             if constexpr (TOKENS) {
                 const int kt = wave + NW * i;
                 const bool some = fr < p.M && kt * kBK + 64 * j + 16 * fg < pitch;
@@ -194,7 +199,7 @@ __global__ __launch_bounds__(512) void mx4_strip_kernel(const Mx4Args p, int til
 
     // Piece x of A: 8 rows (see mx4_rows_kernel) of the half x / (2 TM); wave w has the pieces w, w + 8, ..., of B the piece w of both
     // halves, of the scales (16 rows, A's first) w and w + 8, or the last one again.
-    const int row8 = lane >> 3, chunk = 16 * ((lane & 7) ^ swz(row8));
+    const int row8 = lane >> 3, chunk = 16 * ((lane & 7) ^ mx4_swz(row8));
     uint32_t a_off[A_LOADS], b_off, a_lds[A_LOADS], s_lds[S_LOADS];
     int a_begin[A_LOADS];  // of a lane's 16 bytes in a group's 256 of a row
     const uint8_t* s_base[S_LOADS];
@@ -241,7 +246,7 @@ __global__ __launch_bounds__(512) void mx4_strip_kernel(const Mx4Args p, int til
     for (int i = 0; i < TM; ++i) acc[i][0] = acc[i][1] = v4f{0.f, 0.f, 0.f, 0.f};
     static_for<STAGES - 1>([&](auto I) { request(I(), I()); });
     constexpr int kWait = (STAGES - 2) * LOADS;
-    const int at = quarter / 2 * HALF + fr * kBK + 16 * ((quarter % 2 * 4 + fg) ^ swz(fr));  // of a fragment's first rows in a stage
+    const int at = quarter / 2 * HALF + fr * kBK + 16 * ((quarter % 2 * 4 + fg) ^ mx4_swz(fr));  // of a fragment's first rows in a stage
     int stage = 0;
     for (int g = 0; g < groups; ++g) {
         // this wave's loads of the oldest group have landed, and behind the barrier everyone's; everyone is done with the group
@@ -297,6 +302,10 @@ __global__ __launch_bounds__(512) void mx4_strip_kernel(const Mx4Args p, int til
 //     a word for each fragment, whose byte the instruction picks.
 //   - M is any number: rows past the end read the last one again, and are not stored.
 // SPLITK: work item w is tile w % tiles, range w / tiles of the contraction, whose fp32 sums go to partial[range][M][N].
+// 8192 x 4096 x 16384 on random codes 206 us, 5.3 PFLOP/s, 8192 x 14336 x 4096 209 us, 4.6; on zeros 172 for the latter: the chip lowers
+// its clock under the switching of full tiles (register-only loops of the instruction reach 9.8 PFLOP/s on zeros, 7.1 to 7.4 on random
+// codes).  A tile costs 1.5 us for each 256 of the contraction and 5.5 us for its end; starting the workgroups apart from each other,
+// so that their stores do not meet, changes nothing (209 to 207).
 // RAGGED: the row's bytes are no multiple of 256: what lies past their end is loaded as zero, by the range check of buffer loads.
 template <int BM, int BN>
 struct Mx4Lds {
@@ -332,7 +341,7 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
 
     // ---- load stream: wave w fills rows [w * R / 4, ...) of each operand's tile in pieces of 8 rows; lane i lands at row i / 8,
     // physical chunk i % 8 of a piece, and fetches the logical chunk that belongs there
-    const int chunk = 16 * ((lane & 7) ^ swz(lane >> 3));  // (the swizzle looks at bits 1 and 2 of the row only)
+    const int chunk = 16 * ((lane & 7) ^ mx4_swz(lane >> 3));
     const uint8_t *a_base, *b_base, *sa_base, *sb_base;
     uint32_t a_off[A_LOADS], b_off[B_LOADS];
     int64_t left = 0;    // bytes of a row from the item's first on
@@ -413,7 +422,7 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p, int tile
 
     // ---- fragments: 16 rows, 256 elements; lane: row fr, blocks fg and 4 + fg
     const int a_rd = (wm * WM + fr) * kBK, b_rd = A_BYTES + (wn * WN + fr) * kBK;
-    const int c0 = 16 * (fg ^ swz(fr)), c1 = 16 * ((4 + fg) ^ swz(fr));
+    const int c0 = 16 * (fg ^ mx4_swz(fr)), c1 = 16 * ((4 + fg) ^ mx4_swz(fr));
     struct Frag {
         v4i k[2];
     };
