@@ -831,7 +831,8 @@ f8_status f8_linear_fwd_xq(const f8_linear_desc* d, const f8_scaling_state* stat
  * f8_mx4_linear_bwd: quantises dY [M, N] into saved->dy, then dX [M, K] = dY4 W4 from
  *   dy.q and w.q_t (blocks along N), and dW [N, K] = dY4^T X4 from dy.q_t and x.q_t
  *   (blocks along M).  dX or dW may be NULL, and the pairs for it.
- * M any number >= 0, K and N multiples of 16; all below 2^23.
+ * M any number >= 0, K and N multiples of 16; all below 2^23.  Tensors without
+ * elements need no address, codes or scales, and sums over nothing are zeros.
  */
 #define F8_MX4_TOKENS 4
 #define F8_MX4_TOKEN_K 16384

@@ -177,9 +177,9 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p, int tile
 
 // Tiles of 16 TM x 64 with one ring of STAGES groups (512 elements of each row, with their scales) for eight waves: whatever the
 // height of the tile, all of the LDS but one group is under way, with one barrier a group.  Wave w has all rows and 32 of the
-// columns, and of each group the quarter w % 4; the four quarters' sums meet in LDS at the end.  (The LDS reads are what takes
-// longest: with 16 columns and half of each group a wave reads A twice as often, 300 x 4096 x 4096 10.0 us.  mx4_rows_kernel has
-// a ring for each wave, which a tile of this size leaves two steps.)
+// columns, and of each group the quarter w % 4; the four quarters' sums meet in LDS at the end.  (With 16 columns and half of each
+// group a wave would read A twice as often; mx4_rows_kernel has a ring for each wave, which a tile of this size leaves two steps.)
+// 300 x 4096 x 4096 9.9 us (1.0 PFLOP/s), 300 x 14336 x 4096 19.7: a unit's ring of 110 KB takes 2.3 us to come.
 template <int TM, int STAGES>
 __global__ __launch_bounds__(512) void mx4_strip_kernel(const Mx4Args p, int tiles_m, int tiles_n)
 {
@@ -302,10 +302,10 @@ __global__ __launch_bounds__(512) void mx4_strip_kernel(const Mx4Args p, int til
 //     a word for each fragment, whose byte the instruction picks.
 //   - M is any number: rows past the end read the last one again, and are not stored.
 // SPLITK: work item w is tile w % tiles, range w / tiles of the contraction, whose fp32 sums go to partial[range][M][N].
-// 8192 x 4096 x 16384 on random codes 206 us, 5.3 PFLOP/s, 8192 x 14336 x 4096 209 us, 4.6; on zeros 172 for the latter: the chip lowers
-// its clock under the switching of full tiles (register-only loops of the instruction reach 9.8 PFLOP/s on zeros, 7.1 to 7.4 on random
-// codes).  A tile costs 1.5 us for each 256 of the contraction and 5.5 us for its end; starting the workgroups apart from each other,
-// so that their stores do not meet, changes nothing (209 to 207).
+// On random codes 16384^3 1585 us, 5.55 PFLOP/s, 8192 x 4096 x 14336 179 us, 5.4, 8192 x 14336 x 4096 207 us, 4.65; on zeros 18 to 20 %
+// less: the chip lowers its clock under the switching of full tiles (register-only loops of the instruction reach 9.8 PFLOP/s on zeros,
+// 7.1 to 7.4 on random codes).  A tile costs 1.5 us for each 256 of the contraction and 5.5 us for its end; starting the workgroups
+// apart from each other, so that their stores do not meet, changes nothing (209 to 207).
 // RAGGED: the row's bytes are no multiple of 256: what lies past their end is loaded as zero, by the range check of buffer loads.
 template <int BM, int BN>
 struct Mx4Lds {

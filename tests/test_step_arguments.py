@@ -20,7 +20,7 @@ def call(f, defaults, **change):
 
 EMBED = dict(ids=FAKE, M=5, table=FAKE, ldt=64, V=100, D=64, scale=1.0, out=FAKE, ldo=64, stream=None)
 EMBED_BWD = dict(ids=FAKE, M=5, dout=FAKE, lddo=64, V=100, D=64, scale=1.0, type=0, dtable=FAKE, ldt=64, ws=None, wb=0, stream=None)
-COMMON = [(SHAPE, dict(M=-1)), (SHAPE, dict(M=1 << 31)), (SHAPE, dict(V=-1)), (SHAPE, dict(V=1 << 31)), (SHAPE, dict(D=60)), (SHAPE, dict(D=-8)),
+COMMON = [(SHAPE, dict(M=-1)), (SHAPE, dict(M=1 << 31)), (SHAPE, dict(M=(1 << 28) + 1)), (SHAPE, dict(V=-1)), (SHAPE, dict(V=1 << 31)), (SHAPE, dict(D=60)), (SHAPE, dict(D=-8)),
           (SHAPE, dict(D=(1 << 20) + 8)), (SHAPE, dict(scale=INF)), (SHAPE, dict(scale=NAN)), (SHAPE, dict(ldt=56)), (SHAPE, dict(ldt=68)), (NULL, dict(ids=None)),
           (ALIGN, dict(ids=FAKE + 4))]
 
