@@ -67,6 +67,7 @@ SIZES = {
     "one": [1], "few": [7, 8, 9, 0, 1], "steps": [STEP - 1, STEP, STEP + 1, 3 * STEP + 5, 2 * STEP], "many": [(i * 37) % 300 for i in range(250)],
     "block": [6144 * 64, 64 * 64, 64 * 448, 64, 64], "large": [40_000_003, 17_000_000],
     "past the caches": [90_000_007, 50_000_001],
+    "launches": [(i * 53) % 9000 + 1 for i in range(600)],
 }
 
 
