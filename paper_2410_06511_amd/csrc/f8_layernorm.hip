@@ -4,7 +4,7 @@
 // Bound by memory: 4 bytes an element forward (8 with the sum), 6 backward (8 with the sum's gradient).  A row is held in
 // registers, so that the mean, the sum of squares around it and the result take one reading; both gains' sums run along in the
 // backward's one pass and are joined over the blocks by a second launch, in a fixed order.
-// 16384 x 8192 with a residual, us: forward 184, backward 180 (5.8 and 6.0 TB/s; a large copy 5.0); 8192 x 4096 40.5 and 54.5; 2001 x
+// 16384 x 8192 with a residual, us: forward 184, backward 180 (5.8 and 6.0 TB/s; a large copy 5.0); 8192 x 4096 40.5 and 50; 2001 x
 // 2816 without 7 and 16.
 #include "f8_rows.hpp"
 
@@ -12,7 +12,7 @@ namespace f8 {
 
 constexpr int kLnBlocks = 2048;  // of the forward with a maximum over n: one partial maximum each
 static_assert((size_t)kLnBlocks * sizeof(uint32_t) <= kMinWorkspaceBytes, "one partial per block fits the minimum workspace");
-constexpr int kLnBwdBlocks = 512;  // of the backward, each of which leaves a partial row of both sums
+constexpr int kLnBwdBlocks = 512;  // of the backward at most, each of which leaves a partial row of both sums
 constexpr int64_t kLnOnce = (int64_t)1 << 25;  // elements from which the backward loads past the caches
 
 struct LayerNormArgs {
@@ -268,7 +268,10 @@ static void with_grad_shape(int64_t dc, F&& f)
 static int bwd_blocks(int64_t M, int64_t D)
 {
     const int64_t slots = D / 8 <= 128 ? kWaveRows : 1, most = (M + slots - 1) / slots;
-    const int blocks = D / 8 > 512 ? kLnBwdBlocks / 2 : kLnBwdBlocks;
+    // Rows of seven waves and more: half as many, as few loads at a time are enough then and partial rows cost (8192 x 4096 49.6 us for
+    // 54.6, 300 x 4096 11.3 for 12.6, 16384 x 3584 82.5 for 84, 1000 x 8192 21.2 for 28.5; but 32768 x 2816 139 for 127, 16384 x 2048 63
+    // for 51).
+    const int blocks = D / 8 > 6 * kWave ? kLnBwdBlocks / 2 : kLnBwdBlocks;
     return (int)(most < blocks ? most : blocks);
 }
 
