@@ -639,7 +639,8 @@ size_t f8_residual_norm_bwd_workspace_bytes(int64_t M, int64_t D, int64_t gate_r
  * take no part.  dout [M, D] bf16; dtable [V, D] (pitch ldt in elements) bf16 or
  * fp32 as dtable_type says.  fp32 sums in the order of the tokens, in pieces of a
  * list of the tokens by id, then over the pieces: results are reproducible.
- * workspace: f8_embed_bwd_workspace_bytes (none needed without tokens).
+ * workspace: f8_embed_bwd_workspace_bytes (none needed without tokens), which is
+ * enough for fewer tokens and columns too.
  * 0 <= M <= 2^28, 0 <= V < 2^31; D and the pitches multiples of 8, D <= 2^20, M * D up to
  * 2^36 (f8_embed; whole multiples of 1024 for D); scale finite.
  * out and table, dout and dtable must not overlap.

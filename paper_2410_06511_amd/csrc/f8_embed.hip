@@ -300,6 +300,14 @@ static EmbedPlan plan_embed(int64_t M, int64_t D)
     e.bytes = kMinWorkspaceBytes + e.lists * e.list + (size_t)e.pieces * 2 * D * sizeof(float);
     return e;
 }
+// Enough for M tokens and for any number below: pieces get fewer where they get longer (9217 tokens have 922 of 10, 9216 have 1024 of
+// 9), so their number is taken as its bound for all up to M, of 8 tokens each and 1024 in all.
+static size_t embed_bytes(int64_t M, int64_t D)
+{
+    const EmbedPlan e = plan_embed(M, D);
+    const int64_t eights = (M + 7) / 8, most = eights < 1024 ? eights : 1024;
+    return e.bytes + (size_t)(most - e.pieces) * 2 * D * sizeof(float);
+}
 
 constexpr int64_t kEmbedMaxD = 1 << 20;
 static bool bad_size(int64_t M, int64_t V, int64_t D) { return M < 0 || M > kEmbedMaxTokens || V < 0 || V > 0x7FFFFFFF || D < 0 || D > kEmbedMaxD || (D % 8); }
@@ -314,7 +322,7 @@ extern "C" {
 size_t f8_embed_bwd_workspace_bytes(int64_t M, int64_t V, int64_t D)
 {
     if (bad_size(M, V, D)) return kMinWorkspaceBytes;
-    return plan_embed(M, D).bytes;
+    return embed_bytes(M, D);
 }
 
 f8_status f8_embed(const int64_t* ids, int64_t M, const void* table_bf16, int64_t ldt, int64_t V, int64_t D, float scale, void* out_bf16, int64_t ldo,

@@ -46,6 +46,18 @@ def test_embed_workspace():
         assert 2 * 4 * M <= size <= 8192 + 4 * (4 * M + 256) + (M // 8 + 1) * 2 * 512 * 4
 
 
+@pytest.mark.parametrize("D", [8, 1024, 4096])
+def test_a_workspace_for_the_longest_batch_serves_every_shorter_one(D):
+    """Its size grows with the tokens: around the steps of a piece's length (multiples of 1024) and of the lists (4096), and beyond."""
+    lengths = [0, 1, 7, 8, 9, 4095, 4096, 4097] + [1024 * i + k for i in range(7, 40) for k in (-1, 0, 1, 500)] + [70001, 1 << 20, (1 << 20) + 1, 1 << 28]
+    sizes = [f8.embed_bwd_workspace_bytes(M, 1000, D) for M in lengths]
+    assert sizes == sorted(sizes)
+    l = f8.lib()
+    for longest, M in ((8193, 8192), (10000, 9216), (20000, 8192)):   # (a table without rows: no launch, whose status is a GPU's)
+        room = f8.embed_bwd_workspace_bytes(longest, 0, D)
+        assert l.f8_embed_bwd(FAKE, M, FAKE, D, 0, D, 1.0, 0, None, D, FAKE, room, None) != WORKSPACE
+
+
 NORM = dict(x=FAKE, ldx=64, y=FAKE, ldy=64, M=5, D=64, g=FAKE, b=FAKE, eps=1e-5, h=FAKE, ldh=64, n=FAKE, ldn=64, mean=FAKE, rstd=FAKE, amax=FAKE, ws=None, wb=0,
             stream=None)
 NORM_BWD = dict(h=FAKE, ldh=64, g=FAKE, mean=FAKE, rstd=FAKE, dn=FAKE, lddn=64, dh=FAKE, lddh=64, M=5, D=64, dx=FAKE, lddx=64, dg=FAKE, db=FAKE, amax=FAKE, ws=None,
