@@ -695,7 +695,8 @@ struct Mx4Plan {
 };
 
 // Up to kMxTokens rows have their kernel by the columns alone, so that a product from bf16 has the bits of that from codes.
-static Mx4Plan plan_product(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int cus)
+// (Not static: the tests ask it which kernel a size is for.)
+Mx4Plan plan_product(int64_t M, int64_t N, int64_t K, size_t ws_bytes, int cus)
 {
     if (M <= kMxTokens && K > 0) return {N <= 16 * cus ? Mx4Plan::kRows11 : N <= 32 * cus ? Mx4Plan::kRows12 : Mx4Plan::kRows14, 1, 0};
     const auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };

@@ -111,8 +111,8 @@ def test_every_bf16_value():
 
 PRODUCTS = [(1, 16, 16), (1, 4096, 256), (1, 272, 4096), (3, 48, 48), (16, 64, 512), (17, 528, 1040), (32, 2048, 768), (33, 64, 4112), (64, 272, 2048), (65, 144, 80),
             (130, 80, 1552), (200, 512, 8192), (300, 1040, 528), (128, 256, 1024), (513, 784, 272), (1030, 1552, 1040), (2100, 528, 2064), (257, 4112, 512),
-            # tiles of 128 x 128, 256 x 128 and 256 x 256; whole rounds of these with the rest in smaller ones, by rows and by columns;
-            # ranges of the contraction; each with whole and with odd lengths
+            # tiles of 128 x 128 and 256 x 128, with whole and with odd lengths (a size for each kernel there is, tiles of 256 x 256 and
+            # ranges of the contraction among them: test_gpu_mx4_products.py)
             (2048, 2048, 1024), (2001, 2048, 528), (3000, 1552, 512), (2999, 1552, 1040), (4096, 4096, 512), (4000, 4096, 272), (4097, 4096, 1024), (4100, 4096, 80),
             (4090, 4112, 512), (4096, 4176, 560), (1500, 2000, 8192), (1501, 2000, 6160), (700, 3600, 12304)]
 
