@@ -733,7 +733,8 @@ size_t f8_layernorm_bwd_workspace_bytes(int64_t M, int64_t D);
  * backward: the two numbers above, and two for the teacher's term.
  * f8_distill_bwd: dlogits from d_loss and (nullable, with targets) d_logp, [M] fp32.
  * workspace of both forwards: f8_logits_workspace_bytes(M, V, top_k) bytes (top_k
- * 0 for f8_distill).  1 <= V <= 2^22; any M >= 0.  No atomics on results: they are reproducible.
+ * 0 for f8_distill; it may be more for fewer rows, which are shared by more blocks: for several
+ * M take the largest).  1 <= V <= 2^22; any M >= 0.  No atomics on results: they are reproducible.
  */
 size_t f8_logits_workspace_bytes(int64_t M, int64_t V, int64_t top_k);
 f8_status f8_token_logprobs(const void* logits_bf16, int64_t ld, int64_t M, int64_t V, float scale,

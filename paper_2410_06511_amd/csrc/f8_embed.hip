@@ -9,7 +9,8 @@
 // with the other token's id in a scalar register, in blocks that run beside those that fill the table with zeros.  Longer lists
 // are merged by pairs of sorted runs.
 // 16384 tokens of 4096 columns, 131072 rows of bf16, us: forward 52 (5.1 TB/s), sort and zeros 151 (7.1 TB/s), two merges 12, pieces 44
-// (their rows read once and written once: 5 TB/s), join 9.5.
+// (their rows read once and written once: 5 TB/s), join 9.5.  With a small table the launches have nothing to hide behind: 16384 tokens of
+// 1024 columns into 4000 rows 63 us in all, into 32000 rows 72.
 #include "f8_rows.hpp"
 
 namespace f8 {
@@ -77,8 +78,8 @@ struct SortArgs {
 };
 
 // Blocks [0, sort_blocks) place 64 tokens of a chunk each; the others fill the gradient with zeros, one word a thread: short blocks
-// that start in the order of their addresses write 6.8 TB/s, a block or two a unit that go on by the grid's width 5.2 to 5.8
-// (1 GB; 4 KB blocks 157 us, 8 KB 168, 16 KB 170 to 176, past the caches 164, 256 blocks of 512 threads 186, 2048 of 256 226).
+// that start in the order of their addresses write 6.8 TB/s, one to eight blocks a unit that go on by the grid's width 4.7 to 5.8
+// (1 GiB; 4 KB blocks 157 us, 8 KB 168, 16 KB 170 to 176, past the caches 164, 256 blocks of 512 threads 186, 2048 of 256 226).
 __global__ __launch_bounds__(kSortWaves* kWave) void embed_sort_kernel(const SortArgs p)
 {
     if ((int)blockIdx.x >= p.sort_blocks) {

@@ -4,8 +4,9 @@
 // Bound by memory: 4 bytes an element forward (8 with the sum), 6 backward (8 with the sum's gradient).  A row is held in
 // registers, so that the mean, the sum of squares around it and the result take one reading; both gains' sums run along in the
 // backward's one pass and are joined over the blocks by a second launch, in a fixed order.
-// 16384 x 8192 with a residual, us: forward 184, backward 180 (5.8 and 6.0 TB/s; a large copy 5.0); 8192 x 4096 40.5 and 50; 2001 x
-// 2816 without 7 and 16.
+// The mean is held in fp32, also for the backward: of r deviations, its rounding moves the differences by 2^-24 r deviations.
+// 16384 x 8192 with a residual, us: forward 181 to 185, backward 177 to 200 (5.8 and 5.4 to 6.0 TB/s; a large copy 5.0); 8192 x 4096
+// 40.5 to 53 (53 over sets of inputs that no cache holds) and 50; 2001 x 2816 without 7 and 16.
 #include "f8_rows.hpp"
 
 namespace f8 {
@@ -310,6 +311,7 @@ f8_status f8_layernorm(const void* x_bf16, int64_t ldx, const void* y_bf16, int6
             const int64_t b = (M + kRows - 1) / kRows;
             // rows in the order of the blocks' start read and write faster than rows at a stride of the grid (16384 x 8192 with a
             // residual 184 us for 198, 8192 x 4096 40.7 for 43); where each block leaves a maximum, there is room for so many
+            // (with the launch that joins the maxima 202 us for 185, 8192 x 4096 56 for 53, 2001 x 2816 without a residual 11.4 for 7.2)
             const int64_t most = amax_n ? kLnBlocks : 0x7FFFFFFF / threads;
             nb = (int)(b < most ? b : most);
             const auto kernel = y_bf16 ? layernorm_kernel<T(), U(), true> : layernorm_kernel<T(), U(), false>;

@@ -689,6 +689,13 @@ static void launch_tiles(const Mx4Args& a, int most, hipStream_t st)
 // x contraction; tiles of 16 x 16, 32 x 32, 64 x 64 strips, 96 x 64 strips, 128 x 128, 256 x 256):
 //   1 x 4096 x 4096      4.5   5.0   7.1   9.0  12.7  25.4        300 x 4096 x 4096    53.5  20.2  13.8  10.0  12.9  25.4
 //   1 x 14336 x 4096    14.6  10.7   8.6  10.3  16.9  27.2        1000 x 14336 x 4096   621   223  93.6  87.0  41.4  31.6
+// (tiles of 32 x 32, 64 x 32, strips of 64, 96 and 128 rows, 128 x 128, 256 x 128)
+//   40 x 4144 x 1040     6.6   4.9   5.2   6.0   6.8   7.2   9.4     1287 x 1200 x 1568  20.5  15.5  10.3  13.1   9.1   9.5  12.3
+//   64 x 4096 x 4096     5.6   6.7   7.5   9.4  10.9  11.8  15.4     2068 x 928 x 8192   45.4  33.1  21.3  28.4  19.2  22.3  28.1
+// Ranges of the contraction, with a workspace, against the best of the others: of 44 sizes that the estimates send there 40 gain, by 5 to
+// 46 % (468 x 5456 x 81696 in four 164 us for 305, 3976 x 480 x 65344 in eight 89 for 150, 1500 x 5024 x 87296 in two 294 for 370);
+// where the estimates are close some lose, up to 12 % (2048 x 2032 x 20480 in four 60 for 54, 3976 x 656 x 14336 41 for 38, 721 x 416
+// x 90624 in eight 69 for 64).
 struct Mx4Plan {
     enum Kind { kRows11, kRows12, kRows14, kRows22, kRows42, kStrip4, kStrip6, kStrip8, kQuarter, kHalf, kFull, kFullRows, kFullCols, kSplit } kind;
     int ranges, whole;  // kSplit: ranges of the contraction; kFullRows, kFullCols: tiles in whole rounds, launched on their own
